@@ -49,6 +49,10 @@ typedef int pdattn_status;
                                            outside [0, num_blocks)                                   */
 #define PDATTN_DEVICE_TIMEOUT      (-8) /* reported by pdattn_check(): a bounded wait inside a kernel
                                            gave up; that call's output is undefined                  */
+#define PDATTN_OUT_OF_PAGES        (-9) /* reported by pdattn_check(): pdattn_pages_reserve / _fork asked for
+                                           more pages than the pool holds; nothing was changed       */
+#define PDATTN_BAD_SEQUENCE       (-10) /* reported by pdattn_check(): a page operation was given a row it
+                                           cannot serve (out of range, not empty, named twice, too long) */
 
 typedef struct CUstream_st* pdattn_stream_t; /* a cudaStream_t */
 
@@ -216,6 +220,121 @@ pdattn_status pdattn_append_kv(const void* k_new, const void* v_new, void* k_cac
                                int num_kv_heads, int head_dim, int block_size, int max_blocks_per_seq,
                                int num_blocks, int64_t kv_block_stride, int64_t kv_head_stride,
                                int64_t kv_token_stride, void* workspace, pdattn_stream_t stream);
+
+/*
+ * Rotary positions fused with the KV append: the step between the projections and the attention of a layer, for
+ * prompts (Section 2.1: a rollout starts from a prompt) and for single tokens.  Token t of the batch belongs to the
+ * sequence s with cu_tokens[s] <= t < cu_tokens[s + 1]; the n_s new tokens of a sequence are the LAST n_s of its
+ * context_lens[s] tokens (the lengths count them already, as in pdattn_decode_multi; nothing is advanced here, so
+ * one set of lengths serves every layer of a step), so token t sits at
+ *   pos = context_lens[s] - cu_tokens[s + 1] + t.
+ * Every q and k head is rotated, pair by pair, i < rotary_dim / 2:
+ *   theta = pos * inv_freq[i],  x' = magnitude (x cos theta - y sin theta),  y' = magnitude (y cos theta + x sin theta)
+ * (x, y) = elements (i, i + rotary_dim / 2), or (2i, 2i + 1) with interleaved = 1; elements at or past rotary_dim pass
+ * through.  Scaled contexts (linear, base change, per-band, with an attention factor) are a matter of inv_freq and
+ * magnitude; magnitude is 1 for plain rotary positions.  The angle's product and its reduction are 64-bit.
+ *   q_out[t] = rotated q[t];  slot pos % block_size of page block_table[s, pos / block_size] = rotated k_new[t], v_new[t]
+ * Rounded once, to bf16 (nearest even).
+ *   - A token whose page id is outside [0, num_blocks), or that lies past its table row, is not written to the caches
+ *     (q_out is), and the error word of `workspace` (if given) is set.  A token before position 0 (n_s > context_lens[s])
+ *     is not written either, and its q_out is 0.  Rows of q_out at or past cu_tokens[num_seqs] are left as they were.
+ *   - Pages that are written must be owned by one sequence only.
+ *   - q_out may be q when q is dense (q_token_stride == num_q_heads * head_dim); no other overlap.
+ */
+typedef struct {
+  const void* q;                    /* DEVICE bf16 [num_tokens] rows of num_q_heads * head_dim, q_token_stride apart */
+  void* q_out;                      /* DEVICE bf16 [num_tokens, num_q_heads, head_dim], dense          */
+  const void* k_new;                /* DEVICE bf16 [num_tokens] rows of num_kv_heads * head_dim        */
+  const void* v_new;                /* DEVICE bf16, the same                                          */
+  int64_t q_token_stride, k_token_stride, v_token_stride;   /* elements, multiples of 8               */
+  void* k_cache;                    /* caches and strides as in pdattn_args                           */
+  void* v_cache;
+  const int32_t* block_table;       /* DEVICE int32 [num_seqs, max_blocks_per_seq]                    */
+  const int32_t* context_lens;      /* DEVICE int32 [num_seqs], new tokens included                   */
+  const int32_t* cu_tokens;         /* DEVICE int32 [num_seqs + 1], ascending from 0, or NULL: one new token per
+                                       sequence (num_tokens == num_seqs)                              */
+  const float* inv_freq;            /* DEVICE fp32 [rotary_dim / 2]                                   */
+  float magnitude;
+  int rotary_dim;                   /* a multiple of 16, at most head_dim                             */
+  int interleaved;                  /* 0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1)        */
+  int num_tokens;                   /* rows of q, k_new, v_new; at least cu_tokens[num_seqs]          */
+  int num_seqs, num_q_heads;        /* num_q_heads 0: only k and v (q, q_out may be NULL)             */
+  int num_kv_heads, head_dim, block_size, max_blocks_per_seq, num_blocks;
+  int64_t kv_block_stride, kv_head_stride, kv_token_stride;
+  void* workspace;                  /* DEVICE, may be NULL: its sticky error word (see pdattn_check)  */
+} pdattn_rope_args;
+pdattn_status pdattn_rope_append(const pdattn_rope_args* args, pdattn_stream_t stream);
+/* The same into the fp8 cache of pdattn_decode_fp8 (its layouts; the stride fields of the caches are ignored): rotated
+ * k and v divided by their KV head's scale and rounded once, to e4m3 (saturating). */
+pdattn_status pdattn_rope_append_fp8(const pdattn_rope_args* args, const float* k_scale, const float* v_scale,
+                                     pdattn_stream_t stream);
+
+/*
+ * Page bookkeeping on the device, for rollout groups that share their prompt's pages (Section 2.1): which pages of a pool
+ * are free and how often each is referenced.  The books are caller-owned device arrays; their state is a function of the
+ * references alone: free_list holds the pages without references in descending id (the lowest on top, at index
+ * free_count - 1), -1 at or past free_count.  One pool serves every layer of a model: the operations below change tables
+ * and books once and write the page copies they need as pairs, which pdattn_pages_copy then carries out per layer.
+ * Row s of the block table uses its first ceil(context_lens[s] / block_size) entries; an empty row has length 0.
+ * Every operation runs on `stream`, needs no host copies, and two of them on the same books must not overlap.
+ */
+typedef struct {
+  int32_t* ref_counts;              /* DEVICE int32 [num_blocks]                                      */
+  int32_t* free_list;               /* DEVICE int32 [num_blocks]                                      */
+  int32_t* free_count;              /* DEVICE int32 [1]                                               */
+  int num_blocks;
+} pdattn_page_pool;
+/* Scratch of the operations below; clear it with pdattn_workspace_init before its first use. */
+pdattn_status pdattn_pages_workspace_size(int num_blocks, int num_seqs, size_t* device_bytes);
+/* All pages free. */
+pdattn_status pdattn_pages_init(const pdattn_page_pool* pool, pdattn_stream_t stream);
+/*
+ * Pages for new_tokens[s] >= 0 (DEVICE int32 [num_seqs]) further tokens of every sequence, lowest ids first, in sequence
+ * order; context_lens[s] += new_tokens[s].  A sequence whose row cannot hold them (or with a negative number) is left as
+ * it is: PDATTN_BAD_SEQUENCE from pdattn_check.  Too few free pages for all the others: nothing changes,
+ * PDATTN_OUT_OF_PAGES.
+ */
+pdattn_status pdattn_pages_reserve(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
+                                   const int32_t* new_tokens, int num_seqs, int max_blocks_per_seq, int block_size,
+                                   void* workspace, size_t workspace_bytes, pdattn_stream_t stream);
+/*
+ * Row children[i] (empty) becomes a copy of row parents[i], i < num_forks <= num_seqs: it references the parent's whole pages
+ * and gets a page of its own, lowest free id first, for the tokens of a partial last one; the rest of the row is -1.  The
+ * pairs (copy_src, copy_dst) of those partial pages come first, in order of i; the rest of the num_forks entries is -1.
+ * Refused as a whole (books and rows as before, all pairs -1): a row out of range, a child that is not empty or named
+ * twice (PDATTN_BAD_SEQUENCE), too few free pages (PDATTN_OUT_OF_PAGES).  Lengths are those before the call.
+ */
+pdattn_status pdattn_pages_fork(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
+                                const int32_t* parents, const int32_t* children, int num_forks, int num_seqs,
+                                int max_blocks_per_seq, int block_size, int32_t* copy_src, int32_t* copy_dst,
+                                void* workspace, size_t workspace_bytes, pdattn_stream_t stream);
+/*
+ * Rows seqs[i], i < num_freed, give their references back and become empty (length 0, entries -1).  A row named twice, or
+ * empty already, is freed once; a row out of range is skipped (PDATTN_BAD_SEQUENCE).  An entry that is no page, or one
+ * without references, is reported as PDATTN_BAD_PAGE_INDEX and frees nothing.
+ */
+pdattn_status pdattn_pages_free(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
+                                const int32_t* seqs, int num_freed, int num_seqs, int max_blocks_per_seq, int block_size,
+                                void* workspace, size_t workspace_bytes, pdattn_stream_t stream);
+/*
+ * Makes the referenced pages dense: with n of them, those at or past n move, in ascending order, into the unreferenced
+ * pages below n, in ascending order.  Tables and books are renumbered; the pairs are written to copy_src / copy_dst
+ * [max_copies >= num_blocks / 2], the rest of which becomes -1.
+ */
+pdattn_status pdattn_pages_compact(const pdattn_page_pool* pool, int32_t* block_table, const int32_t* context_lens,
+                                   int num_seqs, int max_blocks_per_seq, int block_size, int32_t* copy_src,
+                                   int32_t* copy_dst, int max_copies, void* workspace, size_t workspace_bytes,
+                                   pdattn_stream_t stream);
+/*
+ * Copies page copy_src[i] to page copy_dst[i] of both caches, i < num_copies; a pair with a negative entry is skipped.  No page
+ * that is written may be another pair's (the pairs of fork and compact never are).  element_bytes 2: bf16 caches with the
+ * strides of pdattn_args; 1: the dense code pools of pdattn_decode_fp8 (strides ignored).  A page outside [0, num_blocks) is
+ * not copied and sets the error word of `workspace` (may be NULL).
+ */
+pdattn_status pdattn_pages_copy(void* k_cache, void* v_cache, const int32_t* copy_src, const int32_t* copy_dst,
+                                int num_copies, int num_kv_heads, int head_dim, int block_size, int num_blocks,
+                                int element_bytes, int64_t kv_block_stride, int64_t kv_head_stride,
+                                int64_t kv_token_stride, void* workspace, pdattn_stream_t stream);
 
 /*
  * Thread-local binding of the arguments the short form below does not carry: the block table's row

@@ -9,9 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libpdattn.so")
-SOURCES = ["pdattn_api.cu", "partition.cpp"]
-HEADERS = ["kernels.cuh", "common.cuh", "tile_bf16.cuh", "tile_fp8.cuh", "decode.cuh", "prefix_mma.cuh",
-           "prefix_umma.cuh", "aux_kernels.cuh", "partition.h", os.path.join("..", "..", "include", "pdattn.h")]
+SOURCES = ["pdattn_api.cu", "ops_api.cu", "host_common.cu", "partition.cpp"]
+HEADERS = ["kernels.cuh", "host_common.h", "common.cuh", "tile_bf16.cuh", "tile_fp8.cuh", "decode.cuh", "prefix_mma.cuh",
+           "prefix_umma.cuh", "aux_kernels.cuh", "rope.cuh", "pages.cuh", "partition.h", os.path.join("..", "..", "include", "pdattn.h")]
 
 
 def _nvcc() -> str:
@@ -50,7 +50,7 @@ def build(force: bool = False, verbose: bool = False, defines=(), out: str = Non
     os.makedirs(os.path.dirname(target), exist_ok=True)
     tmp = target + ".tmp%d" % os.getpid()
     cmd = [_nvcc(), "-std=c++17", "-O3", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-o", tmp]
+           "-t", "0", "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-o", tmp]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += ["-D" + d for d in defines]

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/pdattn.h"
+#include "host_common.h"
 #include "kernels.cuh"
 #include "prefix_umma.cuh"
 #include "partition.h"
@@ -19,7 +20,6 @@ namespace {
 
 using namespace pdattn;
 
-thread_local char g_cuda_err[256] = "";
 thread_local int g_last_launches = 0;
 thread_local cudaEvent_t g_prof_start = nullptr, g_prof_stop = nullptr;
 // Process-wide settings (the pdattn_set_* calls); everything that belongs to one call travels in a CallDesc.
@@ -52,7 +52,6 @@ struct CallDesc {
 };
 
 // What the launchers need to pick a kernel instantiation.
-struct DevInfo;
 struct LaunchCtx {
   int block_size;
   bool chain, probe, fp8;
@@ -69,13 +68,6 @@ struct Binding {
   const int32_t* context_lens_host = nullptr;
 };
 thread_local Binding g_bind;
-
-pdattn_status cuda_fail(const char* what, cudaError_t e) {
-  snprintf(g_cuda_err, sizeof g_cuda_err, "%s: %s", what, cudaGetErrorString(e));
-  return PDATTN_CUDA_ERROR;
-}
-
-inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // ---- workspace layout ----------------------------------------------------------------------
 struct WsLayout {
@@ -95,193 +87,7 @@ WsLayout ws_layout(int num_seqs, int G, int head_dim, int max_spans = MAX_SPANS)
   return w;
 }
 
-pdattn_status check_shape(int num_seqs, int Hq, int Hkv, int d, int bs) {
-  if (num_seqs < 0 || Hq <= 0 || Hkv <= 0 || d <= 0 || bs <= 0) return PDATTN_INVALID_ARG;
-  if (Hq % Hkv != 0) return PDATTN_INVALID_ARG;
-  if (d != 64 && d != 128) return PDATTN_UNSUPPORTED;
-  if (bs != 16 && bs != 32 && bs != 64) return PDATTN_UNSUPPORTED;
-  if (Hq / Hkv > 16) return PDATTN_UNSUPPORTED;
-  return PDATTN_OK;
-}
-
-// ---- per-device facts ------------------------------------------------------------------------
-struct DevInfo {
-  bool ready = false;
-  int sm_count = 0;
-  bool attr_set[2][2][3] = {};      // [D==128][NT==2][page size / 32]
-  bool probe_attr_set[2][2][3] = {};
-  bool chain_attr_set[2][2][3] = {};
-  bool win_attr_set[2][3] = {};     // [D==128][page size / 32]
-  bool fp8_attr_set[2][2][3] = {};  // [D==128][NT==2][page size / 32]
-  bool prefix_fp8_attr_set[2][3] = {};
-  bool prefix_attr_set[2][3] = {};  // [D==128][page size / 32]
-  bool prefix_umma_attr_set[2][3] = {};
-};
-constexpr int kMaxDevices = 64;
-DevInfo g_dev[kMaxDevices];
-std::mutex g_dev_mu;
-
-pdattn_status device_info(int* dev_out, DevInfo** info) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return cuda_fail("cudaGetDevice", e);
-  if (dev < 0 || dev >= kMaxDevices) return PDATTN_UNSUPPORTED;
-  DevInfo& di = g_dev[dev];
-  if (!di.ready) {
-    std::lock_guard<std::mutex> lk(g_dev_mu);
-    if (!di.ready) {
-      int sms = 0, major = 0;
-      e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-      if (e != cudaSuccess) return cuda_fail("cudaDeviceGetAttribute", e);
-      e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
-      if (e != cudaSuccess) return cuda_fail("cudaDeviceGetAttribute", e);
-      if (major != 10) {
-        snprintf(g_cuda_err, sizeof g_cuda_err, "libpdattn is built for sm_100a only (device has major %d)", major);
-        return PDATTN_CUDA_ERROR;
-      }
-      di.sm_count = sms;
-      di.ready = true;
-    }
-  }
-  *dev_out = dev;
-  *info = &di;
-  return PDATTN_OK;
-}
-
-// ---- TMA tensor maps ---------------------------------------------------------------------------
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn g_encode = nullptr;
-
-pdattn_status get_encode() {
-  if (g_encode) return PDATTN_OK;
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult qres;
-  cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
-  if (e != cudaSuccess) return cuda_fail("cudaGetDriverEntryPoint", e);
-  if (!fn || qres != cudaDriverEntryPointSuccess) {
-    snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled not available in this driver");
-    return PDATTN_CUDA_ERROR;
-  }
-  g_encode = reinterpret_cast<EncodeTiledFn>(fn);
-  return PDATTN_OK;
-}
-
-constexpr int kMapK8 = 81, kMapV8 = 82;   // "ranks" of the two fp8 views in make_map
-
-struct MapKey {
-  const void* ptr;
-  int d, bs, hkv, nb, rank;
-  int64_t sb, sh, st;
-  bool operator==(const MapKey& o) const {
-    return ptr == o.ptr && d == o.d && bs == o.bs && hkv == o.hkv && nb == o.nb && rank == o.rank && sb == o.sb &&
-           sh == o.sh && st == o.st;
-  }
-};
-struct MapCacheEntry {
-  bool valid = false;
-  MapKey key;
-  CUtensorMap map;
-};
-thread_local MapCacheEntry g_maps[16];
-thread_local int g_map_next = 0;
-
-// View of a cache as a tensor for TMA, 128-byte swizzle, zero fill out of bounds.
-//   rank 4: (dim, slot, kv head, page); one box = one 64-element column block of a page-head,
-//           [64, block_size, 1, 1]: head_dim / 64 copies per page-head.
-//   rank 5: (dim within column block, slot, column block, kv head, page); one box = a whole
-//           page-head [64, block_size, 2, 1, 1], landing in shared memory column block by column
-//           block exactly like two rank-4 boxes.  head_dim 128 only.
-pdattn_status make_map(const void* ptr, int d, int bs, int hkv, int nb, int64_t sb, int64_t sh, int64_t st, int rank,
-                       CUtensorMap* out) {
-  MapKey key{ptr, d, bs, hkv, nb, rank, sb, sh, st};
-  for (auto& e : g_maps)
-    if (e.valid && e.key == key) {
-      *out = e.map;
-      return PDATTN_OK;
-    }
-  pdattn_status s = get_encode();
-  if (s != PDATTN_OK) return s;
-  const cuuint64_t nbu = static_cast<cuuint64_t>(nb > 0 ? nb : 1);
-  CUtensorMap m;
-  CUresult r;
-  if (rank == kMapK8) {
-    // fp8 K pool [pages, kv heads, slots, d] of one-byte codes: one box = a page-head, [d, block_size, 1, 1]
-    cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(bs), static_cast<cuuint64_t>(hkv), nbu};
-    cuuint64_t strides[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(bs) * d,
-                             static_cast<cuuint64_t>(hkv) * bs * d};
-    cuuint32_t box[4] = {static_cast<cuuint32_t>(d), static_cast<cuuint32_t>(bs), 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    // rows of d bytes: 128-byte swizzle at head_dim 128, 64-byte swizzle at head_dim 64
-    r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(ptr), dims, strides, box, estr,
-                 CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  } else if (rank == kMapV8) {
-    // fp8 V pool [pages, kv heads, d, slots] (transposed inside a page): a page-head is d * block_size
-    // contiguous bytes and lands in shared memory in the same order, so it is described as rows of 256
-    // bytes (8 requests per box; rows of block_size bytes would be 128), no swizzle
-    const cuuint64_t rows = static_cast<cuuint64_t>(d) * bs / 256;
-    cuuint64_t dims[4] = {256, rows, static_cast<cuuint64_t>(hkv), nbu};
-    cuuint64_t strides[3] = {256, static_cast<cuuint64_t>(d) * bs, static_cast<cuuint64_t>(hkv) * d * bs};
-    cuuint32_t box[4] = {256, static_cast<cuuint32_t>(rows), 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(ptr), dims, strides, box, estr,
-                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  } else if (rank == 5) {
-    cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(bs), static_cast<cuuint64_t>(d / 64),
-                          static_cast<cuuint64_t>(hkv), nbu};
-    cuuint64_t strides[4] = {static_cast<cuuint64_t>(st) * 2, 128, static_cast<cuuint64_t>(sh) * 2,
-                             static_cast<cuuint64_t>(sb) * 2};
-    cuuint32_t box[5] = {64, static_cast<cuuint32_t>(bs), static_cast<cuuint32_t>(d / 64), 1, 1};
-    cuuint32_t estr[5] = {1, 1, 1, 1, 1};
-    r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(ptr), dims, strides, box, estr,
-                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  } else {
-    cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(bs), static_cast<cuuint64_t>(hkv), nbu};
-    cuuint64_t strides[3] = {static_cast<cuuint64_t>(st) * 2, static_cast<cuuint64_t>(sh) * 2,
-                             static_cast<cuuint64_t>(sb) * 2};
-    cuuint32_t box[4] = {64, static_cast<cuuint32_t>(bs), 1, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr,
-                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  }
-  if (r != CUDA_SUCCESS) {
-    snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled (rank %d) failed with CUresult %d", rank,
-             static_cast<int>(r));
-    return PDATTN_CUDA_ERROR;
-  }
-  MapCacheEntry& e = g_maps[g_map_next];
-  g_map_next = (g_map_next + 1) % 16;
-  e.valid = true;
-  e.key = key;
-  e.map = m;
-  *out = m;
-  return PDATTN_OK;
-}
-
 // ---- launches ------------------------------------------------------------------------------------
-// Launch that may begin while the kernel before it on the stream drains (programmatic dependent launch); the
-// kernel itself waits (griddepcontrol.wait) before it touches global memory.
-template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t stream, bool dependent,
-                             Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(block);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = dependent ? 1 : 0;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
-}
-
 template <int D, int NT, int BS>
 pdattn_status launch_bs(const CUtensorMap& mk, const CUtensorMap& mv, const DecodeParams& P, int grid, int combine_grid,
                      int n_spans_host, const LaunchCtx& lc) {
@@ -830,6 +636,8 @@ pdattn_status pdattn_check(void* workspace, pdattn_stream_t stream_) {
   e = cudaStreamSynchronize(stream);
   if (e != cudaSuccess) return cuda_fail("cudaStreamSynchronize", e);
   if (word & ERR_TIMEOUT) return PDATTN_DEVICE_TIMEOUT;
+  if (word & ERR_OUT_OF_PAGES) return PDATTN_OUT_OF_PAGES;
+  if (word & ERR_BAD_SEQUENCE) return PDATTN_BAD_SEQUENCE;
   if (word & ERR_TOO_LARGE) return PDATTN_UNSUPPORTED;   // the device-side planner refused the batch (tile count)
   return PDATTN_BAD_PAGE_INDEX;
 }
@@ -856,7 +664,7 @@ pdattn_status static_scratch_address(int dev, uint8_t** out) {
     cudaError_t e = cudaGetSymbolAddress(&p, g_static_scratch);
     if (e != cudaSuccess) return cuda_fail("cudaGetSymbolAddress(static scratch)", e);
     if (!p || (reinterpret_cast<uintptr_t>(p) & 255)) {
-      snprintf(g_cuda_err, sizeof g_cuda_err, "static scratch address is null or misaligned");
+      snprintf(cuda_error_text(), kCudaErrorTextBytes, "static scratch address is null or misaligned");
       return PDATTN_CUDA_ERROR;
     }
     g_static_scratch_ptr[dev] = p;
@@ -926,7 +734,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     wl = ws_layout(a->num_seqs, G * T, a->head_dim, n_ctas);
     need = scratch_need(wl, &off_start, &off_pfx);
     if (a->num_seqs > PDATTN_STATIC_SCRATCH_MAX_SEQS || need > PDATTN_STATIC_SCRATCH_BYTES) {
-      snprintf(g_cuda_err, sizeof g_cuda_err,
+      snprintf(cuda_error_text(), kCudaErrorTextBytes,
                "pdattn_decode_static_scratch: %d sequences need %zu bytes of scratch; the built-in array holds %u "
                "bytes and at most %d sequences",
                a->num_seqs, need, PDATTN_STATIC_SCRATCH_BYTES, PDATTN_STATIC_SCRATCH_MAX_SEQS);
@@ -1202,10 +1010,12 @@ const char* pdattn_status_string(pdattn_status st) {
     case PDATTN_CUDA_ERROR: return "CUDA error";
     case PDATTN_BAD_PAGE_INDEX: return "block_table entry out of range";
     case PDATTN_DEVICE_TIMEOUT: return "bounded wait expired inside a kernel";
+    case PDATTN_OUT_OF_PAGES: return "the page pool holds too few free pages";
+    case PDATTN_BAD_SEQUENCE: return "a page operation named a row it cannot serve";
     default: return "unknown status";
   }
 }
 
-const char* pdattn_last_cuda_error(void) { return g_cuda_err; }
+const char* pdattn_last_cuda_error(void) { return cuda_error_text(); }
 
 }  // extern "C"

@@ -25,6 +25,8 @@ NOT_BOUND = -5
 CUDA_ERROR = -6
 BAD_PAGE_INDEX = -7
 DEVICE_TIMEOUT = -8
+OUT_OF_PAGES = -9
+BAD_SEQUENCE = -10
 
 EXPORTS = [
     "pdattn_workspace_size", "pdattn_workspace_init", "pdattn_decode_ex", "pdattn_bind", "pdattn_decode",
@@ -36,6 +38,9 @@ EXPORTS = [
     "pdattn_decode_static_scratch", "pdattn_append_kv",
     "pdattn_grouped_workspace_size", "pdattn_decode_grouped",
     "pdattn_multi_workspace_size", "pdattn_decode_multi", "pdattn_decode_fp8", "pdattn_append_kv_fp8", "pdattn_decode_fp8_multi",
+    "pdattn_rope_append", "pdattn_rope_append_fp8",
+    "pdattn_pages_workspace_size", "pdattn_pages_init", "pdattn_pages_reserve", "pdattn_pages_fork", "pdattn_pages_free",
+    "pdattn_pages_compact", "pdattn_pages_copy",
 ]
 
 
@@ -61,6 +66,26 @@ class Args(ctypes.Structure):
         ("scale", ctypes.c_float),
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
     ]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [
+        ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p),
+        ("q_token_stride", ctypes.c_int64), ("k_token_stride", ctypes.c_int64), ("v_token_stride", ctypes.c_int64),
+        ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+        ("context_lens", ctypes.c_void_p), ("cu_tokens", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p),
+        ("magnitude", ctypes.c_float), ("rotary_dim", ctypes.c_int), ("interleaved", ctypes.c_int),
+        ("num_tokens", ctypes.c_int), ("num_seqs", ctypes.c_int), ("num_q_heads", ctypes.c_int),
+        ("num_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("block_size", ctypes.c_int),
+        ("max_blocks_per_seq", ctypes.c_int), ("num_blocks", ctypes.c_int),
+        ("kv_block_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64), ("kv_token_stride", ctypes.c_int64),
+        ("workspace", ctypes.c_void_p),
+    ]
+
+
+class PoolArgs(ctypes.Structure):
+    _fields_ = [("ref_counts", ctypes.c_void_p), ("free_list", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+                ("num_blocks", ctypes.c_int)]
 
 
 class Plan(ctypes.Structure):
@@ -107,6 +132,16 @@ def lib():
         L.pdattn_append_kv_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
         L.pdattn_append_kv.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i64, i64, i64, vp, vp]
         L.pdattn_check.argtypes = [vp, vp]
+        L.pdattn_rope_append.argtypes = [ctypes.POINTER(RopeArgs), vp]
+        L.pdattn_rope_append_fp8.argtypes = [ctypes.POINTER(RopeArgs), vp, vp, vp]
+        pool = ctypes.POINTER(PoolArgs)
+        L.pdattn_pages_workspace_size.argtypes = [i32, i32, ctypes.POINTER(sz)]
+        L.pdattn_pages_init.argtypes = [pool, vp]
+        L.pdattn_pages_reserve.argtypes = [pool, vp, vp, vp, i32, i32, i32, vp, sz, vp]
+        L.pdattn_pages_fork.argtypes = [pool, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.pdattn_pages_free.argtypes = [pool, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]
+        L.pdattn_pages_compact.argtypes = [pool, vp, vp, i32, i32, i32, vp, vp, i32, vp, sz, vp]
+        L.pdattn_pages_copy.argtypes = [vp] * 4 + [i32] * 6 + [i64] * 3 + [vp, vp]
         L.pdattn_profile_events.argtypes = [vp, vp]
         L.pdattn_gather_probe.argtypes = [ctypes.POINTER(Args), vp]
         L.pdattn_stream_read_probe.argtypes = [vp, sz, vp, vp]
@@ -387,6 +422,242 @@ def append_kv(k_new, v_new, k_cache, v_cache, block_table, context_lens, workspa
                                 workspace.data_ptr() if workspace is not None else None, _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, "pdattn_append_kv")
+    return st
+
+
+def _ptr(t) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _expect(where: str, dtype, *tensors):
+    """dtype and device checks of the tensors a call takes (None is passed over): the library sees plain pointers."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise TypeError(f"{where}: a tensor of {dtype} is wanted, got {t.dtype}")
+        if t.device.type != "cuda" or t.device.index != here:
+            raise ValueError(f"{where}: a tensor lives on {t.device}, the current device is cuda:{here}")
+
+
+def _dense(where: str, *tensors):
+    for t in tensors:
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{where}: a dense tensor is wanted, got strides {t.stride()} for shape {tuple(t.shape)}")
+
+
+def _same_cache(where: str, k_cache, v_cache):
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1:
+        raise ValueError(f"{where}: k_cache and v_cache need the same shape and strides, head_dim contiguous")
+
+
+def _code_pools(where: str, k8, v8, k_scale, v_scale):
+    NB, Hkv, bs, d = k8.shape
+    _expect(where, torch.uint8, k8, v8)
+    _expect(where, torch.float32, k_scale, v_scale)
+    _dense(where, k8, v8, k_scale, v_scale)
+    if tuple(v8.shape) != (NB, Hkv, d, bs) or k_scale.numel() != Hkv or v_scale.numel() != Hkv:
+        raise ValueError(f"{where}: code pools {tuple(k8.shape)} and {tuple(v8.shape)} with {k_scale.numel()} and "
+                         f"{v_scale.numel()} scales do not belong together")
+
+
+def _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, cu_tokens,
+               rotary_dim, interleaved, magnitude, workspace) -> RopeArgs:
+    N, Hkv, d = k_new.shape
+    NB, bs = k_cache.shape[0], k_cache.shape[2]
+    Hq = 0 if q is None else q.shape[1]
+    _expect(where, torch.bfloat16, q, q_out, k_new, v_new)
+    _expect(where, torch.int32, block_table, context_lens, cu_tokens)
+    _expect(where, torch.float32, inv_freq)
+    _dense(where, q_out, block_table, context_lens, cu_tokens, inv_freq)
+    for t in (q, k_new, v_new):
+        if t is not None and N and (t.shape[0] != N or t.shape[2] != d or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
+            raise ValueError(f"{where}: rows of dense heads are wanted, got strides {t.stride()} for shape {tuple(t.shape)}")
+    S = context_lens.numel()
+    rotary = d if rotary_dim is None else int(rotary_dim)
+    if (v_new.shape != k_new.shape or tuple(k_cache.shape[1::2]) != (Hkv, d) or block_table.shape[0] != S
+            or (cu_tokens is not None and cu_tokens.numel() != S + 1) or inv_freq.numel() * 2 != rotary
+            or (q is not None and (q_out is None or tuple(q_out.shape) != tuple(q.shape)))):
+        raise ValueError(f"{where}: shapes do not belong together")
+    a = RopeArgs()
+    a.q, a.q_out, a.k_new, a.v_new = _ptr(q), _ptr(q_out) if q is not None else None, k_new.data_ptr(), v_new.data_ptr()
+    a.q_token_stride = 0 if q is None else q.stride(0) if N > 1 else Hq * d
+    a.k_token_stride, a.v_token_stride = (k_new.stride(0), v_new.stride(0)) if N > 1 else (Hkv * d, Hkv * d)
+    a.k_cache, a.v_cache, a.block_table = k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr()
+    a.context_lens, a.cu_tokens, a.inv_freq = context_lens.data_ptr(), _ptr(cu_tokens), inv_freq.data_ptr()
+    a.magnitude, a.rotary_dim, a.interleaved = float(magnitude), rotary, int(bool(interleaved))
+    a.num_tokens, a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = N, S, Hq, Hkv, d, bs
+    a.max_blocks_per_seq, a.num_blocks = block_table.shape[1], NB
+    a.workspace = _ptr(workspace)
+    return a
+
+
+def rope_append(q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, *, cu_tokens=None,
+                rotary_dim=None, interleaved: bool = False, magnitude: float = 1.0, workspace=None, stream=None,
+                check: bool = True) -> int:
+    """pdattn_rope_append: rotate q ([N, Hq, d], rows of any token stride; None: only k and v) into q_out and k_new into
+    the paged cache beside v_new ([N, Hkv, d]).  context_lens counts the new tokens; cu_tokens [S + 1] (None: one new
+    token per sequence)."""
+    where = "pdattn_rope_append"
+    _expect(where, torch.bfloat16, k_cache, v_cache)
+    _same_cache(where, k_cache, v_cache)
+    a = _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, cu_tokens,
+                   rotary_dim, interleaved, magnitude, workspace)
+    a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = k_cache.stride(0), k_cache.stride(1), k_cache.stride(2)
+    st = lib().pdattn_rope_append(ctypes.byref(a), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def rope_append_fp8(q, k_new, v_new, q_out, k8, v8, k_scale, v_scale, block_table, context_lens, inv_freq, *,
+                    cu_tokens=None, rotary_dim=None, interleaved: bool = False, magnitude: float = 1.0, workspace=None,
+                    stream=None, check: bool = True) -> int:
+    """pdattn_rope_append_fp8: rope_append into the e4m3 code pools of decode_fp8."""
+    where = "pdattn_rope_append_fp8"
+    _code_pools(where, k8, v8, k_scale, v_scale)
+    a = _rope_args(where, q, k_new, v_new, q_out, k8, v8, block_table, context_lens, inv_freq, cu_tokens, rotary_dim,
+                   interleaved, magnitude, workspace)
+    st = lib().pdattn_rope_append_fp8(ctypes.byref(a), k_scale.data_ptr(), v_scale.data_ptr(), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+class PagePool:
+    """The books of a page pool (pdattn_page_pool): int32 device tensors ref_counts [num_blocks], free_list [num_blocks],
+    free_count [1]."""
+
+    def __init__(self, ref_counts, free_list, free_count):
+        _expect("PagePool", torch.int32, ref_counts, free_list, free_count)
+        _dense("PagePool", ref_counts, free_list, free_count)
+        if free_list.numel() != ref_counts.numel() or free_count.numel() != 1:
+            raise ValueError("PagePool: ref_counts and free_list have one entry per page, free_count has one")
+        self.ref_counts, self.free_list, self.free_count = ref_counts, free_list, free_count
+        self.num_blocks = ref_counts.numel()
+        self.args = PoolArgs(ref_counts.data_ptr(), free_list.data_ptr(), free_count.data_ptr(), self.num_blocks)
+
+    @classmethod
+    def create(cls, num_blocks: int, device="cuda", stream=None) -> "PagePool":
+        """A pool whose pages are all free."""
+        pool = cls(*(torch.empty(n, dtype=torch.int32, device=device) for n in (num_blocks, num_blocks, 1)))
+        st = lib().pdattn_pages_init(ctypes.byref(pool.args), _stream_ptr(stream))
+        if st != OK:
+            raise PdattnError(st, "pdattn_pages_init")
+        return pool
+
+
+def pages_workspace_size(num_blocks: int, num_seqs: int) -> int:
+    n = ctypes.c_size_t(0)
+    st = lib().pdattn_pages_workspace_size(num_blocks, num_seqs, ctypes.byref(n))
+    if st != OK:
+        raise PdattnError(st, "pdattn_pages_workspace_size")
+    return n.value
+
+
+def alloc_pages_workspace(num_blocks: int, num_seqs: int, device="cuda", stream=None):
+    n = pages_workspace_size(num_blocks, num_seqs)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    st = lib().pdattn_workspace_init(ws.data_ptr(), n, _stream_ptr(stream))
+    if st != OK:
+        raise PdattnError(st, "pdattn_workspace_init")
+    return ws
+
+
+def _pages_check(where, block_table, context_lens, *lists):
+    _expect(where, torch.int32, block_table, context_lens, *lists)
+    _dense(where, block_table, context_lens, *lists)
+    if block_table.dim() != 2 or context_lens.numel() != block_table.shape[0]:
+        raise ValueError(f"{where}: block_table [S, MB] and context_lens [S] do not belong together")
+
+
+def pages_reserve(pool: PagePool, block_table, context_lens, new_tokens, block_size: int, workspace, stream=None,
+                  check: bool = True) -> int:
+    """pdattn_pages_reserve: pages for new_tokens[s] further tokens of every sequence; context_lens advances (in place)."""
+    where = "pdattn_pages_reserve"
+    _pages_check(where, block_table, context_lens, new_tokens)
+    S, MB = block_table.shape
+    if new_tokens.numel() != S:
+        raise ValueError(f"{where}: new_tokens has one entry per row")
+    st = lib().pdattn_pages_reserve(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(),
+                                    new_tokens.data_ptr(), S, MB, block_size, workspace.data_ptr(), workspace.numel(),
+                                    _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def pages_fork(pool: PagePool, block_table, context_lens, parents, children, copy_src, copy_dst, block_size: int,
+               workspace, stream=None, check: bool = True) -> int:
+    """pdattn_pages_fork: the empty rows children[i] become copies of the rows parents[i]; the partial pages to copy are
+    written to (copy_src, copy_dst)."""
+    where = "pdattn_pages_fork"
+    _pages_check(where, block_table, context_lens, parents, children, copy_src, copy_dst)
+    n = parents.numel()
+    if children.numel() != n or copy_src.numel() < n or copy_dst.numel() < n:
+        raise ValueError(f"{where}: {n} parents, {children.numel()} children, room for {copy_src.numel()} and {copy_dst.numel()} copies")
+    S, MB = block_table.shape
+    st = lib().pdattn_pages_fork(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(), parents.data_ptr(),
+                                 children.data_ptr(), n, S, MB, block_size, copy_src.data_ptr(), copy_dst.data_ptr(),
+                                 workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def pages_free(pool: PagePool, block_table, context_lens, seqs, block_size: int, workspace, stream=None,
+               check: bool = True) -> int:
+    """pdattn_pages_free: rows seqs give their pages back and become empty."""
+    where = "pdattn_pages_free"
+    _pages_check(where, block_table, context_lens, seqs)
+    S, MB = block_table.shape
+    st = lib().pdattn_pages_free(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(), seqs.data_ptr(),
+                                 seqs.numel(), S, MB, block_size, workspace.data_ptr(), workspace.numel(),
+                                 _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def pages_compact(pool: PagePool, block_table, context_lens, copy_src, copy_dst, block_size: int, workspace, stream=None,
+                  check: bool = True) -> int:
+    """pdattn_pages_compact: renumber the referenced pages densely; the moves are written to (copy_src, copy_dst)."""
+    where = "pdattn_pages_compact"
+    _pages_check(where, block_table, context_lens, copy_src, copy_dst)
+    if copy_src.numel() != copy_dst.numel():
+        raise ValueError(f"{where}: copy_src and copy_dst have the same length")
+    S, MB = block_table.shape
+    st = lib().pdattn_pages_compact(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(), S, MB, block_size,
+                                    copy_src.data_ptr(), copy_dst.data_ptr(), copy_src.numel(), workspace.data_ptr(),
+                                    workspace.numel(), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def pages_copy(k_cache, v_cache, copy_src, copy_dst, workspace=None, stream=None, check: bool = True) -> int:
+    """pdattn_pages_copy: page copy_src[i] to page copy_dst[i] in both caches ([page, kv_head, slot, dim] bf16, or the
+    uint8 code pools of decode_fp8)."""
+    where = "pdattn_pages_copy"
+    _expect(where, torch.int32, copy_src, copy_dst)
+    _dense(where, copy_src, copy_dst)
+    if copy_src.numel() != copy_dst.numel():
+        raise ValueError(f"{where}: copy_src and copy_dst have the same length")
+    NB, Hkv, bs, d = k_cache.shape
+    if k_cache.dtype == torch.uint8:
+        _expect(where, torch.uint8, k_cache, v_cache)
+        _dense(where, k_cache, v_cache)
+        if tuple(v_cache.shape) != (NB, Hkv, d, bs):
+            raise ValueError(f"{where}: code pools {tuple(k_cache.shape)} and {tuple(v_cache.shape)} do not belong together")
+    else:
+        _expect(where, torch.bfloat16, k_cache, v_cache)
+        _same_cache(where, k_cache, v_cache)
+    st = lib().pdattn_pages_copy(k_cache.data_ptr(), v_cache.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(),
+                                 copy_src.numel(), Hkv, d, bs, NB, k_cache.element_size(), k_cache.stride(0),
+                                 k_cache.stride(1), k_cache.stride(2), _ptr(workspace), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
     return st
 
 

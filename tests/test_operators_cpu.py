@@ -1,0 +1,104 @@
+"""Refusals of the operators around the decode step, without a GPU: every bad argument is answered before any CUDA call."""
+import ctypes
+
+import pytest
+
+from paper_2607_09207_b200 import build as pd_build
+from paper_2607_09207_b200 import pdattn
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    pd_build.build()
+
+
+P = 0x10000      # an aligned address that no call may touch
+
+
+def rope(**kw):
+    a = pdattn.RopeArgs()
+    for f in ("q", "q_out", "k_new", "v_new", "k_cache", "v_cache", "block_table", "context_lens", "cu_tokens", "inv_freq"):
+        setattr(a, f, P)
+    a.q_out = 2 * P
+    a.q_token_stride, a.k_token_stride, a.v_token_stride = 256, 128, 128
+    a.magnitude, a.rotary_dim, a.interleaved = 1.0, 64, 0
+    a.num_tokens, a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = 8, 3, 4, 2, 64, 16
+    a.max_blocks_per_seq, a.num_blocks = 4, 12
+    a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = 2048, 1024, 64
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_rope_append_refusals(fp8):
+    L = pdattn.lib()
+
+    def call(**kw):
+        a = rope(**kw)
+        return L.pdattn_rope_append_fp8(ctypes.byref(a), P, P, None) if fp8 else L.pdattn_rope_append(ctypes.byref(a), None)
+    assert L.pdattn_rope_append(None, None) == pdattn.INVALID_ARG
+    assert call(num_tokens=0) == pdattn.OK                                       # nothing to do
+    for kw in (dict(num_tokens=-1), dict(num_seqs=0), dict(num_seqs=-1), dict(num_kv_heads=0), dict(num_q_heads=-1),
+               dict(rotary_dim=0), dict(rotary_dim=80), dict(interleaved=2), dict(k_new=None), dict(v_new=None),
+               dict(k_cache=None), dict(v_cache=None), dict(block_table=None), dict(context_lens=None), dict(inv_freq=None),
+               dict(q=None), dict(q_out=None), dict(cu_tokens=None), dict(max_blocks_per_seq=0), dict(num_blocks=0),
+               dict(q_token_stride=248), dict(k_token_stride=120), dict(v_token_stride=120),
+               dict(q_out=P, q_token_stride=512)):
+        assert call(**kw) == pdattn.INVALID_ARG, kw
+    for kw in (dict(head_dim=96), dict(block_size=8), dict(rotary_dim=24), dict(q_token_stride=260), dict(k_token_stride=132)):
+        assert call(**kw) == pdattn.UNSUPPORTED, kw
+    for kw in (dict(q=P + 2), dict(q_out=P + 8), dict(k_new=P + 4), dict(v_new=P + 8), dict(k_cache=P + 8), dict(v_cache=P + 2)):
+        assert call(**kw) == pdattn.MISALIGNED, kw
+    if fp8:
+        a = rope()
+        assert L.pdattn_rope_append_fp8(ctypes.byref(a), None, P, None) == pdattn.INVALID_ARG
+        assert L.pdattn_rope_append_fp8(ctypes.byref(a), P, None, None) == pdattn.INVALID_ARG
+    else:
+        assert call(kv_block_stride=0) == pdattn.INVALID_ARG and call(kv_token_stride=32) == pdattn.INVALID_ARG
+        assert call(kv_head_stride=1028) == pdattn.UNSUPPORTED
+
+
+def test_pages_refusals():
+    L = pdattn.lib()
+    n = pdattn.pages_workspace_size(12, 3)
+    assert n % 256 == 0 and pdattn.pages_workspace_size(100000, 3) > n
+    for bad in ((0, 3), (12, -1)):
+        with pytest.raises(pdattn.PdattnError):
+            pdattn.pages_workspace_size(*bad)
+    good = pdattn.PoolArgs(P, P, P, 12)
+
+    def calls(pool=good, table=P, lens=P, a=P, b=P, src=P, dst=P, S=3, MB=4, bs=16, n_fork=2, cap=6, ws=P, nb=n):
+        p = ctypes.byref(pool) if pool is not None else None
+        return [L.pdattn_pages_reserve(p, table, lens, a, S, MB, bs, ws, nb, None),
+                L.pdattn_pages_fork(p, table, lens, a, b, n_fork, S, MB, bs, src, dst, ws, nb, None),
+                L.pdattn_pages_free(p, table, lens, a, 2, S, MB, bs, ws, nb, None),
+                L.pdattn_pages_compact(p, table, lens, S, MB, bs, src, dst, cap, ws, nb, None)]
+    for kw in (dict(pool=None), dict(pool=pdattn.PoolArgs(None, P, P, 12)), dict(pool=pdattn.PoolArgs(P, None, P, 12)),
+               dict(pool=pdattn.PoolArgs(P, P, None, 12)), dict(pool=pdattn.PoolArgs(P, P, P, 0)), dict(table=None),
+               dict(lens=None), dict(S=-1), dict(MB=0), dict(bs=0), dict(ws=None)):
+        assert calls(**kw) == [pdattn.INVALID_ARG] * 4, kw
+    assert calls(bs=24) == [pdattn.UNSUPPORTED] * 4
+    assert calls(ws=P + 64) == [pdattn.MISALIGNED] * 4
+    assert calls(nb=n - 1) == [pdattn.WORKSPACE_TOO_SMALL] * 4
+    assert calls(a=None)[:3] == [pdattn.INVALID_ARG] * 3
+    assert calls(b=None)[1] == calls(src=None)[1] == calls(dst=None)[1] == calls(n_fork=4)[1] == calls(n_fork=-1)[1] == pdattn.INVALID_ARG
+    assert calls(cap=5)[3] == calls(src=None)[3] == calls(dst=None)[3] == pdattn.INVALID_ARG
+    assert L.pdattn_pages_reserve(ctypes.byref(good), None, None, None, 0, 4, 16, P, n, None) == pdattn.OK
+    assert L.pdattn_pages_fork(ctypes.byref(good), P, P, None, None, 0, 3, 4, 16, None, None, P, n, None) == pdattn.OK
+    assert L.pdattn_pages_init(None, None) == pdattn.INVALID_ARG
+
+    def copy(k=P, v=P, src=P, dst=P, n=4, H=2, d=64, bs=16, NB=12, eb=2, sb=2048, sh=1024, st=64):
+        return L.pdattn_pages_copy(k, v, src, dst, n, H, d, bs, NB, eb, sb, sh, st, None, None)
+    assert copy(n=0) == pdattn.OK
+    for kw in (dict(k=None), dict(v=None), dict(src=None), dict(dst=None), dict(n=-1), dict(H=0), dict(NB=0), dict(sb=0),
+               dict(sh=-8), dict(st=56)):
+        assert copy(**kw) == pdattn.INVALID_ARG, kw
+    for kw in (dict(d=32), dict(bs=48), dict(eb=4), dict(sh=1028)):
+        assert copy(**kw) == pdattn.UNSUPPORTED, kw
+    assert copy(k=P + 8) == copy(v=P + 4) == pdattn.MISALIGNED
+
+
+def test_status_strings_of_the_page_operations():
+    L = pdattn.lib()
+    assert len({L.pdattn_status_string(-i) for i in range(0, 11)}) == 11
