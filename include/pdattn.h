@@ -270,6 +270,44 @@ pdattn_status pdattn_rope_append_fp8(const pdattn_rope_args* args, const float* 
                                      pdattn_stream_t stream);
 
 /*
+ * Modified scores and masks, for pdattn_prefill and pdattn_decode_scored.  Query token at position pos, query head h,
+ * key t:
+ *   x = scale * q . k_t;   logit_cap > 0: x = logit_cap * tanh(x / logit_cap);   bias_slopes: x -= bias_slopes[h] * |pos - t|
+ * and the token sees the keys lo <= t < hi,
+ *   lo = max(0, key_begin[token], window > 0 ? pos - window + 1 : 0),   hi = min(L_s, max(pos + 1, prefix_lens[s])).
+ * key_begin is a document mask (the first key of the token's own document); prefix_lens is a prefix mask (every token
+ * of the sequence sees the first prefix_lens[s] keys, whatever its position); window is a sliding window.  A token that
+ * sees no key gets zeros.  What a token does not see never reaches its output, infinities and NaN included.
+ * All members zero / NULL: plain causal attention.
+ */
+typedef struct {
+  float logit_cap;                  /* 0: none                                                        */
+  const float* bias_slopes;         /* DEVICE fp32 [num_q_heads], or NULL                             */
+  int window;                       /* 0: none                                                        */
+  const int32_t* key_begin;         /* DEVICE int32, one per query token, or NULL                     */
+  const int32_t* prefix_lens;       /* DEVICE int32 [num_seqs], or NULL.  pdattn_decode_scored ignores it: a single
+                                       token sees all keys up to itself in any case                   */
+  const int32_t* key_begin_host;    /* HOST copy of key_begin.  pdattn_decode_scored: required with key_begin when
+                                       context_lens_host is given; else ignored                       */
+} pdattn_score_args;
+
+/*
+ * Prompt attention (Section 2.1: the prompt's attention precedes its decoding; Appendix A.1.2's prefill term): n_s new
+ * tokens per sequence, any number, over the paged bf16 cache that already holds their K and V.  Layouts and positions
+ * as in pdattn_rope_append: q, out DEVICE bf16 [num_tokens, num_q_heads, head_dim], dense; args->context_lens counts the
+ * new tokens; cu_tokens DEVICE int32 [num_seqs + 1].  Each token attends by the rules of pdattn_score_args (score NULL:
+ * plain causal).  Takes no host copies: the launch does not depend on the lengths (args->context_lens_host is not read).
+ * The softmax weights are rounded to bf16 for the second product; fp32 otherwise.
+ *   - Bad page ids, slots past the end and pages that no row references: as in pdattn_decode_ex.
+ *   - Rows of out at or past cu_tokens[num_seqs] are left as they were.  A token before position 0 gets zeros.
+ *   - args->workspace holds pdattn_prefill_workspace_size() bytes.
+ */
+pdattn_status pdattn_prefill_workspace_size(int num_seqs, int num_tokens, int num_q_heads, int num_kv_heads, int head_dim,
+                                            int block_size, size_t* device_bytes);
+pdattn_status pdattn_prefill(const pdattn_args* args, const int32_t* cu_tokens, int num_tokens,
+                             const pdattn_score_args* score, pdattn_stream_t stream);
+
+/*
  * Page bookkeeping on the device, for rollout groups that share their prompt's pages (Section 2.1): which pages of a pool
  * are free and how often each is referenced.  The books are caller-owned device arrays; their state is a function of the
  * references alone: free_list holds the pages without references in descending id (the lowest on top, at index

@@ -141,6 +141,17 @@ pdattn_status make_map(const void* ptr, int d, int bs, int hkv, int nb, int64_t 
     r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(ptr), dims, strides, box, estr,
                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  } else if (rank == kMapQ) {
+    // dense query rows [nb tokens, hkv KV heads, sh heads of a KV head, d]; one box = a 64-element column block of the
+    // heads of one KV head for bs tokens, row = token * heads + head
+    const cuuint64_t G = static_cast<cuuint64_t>(sh), H = static_cast<cuuint64_t>(hkv), dd = static_cast<cuuint64_t>(d);
+    cuuint64_t dims[4] = {dd, G, H, nbu};
+    cuuint64_t strides[3] = {dd * 2, G * dd * 2, H * G * dd * 2};
+    cuuint32_t box[4] = {64, static_cast<cuuint32_t>(G), 1, static_cast<cuuint32_t>(bs)};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims, strides, box, estr,
+                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   } else if (rank == 5) {
     cuuint64_t dims[5] = {64, static_cast<cuuint64_t>(bs), static_cast<cuuint64_t>(d / 64),
                           static_cast<cuuint64_t>(hkv), nbu};

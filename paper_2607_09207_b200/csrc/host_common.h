@@ -42,6 +42,7 @@ PDATTN_HIDDEN pdattn_status device_info(int* dev_out, DevInfo** info);
 
 // ---- TMA tensor maps ---------------------------------------------------------------------------
 constexpr int kMapK8 = 81, kMapV8 = 82;   // "ranks" of the two fp8 views in make_map
+constexpr int kMapQ = 83;                 // ... and of the packed query rows of pdattn_prefill
 // View of a cache as a tensor for TMA (see host_common.cu); cached per thread, pointer and shape.
 PDATTN_HIDDEN pdattn_status make_map(const void* ptr, int d, int bs, int hkv, int nb, int64_t sb, int64_t sh, int64_t st,
                                      int rank, CUtensorMap* out);

@@ -38,7 +38,7 @@ EXPORTS = [
     "pdattn_decode_static_scratch", "pdattn_append_kv",
     "pdattn_grouped_workspace_size", "pdattn_decode_grouped",
     "pdattn_multi_workspace_size", "pdattn_decode_multi", "pdattn_decode_fp8", "pdattn_append_kv_fp8", "pdattn_decode_fp8_multi",
-    "pdattn_rope_append", "pdattn_rope_append_fp8",
+    "pdattn_rope_append", "pdattn_rope_append_fp8", "pdattn_prefill_workspace_size", "pdattn_prefill",
     "pdattn_pages_workspace_size", "pdattn_pages_init", "pdattn_pages_reserve", "pdattn_pages_fork", "pdattn_pages_free",
     "pdattn_pages_compact", "pdattn_pages_copy",
 ]
@@ -81,6 +81,11 @@ class RopeArgs(ctypes.Structure):
         ("kv_block_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64), ("kv_token_stride", ctypes.c_int64),
         ("workspace", ctypes.c_void_p),
     ]
+
+
+class ScoreArgs(ctypes.Structure):
+    _fields_ = [("logit_cap", ctypes.c_float), ("bias_slopes", ctypes.c_void_p), ("window", ctypes.c_int),
+                ("key_begin", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p), ("key_begin_host", ctypes.c_void_p)]
 
 
 class PoolArgs(ctypes.Structure):
@@ -134,6 +139,8 @@ def lib():
         L.pdattn_check.argtypes = [vp, vp]
         L.pdattn_rope_append.argtypes = [ctypes.POINTER(RopeArgs), vp]
         L.pdattn_rope_append_fp8.argtypes = [ctypes.POINTER(RopeArgs), vp, vp, vp]
+        L.pdattn_prefill_workspace_size.argtypes = [i32] * 6 + [ctypes.POINTER(sz)]
+        L.pdattn_prefill.argtypes = [ctypes.POINTER(Args), vp, i32, ctypes.POINTER(ScoreArgs), vp]
         pool = ctypes.POINTER(PoolArgs)
         L.pdattn_pages_workspace_size.argtypes = [i32, i32, ctypes.POINTER(sz)]
         L.pdattn_pages_init.argtypes = [pool, vp]
@@ -520,6 +527,91 @@ def rope_append_fp8(q, k_new, v_new, q_out, k8, v8, k_scale, v_scale, block_tabl
     a = _rope_args(where, q, k_new, v_new, q_out, k8, v8, block_table, context_lens, inv_freq, cu_tokens, rotary_dim,
                    interleaved, magnitude, workspace)
     st = lib().pdattn_rope_append_fp8(ctypes.byref(a), k_scale.data_ptr(), v_scale.data_ptr(), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+class Score:
+    """Modified scores and masks (pdattn_score_args): logit_cap, bias_slopes (fp32 [Hq]), window, key_begin (int32, one per
+    query token), prefix_lens (int32 [S]); key_begin_host: the host copy a decode call with host lengths needs."""
+
+    def __init__(self, logit_cap: float = 0.0, bias_slopes=None, window: int = 0, key_begin=None, prefix_lens=None,
+                 key_begin_host: Optional[np.ndarray] = None):
+        _expect("Score", torch.float32, bias_slopes)
+        _expect("Score", torch.int32, key_begin, prefix_lens)
+        _dense("Score", bias_slopes, key_begin, prefix_lens)
+        host = None if key_begin_host is None else np.ascontiguousarray(key_begin_host, dtype=np.int32)
+        self.keep = (bias_slopes, key_begin, prefix_lens, host)
+        self.args = ScoreArgs(float(logit_cap), _ptr(bias_slopes), int(window), _ptr(key_begin), _ptr(prefix_lens),
+                              None if host is None else host.ctypes.data)
+
+    def fits(self, where: str, num_q_heads: int, num_tokens: int, num_seqs: int):
+        slopes, begin, prefix, host = self.keep
+        for what, t, n in (("bias_slopes", slopes, num_q_heads), ("key_begin", begin, num_tokens),
+                           ("prefix_lens", prefix, num_seqs)):
+            if t is not None and t.numel() != n:
+                raise ValueError(f"{where}: {what} has {t.numel()} entries, {n} are wanted")
+        if host is not None and host.size != num_tokens:
+            raise ValueError(f"{where}: key_begin_host has {host.size} entries, {num_tokens} are wanted")
+
+
+def _step_args(where, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace) -> Args:
+    """The argument block of a call over bf16 or code caches whose q and out are [rows, Hq, d]."""
+    N, Hq, d = q.shape
+    NB, Hkv, bs = k_cache.shape[:3]
+    _expect(where, torch.bfloat16, q, out)
+    _expect(where, torch.int32, block_table, context_lens)
+    _dense(where, q, out, block_table, context_lens)
+    S = context_lens.numel()
+    if k_cache.shape[3] != d or tuple(out.shape) != (N, Hq, d) or block_table.dim() != 2 or block_table.shape[0] != S:
+        raise ValueError(f"{where}: shapes do not belong together")
+    a = Args()
+    a.q, a.k_cache, a.v_cache, a.out = q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr()
+    a.block_table, a.context_lens = block_table.data_ptr(), context_lens.data_ptr()
+    a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = S, Hq, Hkv, d, bs
+    a.max_blocks_per_seq, a.num_blocks = block_table.shape[1], NB
+    a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = k_cache.stride(0), k_cache.stride(1), k_cache.stride(2)
+    a.scale = float(scale)
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    return a
+
+
+def prefill_workspace_size(num_seqs, num_tokens, num_q_heads, num_kv_heads, head_dim, block_size=16) -> int:
+    n = ctypes.c_size_t(0)
+    st = lib().pdattn_prefill_workspace_size(num_seqs, num_tokens, num_q_heads, num_kv_heads, head_dim, block_size,
+                                             ctypes.byref(n))
+    if st != OK:
+        raise PdattnError(st, "pdattn_prefill_workspace_size")
+    return n.value
+
+
+def alloc_prefill_workspace(num_seqs, num_tokens, num_q_heads, num_kv_heads, head_dim, block_size=16, device="cuda",
+                            stream=None):
+    n = prefill_workspace_size(num_seqs, num_tokens, num_q_heads, num_kv_heads, head_dim, block_size)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    st = lib().pdattn_workspace_init(ws.data_ptr(), n, _stream_ptr(stream))
+    if st != OK:
+        raise PdattnError(st, "pdattn_workspace_init")
+    return ws
+
+
+def prefill(q, k_cache, v_cache, block_table, context_lens, cu_tokens, scale, out, workspace, *,
+            score: Optional[Score] = None, stream=None, check: bool = True) -> int:
+    """pdattn_prefill: q and out [N, Hq, d]; the tokens cu_tokens[s] .. cu_tokens[s + 1] are the last ones of sequence s's
+    context_lens[s] (their K and V are in the caches); each attends by the rules of `score` (None: plain causal)."""
+    where = "pdattn_prefill"
+    _expect(where, torch.bfloat16, k_cache, v_cache)
+    _expect(where, torch.int32, cu_tokens)
+    _dense(where, cu_tokens)
+    _same_cache(where, k_cache, v_cache)
+    a = _step_args(where, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace)
+    if cu_tokens.numel() != a.num_seqs + 1:
+        raise ValueError(f"{where}: cu_tokens has {cu_tokens.numel()} entries for {a.num_seqs} sequences")
+    if score is not None:
+        score.fits(where, a.num_q_heads, q.shape[0], a.num_seqs)
+    st = lib().pdattn_prefill(ctypes.byref(a), cu_tokens.data_ptr(), q.shape[0],
+                              ctypes.byref(score.args) if score is not None else None, _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
     return st

@@ -1,0 +1,321 @@
+"""Prompt attention over the paged cache, with modified scores and masks, against the definition in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_09207_b200 import pdattn
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def make(n, L, Hq, Hkv, d, bs, seed=0, nhd=False, sharp=1.0):
+    """n[s] new tokens of L[s] per sequence.  Slots past the end and pages that no row references hold NaN."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    n, L = np.asarray(n), np.asarray(L)
+    N, pages = int(n.sum()), np.maximum(0, -(-L // bs))
+    NB, MB = int(pages.sum()) + 2, int(max(1, pages.max())) + 1
+    perm = np.random.default_rng(seed).permutation(NB)
+    table = np.full((len(n), MB), -7, np.int32)
+    shape = (NB, bs, Hkv, d) if nhd else (NB, Hkv, bs, d)
+    kc, vc = (torch.randn(*shape, device="cuda", dtype=BF16, generator=g) for _ in range(2))
+    if nhd:
+        kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
+    used = torch.zeros(NB, bs, dtype=torch.bool, device="cuda")
+    at = 0
+    for s in range(len(n)):
+        table[s, :pages[s]] = perm[at:at + pages[s]]
+        at += pages[s]
+        for b in range(pages[s]):
+            used[table[s, b], :min(bs, L[s] - b * bs)] = True
+    for x in (kc, vc):
+        x.masked_fill_(~used[:, None, :, None], float("nan"))
+    q = (torch.randn(N, Hq, d, device="cuda", generator=g) * sharp).to(BF16)
+    i32 = lambda x: torch.from_numpy(np.asarray(x, np.int32)).cuda()  # noqa: E731
+    return dict(q=q, kc=kc, vc=vc, table=i32(table), lens=i32(L), cu=i32(np.concatenate([[0], np.cumsum(n)])), n=n, L=L, bs=bs,
+                tab=table, scale=1.0 / math.sqrt(d))
+
+
+def reference(c, cap=0.0, slopes=None, window=0, begin=None, prefix=None, bad=()):
+    """(output, sum of weight times |v|) in 64 bits; bad: pages whose tokens are left out."""
+    N, Hq, d = c["q"].shape
+    Hkv, bs = c["kc"].shape[1], c["bs"]
+    G = Hq // Hkv
+    out, size = np.zeros((N, Hq, d)), np.zeros((N, Hq, d))
+    t0 = 0
+    for s in range(len(c["n"])):
+        n, L = int(c["n"][s]), int(c["L"][s])
+        if n == 0:
+            continue
+        pg = torch.from_numpy(np.clip(c["tab"][s, :-(-max(L, 1) // bs)], 0, c["kc"].shape[0] - 1)).long().cuda()
+        pos = torch.arange(L - n, L, device="cuda")
+        t = torch.arange(L, device="cuda")
+        lo = torch.zeros_like(pos)
+        if window:
+            lo = (pos - window + 1).clamp(min=0)
+        if begin is not None:
+            lo = torch.maximum(lo, torch.from_numpy(np.asarray(begin[t0:t0 + n])).long().cuda())
+        hi = pos + 1
+        if prefix is not None:
+            hi = hi.clamp(min=int(prefix[s]))
+        hi = torch.where(pos < 0, 0, hi.clamp(max=L))
+        seen = (t >= lo[:, None]) & (t < hi[:, None])
+        if len(bad):
+            here = torch.from_numpy(np.isin(c["tab"][s, t.cpu().numpy() // bs], bad)).cuda()
+            seen &= ~here
+        for h in range(Hkv):
+            k = c["kc"][pg, h].reshape(-1, d)[:L].double()
+            v = c["vc"][pg, h].reshape(-1, d)[:L].double()
+            x = torch.einsum("ngd,td->gnt", c["q"][t0:t0 + n, h * G:(h + 1) * G].double(), k) * c["scale"]
+            if cap:
+                x = cap * torch.tanh(x / cap)
+            if slopes is not None:
+                x = x - slopes[h * G:(h + 1) * G].double().view(-1, 1, 1) * (pos[:, None] - t).abs()
+            x = torch.where(seen, x, -math.inf)
+            p = torch.nan_to_num(torch.softmax(x, -1), nan=0.0)
+            v0 = torch.nan_to_num(v, nan=0.0, posinf=0.0, neginf=0.0)
+            o = torch.einsum("gnt,td->ngd", p, v0)
+            for mark in (math.inf, -math.inf, math.nan):      # what a row sees of non-finite elements decides its output
+                m = (v.isnan() if mark != mark else v == mark).double()
+                if m.any():
+                    hit = torch.einsum("nt,td->nd", seen.double(), m) > 0
+                    o = o + torch.where(hit, mark, 0.0)[:, None]
+            out[t0:t0 + n, h * G:(h + 1) * G] = o.cpu().numpy()
+            size[t0:t0 + n, h * G:(h + 1) * G] = torch.einsum("gnt,td->ngd", p, v0.abs()).cpu().numpy()
+        t0 += n
+    return out, size
+
+
+def close(got, want, size):
+    # The weights are rounded to bf16 (2^-8 of each at most): 2^-8 of sum p |v|.  The result once more: 2^-8 of it.  Scores and
+    # sums in fp32 with exponentials good to 2^-22: below 2^-12 of sum p |v| for scores up to a few hundred.
+    got = got.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(np.isinf(got), np.isinf(want))
+    f = np.isfinite(want)
+    assert np.array_equal(got[np.isinf(want)], want[np.isinf(want)])
+    err, tol = abs(got[f] - want[f]), 2.0 ** -8 * abs(want[f]) + (2.0 ** -8 + 2.0 ** -12) * size[f] + 1e-30
+    assert (err <= tol).all(), (err / tol).max()
+
+
+def run(c, ws=None, q=None, out=None, **score):
+    N, Hq, d = c["q"].shape
+    ws = ws if ws is not None else pdattn.alloc_prefill_workspace(len(c["n"]), N, Hq, c["kc"].shape[1], d, c["bs"])
+    out = out if out is not None else torch.full_like(c["q"], 7.0)
+    pdattn.prefill(c["q"] if q is None else q, c["kc"], c["vc"], c["table"], c["lens"], c["cu"], c["scale"], out, ws,
+                   score=pdattn.Score(**score) if score else None)
+    assert pdattn.check(ws) == pdattn.OK
+    return out
+
+
+def begins(c, size):
+    return np.concatenate([np.arange(L - n, L) // size * size for n, L in zip(c["n"], c["L"])]).astype(np.int32)
+
+
+@pytest.mark.parametrize("Hq,Hkv,d,bs", [(28, 4, 128, 16), (4, 1, 64, 16), (8, 8, 128, 64), (16, 1, 128, 32), (6, 2, 64, 64),
+                                       (5, 1, 128, 16), (13, 1, 64, 32), (9, 1, 128, 64)])
+def test_plain_causal(Hq, Hkv, d, bs):
+    c = make([1, 0, 37, 300, 5, 130, 0, 64], [1, 40, 37, 300, 700, 131, 0, 1000], Hq, Hkv, d, bs, seed=Hq)
+    close(run(c), *reference(c))
+
+
+@pytest.mark.parametrize("n,L", [([1], [1]), ([1], [129]), ([128], [128]), ([129], [257]), ([2000], [2000]), ([1] * 200, list(range(1, 201))),
+                                 ([700, 3], [5000, 20000])])
+def test_lengths(n, L):
+    c = make(n, L, 14, 2, 128, 16, seed=len(n))
+    close(run(c), *reference(c))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cap,bias", [(0, True), (30.0, False), (5.0, True)])
+@pytest.mark.parametrize("mask", ["causal", "window", "documents", "prefix", "all"])
+def test_scores_and_masks(d, cap, bias, mask):
+    c = make([200, 1, 33, 400, 90], [200, 77, 400, 900, 300], 6, 2, d, 32, seed=d, sharp=3.0)
+    score, ref = {}, {}
+    if cap:
+        score["logit_cap"] = ref["cap"] = cap
+    if bias:
+        score["bias_slopes"] = ref["slopes"] = torch.tensor([0.5, 0.2, 0.01, 0.0, -0.001, 1.0], device="cuda")
+    if mask in ("window", "all"):
+        score["window"] = ref["window"] = 100
+    if mask in ("documents", "all"):
+        ref["begin"] = begins(c, 90)
+        score["key_begin"] = torch.from_numpy(ref["begin"]).cuda()
+    if mask in ("prefix", "all"):
+        ref["prefix"] = np.array([150, 1000, 0, 450, 300], np.int32)
+        score["prefix_lens"] = torch.from_numpy(ref["prefix"]).cuda()
+    close(run(c, **score), *reference(c, **ref))
+
+
+def test_rows_that_see_nothing_and_unordered_documents():
+    """First keys drawn at random: many rows see nothing, others a single key; the tiles of a pair need not touch."""
+    c = make([150, 260, 40], [150, 500, 2000], 4, 2, 128, 16)
+    r = np.random.default_rng(5)
+    pos = np.concatenate([np.arange(L - n, L) for n, L in zip(c["n"], c["L"])])
+    begin = (pos - r.integers(-40, 1500, len(pos)) * (r.random(len(pos)) < 0.8)).astype(np.int32)
+    begin[:128] = 5000                                       # a whole tile without keys
+    out = run(c, key_begin=torch.from_numpy(begin).cuda())
+    want, size = reference(c, begin=begin)
+    close(out, want, size)
+    assert not out[:128].any()
+
+
+def test_fewer_keys_than_tokens_and_padding():
+    """A sequence with more new tokens than its context: those before position 0 get zeros; rows behind the last sequence
+    stay as they are."""
+    c = make([10, 200, 3], [4, 150, 3], 8, 2, 64, 16)
+    q = torch.cat([c["q"], torch.full((300, 8, 64), float("nan"), device="cuda", dtype=BF16)])
+    out = run(c, q=q, out=torch.full_like(q, 7.0))
+    close(out[:213], *reference(c))
+    assert not out[:6].any() and not out[10:60].any()
+    assert bool((out[213:] == 7).all())
+
+
+def test_negative_and_zero_scale():
+    c = make([100, 9], [100, 300], 4, 1, 128, 16)
+    for scale in (-0.1, 0.0):
+        c["scale"] = scale
+        close(run(c), *reference(c))
+        close(run(c, logit_cap=2.0), *reference(c, cap=2.0))
+
+
+def test_values_that_are_not_finite():
+    """Infinities and NaN in V reach exactly the rows that see them; in K and in masked places they reach nobody else."""
+    c = make([300, 260], [300, 700], 4, 2, 128, 16)
+    v, tab = c["vc"], c["tab"]
+    for s, t, h, j, x in ((0, 137, 0, 5, math.inf), (0, 200, 1, 100, math.nan), (1, 650, 0, 64, -math.inf), (1, 650, 0, 3, math.inf),
+                          (1, 690, 0, 3, -math.inf), (1, 10, 1, 127, math.nan)):
+        v[tab[s, t // 16], h, t % 16, j] = x
+    close(run(c), *reference(c))
+    begin = begins(c, 140)
+    close(run(c, key_begin=torch.from_numpy(begin).cuda()), *reference(c, begin=begin))
+    # masked keys may be anything
+    c["kc"][tab[1, 0:20]] = math.nan
+    c["kc"][tab[1, 20:25]] = math.inf
+    c["vc"][tab[1, 0:25]] = math.nan
+    begin = np.concatenate([np.zeros(300), np.full(260, 400)]).astype(np.int32)
+    out = run(c, key_begin=torch.from_numpy(begin).cuda())
+    close(out, *reference(c, begin=begin))
+
+
+def test_a_key_of_nan_reaches_only_those_who_see_it():
+    c = make([200], [200], 4, 2, 64, 16)
+    want, size = reference(c)
+    c["kc"][c["tab"][0, 150 // 16], 0, 150 % 16] = math.nan
+    out = run(c)
+    close(out[:150], want[:150], size[:150])
+    close(out[:, 2:], want[:, 2:], size[:, 2:])
+    assert bool(out[150:, :2].isnan().all())
+
+
+def test_bad_pages_are_left_out_and_reported():
+    c = make([100, 64, 30], [300, 64, 90], 4, 2, 128, 16)
+    NB = c["kc"].shape[0]
+    c["tab"][0, 3], c["tab"][0, 18], c["tab"][1, 2] = NB, -1, NB + 5
+    c["table"] = torch.from_numpy(c["tab"]).cuda()
+    ws = pdattn.alloc_prefill_workspace(3, 194, 4, 2, 128)
+    out = torch.empty_like(c["q"])
+    args = (c["q"], c["kc"], c["vc"], c["table"], c["lens"], c["cu"], c["scale"], out, ws)
+    pdattn.prefill(*args)
+    assert pdattn.check(ws) == pdattn.BAD_PAGE_INDEX and pdattn.check(ws) == pdattn.OK
+    close(out, *reference(c, bad=(NB, -1, NB + 5)))
+    # a context longer than its table row: the tokens past the row are left out, nothing past the row is read
+    short = c["table"][:, :10].contiguous()
+    c["tab"] = np.concatenate([c["tab"][:, :10], np.full((3, 12), -1, np.int32)], 1)
+    pdattn.prefill(c["q"], c["kc"], c["vc"], short, c["lens"], c["cu"], c["scale"], out, ws)
+    assert pdattn.check(ws) == pdattn.BAD_PAGE_INDEX
+    close(out, *reference(c, bad=(NB, -1, NB + 5)))
+
+
+def test_token_major_pages_and_shared_pages():
+    c = make([120, 120], [120, 120], 8, 4, 128, 32, nhd=True)
+    close(run(c), *reference(c))
+    c = make([50, 50], [300, 300], 8, 4, 128, 16)
+    c["tab"][1, :10] = c["tab"][0, :10]
+    c["table"] = torch.from_numpy(c["tab"]).cuda()
+    close(run(c), *reference(c))
+
+
+def test_same_bits_every_time_and_under_renumbered_pages():
+    c = make([700, 5, 260], [700, 900, 1500], 14, 2, 128, 16)
+    score = dict(logit_cap=30.0, bias_slopes=torch.linspace(0, 0.5, 14, device="cuda"))
+    a = run(c, **score)
+    for _ in range(3):
+        assert torch.equal(run(c, **score), a)
+    perm = torch.randperm(c["kc"].shape[0], device="cuda")
+    c["kc"], c["vc"] = c["kc"][perm].contiguous(), c["vc"][perm].contiguous()
+    back = torch.argsort(perm).int()
+    c["table"] = torch.where(c["table"] >= 0, back[c["table"].clamp(min=0).long()], c["table"])
+    assert torch.equal(run(c, **score), a)
+
+
+def test_agrees_with_the_decode_step():
+    """One new token per sequence is the decode step; several are pdattn_decode_multi's."""
+    c = make([1] * 20, np.arange(1, 21) * 37, 8, 2, 128, 16)
+    out, other = run(c), torch.empty_like(c["q"])
+    ws = pdattn.alloc_workspace(20, 8, 2, 128)
+    pdattn.decode_ex(c["q"], c["kc"], c["vc"], c["table"], c["lens"], c["scale"], other, ws)
+    want, size = reference(c)
+    close(out, want, size)
+    assert (abs(out.double() - other.double()).cpu().numpy() <= 2.0 ** -7 * abs(want) + 2.0 ** -7 * size).all()
+
+
+def test_largest_pool_offsets():
+    """Pages past 2^32 elements of a pool."""
+    NB, Hkv, bs, d = 300000, 2, 64, 128                     # 4.9e9 elements a cache
+    kc, vc = (torch.zeros(NB, Hkv, bs, d, device="cuda", dtype=BF16) for _ in range(2))
+    pages = [NB - 1, 3, NB - 2]
+    for p in pages:
+        kc[p].normal_()
+        vc[p].normal_()
+    q = torch.randn(70, 4, d, device="cuda").to(BF16)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    c = dict(q=q, kc=kc, vc=vc, table=i32([pages]), lens=i32([190]), cu=i32([0, 70]), n=np.array([70]), L=np.array([190]), bs=bs,
+             tab=np.array([pages]), scale=0.1)
+    vc[NB - 1, 0, 5, 7] = math.inf
+    close(run(c), *reference(c))
+
+
+def test_captured_replayed_and_on_another_stream():
+    c = make([40, 100], [200, 100], 4, 2, 128, 16)
+    ws = pdattn.alloc_prefill_workspace(2, 140, 4, 2, 128)
+    out = run(c, ws=ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pdattn.prefill(c["q"], c["kc"], c["vc"], c["table"], c["lens"], c["cu"], c["scale"], out, ws)
+        pdattn.prefill(c["q"], c["kc"], c["vc"], c["table"], c["lens"], c["cu"], c["scale"], out, ws)
+    c["cu"][1] = 30                                          # the replayed call goes by the tokens of its time
+    c["n"] = np.array([30, 110])
+    c["lens"][1] = 110
+    c["L"] = np.array([200, 110])
+    c["vc"].nan_to_num_(0.0)
+    c["kc"].nan_to_num_(0.0)
+    graph.replay()
+    close(out, *reference(c))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = torch.empty_like(out)
+    pdattn.prefill(c["q"], c["kc"], c["vc"], c["table"], c["lens"], c["cu"], c["scale"], other, ws, stream=side)
+    side.synchronize()
+    assert torch.equal(other, out)
+
+
+def test_wrapper_refuses_what_the_library_cannot_see():
+    c = make([4], [20], 4, 2, 64, 16)
+    ws = pdattn.alloc_prefill_workspace(1, 4, 4, 2, 64)
+    good = dict(q=c["q"], k_cache=c["kc"], v_cache=c["vc"], block_table=c["table"], context_lens=c["lens"], cu_tokens=c["cu"], scale=1.0,
+                out=torch.empty_like(c["q"]), workspace=ws)
+    for name, bad in [("q", c["q"].half()), ("cu_tokens", c["cu"].long()), ("k_cache", c["kc"].float())]:
+        with pytest.raises(TypeError):
+            pdattn.prefill(**dict(good, **{name: bad}))
+    for name, bad in [("out", good["out"][:2]), ("cu_tokens", c["cu"][:1]), ("v_cache", c["vc"][:, :1]), ("block_table", c["table"].expand(2, -1)),
+                      ("q", c["q"].transpose(0, 1))]:
+        with pytest.raises(ValueError):
+            pdattn.prefill(**dict(good, **{name: bad}))
+    with pytest.raises(ValueError):
+        pdattn.prefill(**good, score=pdattn.Score(bias_slopes=torch.zeros(3, device="cuda")))
+    with pytest.raises(ValueError):
+        pdattn.prefill(**good, score=pdattn.Score(key_begin=torch.zeros(5, dtype=torch.int32, device="cuda")))
+    with pytest.raises(pdattn.PdattnError):
+        pdattn.prefill(**good, score=pdattn.Score(logit_cap=-1.0))

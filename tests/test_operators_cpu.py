@@ -102,3 +102,43 @@ def test_pages_refusals():
 def test_status_strings_of_the_page_operations():
     L = pdattn.lib()
     assert len({L.pdattn_status_string(-i) for i in range(0, 11)}) == 11
+
+
+def step(**kw):
+    a = pdattn.Args()
+    for f in ("q", "k_cache", "v_cache", "out", "block_table", "context_lens", "workspace"):
+        setattr(a, f, P)
+    a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = 3, 4, 2, 64, 16
+    a.max_blocks_per_seq, a.num_blocks, a.scale = 4, 12, 0.1
+    a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = 2048, 1024, 64
+    a.workspace_bytes = 1 << 30
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+BAD_STEPS = [(dict(num_seqs=-1), pdattn.INVALID_ARG), (dict(num_q_heads=5), pdattn.INVALID_ARG), (dict(head_dim=96), pdattn.UNSUPPORTED),
+             (dict(block_size=8), pdattn.UNSUPPORTED), (dict(num_q_heads=34), pdattn.UNSUPPORTED), (dict(max_blocks_per_seq=0), pdattn.INVALID_ARG),
+             (dict(num_blocks=0), pdattn.INVALID_ARG), (dict(kv_head_stride=0), pdattn.INVALID_ARG), (dict(kv_token_stride=56), pdattn.INVALID_ARG),
+             (dict(kv_block_stride=2052), pdattn.UNSUPPORTED), (dict(workspace=P + 128), pdattn.MISALIGNED),
+             (dict(workspace_bytes=8447), pdattn.WORKSPACE_TOO_SMALL)]
+BAD_STEPS += [({f: None}, pdattn.INVALID_ARG) for f in ("q", "k_cache", "v_cache", "out", "block_table", "context_lens", "workspace")]
+BAD_STEPS += [({f: P + 8}, pdattn.MISALIGNED) for f in ("q", "k_cache", "v_cache", "out")]
+BAD_SCORES = [(-1.0, 0), (float("nan"), 0), (float("inf"), 0), (0.0, -1)]
+
+
+def test_prefill_refusals():
+    L = pdattn.lib()
+
+    def call(score=None, cu=P, n=9, **kw):
+        return L.pdattn_prefill(ctypes.byref(step(**kw)), cu, n, None if score is None else ctypes.byref(score), None)
+    assert L.pdattn_prefill(None, P, 9, None, None) == pdattn.INVALID_ARG
+    assert call(n=0) == call(num_seqs=0) == pdattn.OK                            # nothing to do
+    assert call(n=-1) == call(cu=None) == pdattn.INVALID_ARG
+    for kw, why in BAD_STEPS:
+        assert call(**kw) == why, kw
+    for cap, window in BAD_SCORES:
+        assert call(pdattn.ScoreArgs(cap, None, window, None, None, None)) == pdattn.INVALID_ARG
+    assert pdattn.prefill_workspace_size(3, 9, 4, 2, 64) >= 8448
+    with pytest.raises(pdattn.PdattnError):
+        pdattn.prefill_workspace_size(3, -1, 4, 2, 64)
