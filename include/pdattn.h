@@ -308,6 +308,14 @@ pdattn_status pdattn_prefill(const pdattn_args* args, const int32_t* cu_tokens, 
                              const pdattn_score_args* score, pdattn_stream_t stream);
 
 /*
+ * The decode step of pdattn_decode_ex / pdattn_decode_fp8 with the scores and masks of pdattn_score_args (score must not
+ * be NULL; key_begin has one entry per sequence).  Keys before lo are not read.  Workspace as for pdattn_decode_ex.
+ */
+pdattn_status pdattn_decode_scored(const pdattn_args* args, const pdattn_score_args* score, pdattn_stream_t stream);
+pdattn_status pdattn_decode_scored_fp8(const pdattn_args* args, const pdattn_score_args* score, const float* k_scale,
+                                       const float* v_scale, pdattn_stream_t stream);
+
+/*
  * Page bookkeeping on the device, for rollout groups that share their prompt's pages (Section 2.1): which pages of a pool
  * are free and how often each is referenced.  The books are caller-owned device arrays; their state is a function of the
  * references alone: free_list holds the pages without references in descending id (the lowest on top, at index

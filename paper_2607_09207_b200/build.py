@@ -9,9 +9,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_DIR = os.path.join(HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libpdattn.so")
-SOURCES = ["pdattn_api.cu", "ops_api.cu", "prefill_api.cu", "host_common.cu", "partition.cpp"]
+SOURCES = ["pdattn_api.cu", "ops_api.cu", "prefill_api.cu", "scored_api.cu", "host_common.cu", "partition.cpp"]
 HEADERS = ["kernels.cuh", "host_common.h", "common.cuh", "tile_bf16.cuh", "tile_fp8.cuh", "decode.cuh", "prefix_mma.cuh",
-           "prefix_umma.cuh", "aux_kernels.cuh", "rope.cuh", "pages.cuh", "prefill_umma.cuh", "umma.cuh", "partition.h", os.path.join("..", "..", "include", "pdattn.h")]
+           "prefix_umma.cuh", "aux_kernels.cuh", "rope.cuh", "pages.cuh", "prefill_umma.cuh", "umma.cuh", "scored.h", "partition.h", os.path.join("..", "..", "include", "pdattn.h")]
 
 
 def _nvcc() -> str:

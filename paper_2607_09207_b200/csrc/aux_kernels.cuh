@@ -312,7 +312,11 @@ __device__ __forceinline__ int block_scan_1024(int v, int* warp_sums, int lane, 
 __global__ void __launch_bounds__(1024)
 plan_kernel(const int32_t* __restrict__ context_lens, const int32_t* __restrict__ start_tiles, int S, int Hkv,
             int n_static, int n_dyn_max, int32_t* __restrict__ prefix, SpanStart* __restrict__ spans, WsHeader* hdr,
-            int with_merge_words) {
+            int with_merge_words, const int32_t* __restrict__ key_begin, int window) {
+  // leading tiles that the plan leaves out: given, or those before the first key that the token sees
+  auto skipped = [&](int s, int L) {
+    return start_tiles ? start_tiles[s] : first_key(L, key_begin ? key_begin[s] : 0, window) / TILE;
+  };
   __shared__ int warp_sums[32];
   __shared__ int carry_c, carry_t;
   __shared__ PlanParams pp_s;
@@ -333,7 +337,7 @@ plan_kernel(const int32_t* __restrict__ context_lens, const int32_t* __restrict_
   for (int base = 0; base < S; base += 1024) {
     const int s = base + tid;
     int nt = 0;
-    if (s < S) nt = static_cast<int>(seq_tiles(context_lens[s], start_tiles ? start_tiles[s] : 0));
+    if (s < S) nt = static_cast<int>(seq_tiles(context_lens[s], skipped(s, context_lens[s])));
     mine64 += static_cast<unsigned long long>(seq_cost(nt, Hkv));
     const int ic = block_scan_1024(static_cast<int>(seq_cost(nt, Hkv)), warp_sums, lane, wid) + carry_c;
     const int itl = block_scan_1024(nt * Hkv, warp_sums, lane, wid) + carry_t;
@@ -391,7 +395,7 @@ plan_kernel(const int32_t* __restrict__ context_lens, const int32_t* __restrict_
         const int mid = (lo + hi) >> 1;
         if (pcost[mid] <= x) lo = mid; else hi = mid;
       }
-      const int nt = static_cast<int>(seq_tiles(context_lens[lo], start_tiles ? start_tiles[lo] : 0));
+      const int nt = static_cast<int>(seq_tiles(context_lens[lo], skipped(lo, context_lens[lo])));
       int k, tile;
       locate_in_seq(x - pcost[lo], nt, &k, &tile);
       sp.unit = lo * Hkv + k;

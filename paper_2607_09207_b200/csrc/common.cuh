@@ -74,6 +74,12 @@ struct DecodeParams {
   int use_ws_plan;
   int box5d;                // 1: the tensor maps are 5-D and one TMA op brings a whole page-head
   int32_t* tickets;         // [MAX_SPANS] ticket words (see WS_TICKETS_OFFSET)
+  // modified scores and masks (decode_kernel with MOD): see pdattn_score_args
+  const int32_t* key_begin;   // per sequence, or null
+  const float* slopes;        // per query head, or null
+  int window;                 // 0: none
+  float cap2;                 // cap * log2(e); 0: none
+  float cap_r;                // 2 / cap
   int inkernel_max;         // > 0: a cut unit whose followers all lie within this many spans after its first one is
                             // merged by the CTA that writes its last partial; 0: every cut unit is left to combine_kernel
   SpanStart spans[MAX_PARAM_SPANS + 1];
@@ -309,25 +315,31 @@ static_assert(sizeof(Ctrl) <= 1280, "control block");
 // ------------------------------------------------------------------------------------------
 struct Piece {
   int unit, s, g, L, nt, tb, te;
-  int t0;   // tiles of the sequence that are skipped (shared prefix handled elsewhere): tile t of the
-            // piece is tile t0 + t of the sequence
+  int t0;   // tiles of the sequence that are skipped (shared prefix handled elsewhere, or keys the token does not
+            // see): tile t of the piece is tile t0 + t of the sequence
+  int lo;   // MOD only: first key that the token sees
 };
-struct Walker {
+// MOD: `start` is key_begin (first key per sequence, may be null) and the skipped tiles follow from it and the window.
+template <bool MOD>
+struct WalkerT {
   const int32_t* ctx;
-  const int32_t* start_tiles;   // per sequence, may be null (= 0)
+  const int32_t* start;         // start tiles per sequence, may be null (= 0)
   int Hkv, nunits, unit, tb, rem;
+  int window = 0;
   int pf_unit = -1, pf_L = 0, pf_t0 = 0;   // the following unit's length and start, loaded one piece early
   __device__ __forceinline__ bool next(Piece& p) {
     while (rem > 0 && unit < nunits) {
       const int s = unit / Hkv;
       const bool hit = unit == pf_unit;
       const int L = hit ? pf_L : __ldg(ctx + s);
-      const int t0 = hit ? pf_t0 : (start_tiles ? __ldg(start_tiles + s) : 0);
+      const int st = hit ? pf_t0 : (start ? __ldg(start + s) : 0);
       if (unit + 1 < nunits) {
         pf_unit = unit + 1;
         pf_L = __ldg(ctx + (unit + 1) / Hkv);
-        pf_t0 = start_tiles ? __ldg(start_tiles + (unit + 1) / Hkv) : 0;
+        pf_t0 = start ? __ldg(start + (unit + 1) / Hkv) : 0;
       }
+      const int lo = MOD ? first_key(L, st, window) : 0;
+      const int t0 = MOD ? lo / TILE : st;
       const int nt_all = L > 0 ? (L + TILE - 1) / TILE : 0;
       const int nt = nt_all > t0 ? nt_all - t0 : 0;
       if (tb >= nt) {
@@ -341,6 +353,7 @@ struct Walker {
       p.L = L;
       p.nt = nt;
       p.t0 = t0;
+      p.lo = lo;
       p.tb = tb;
       p.te = min(nt, tb + rem);
       rem -= p.te - p.tb;
@@ -349,6 +362,27 @@ struct Walker {
       return true;
     }
     return false;
+  }
+};
+using Walker = WalkerT<false>;
+
+// Modified scores of one tile on one warp (compute_tile and compute_tile_f8 with MOD).
+template <int NT>
+struct TileMod {
+  float cap2, cap_k;        // cap tanh(s / cap) in base-2 units: cap2 - 2 cap2 / (1 + 2^(s cap_k)); cap2 == 0: none
+  float slope2[NT][2];      // per score column of this lane: -slope * log2(e)
+  int head;                 // tokens of the tile before the first one seen (<= 0: none)
+  // score of a token `dist` positions before the current one
+  __device__ __forceinline__ float score(float s, float sl2, int nt, int e, int dist) const {
+    float v = s * sl2;
+    if (cap2 != 0.f) {
+      // exact to 2^-21 of the cap, at both ends of the range too
+      float rc;
+      const float ex = fast_exp2(s * cap_k) + 1.f;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(ex));
+      v = fmaf(-2.f * cap2, rc, cap2);
+    }
+    return fmaf(slope2[nt][e], static_cast<float>(dist), v);
   }
 };
 

@@ -264,7 +264,7 @@ __device__ __forceinline__ void stage_queries_loop(const DecodeParams& P, Ctrl* 
 // which class of which of those pieces may touch it next.  Warps that hold no tile of a piece skip it
 // (they do not even read its query rows), so up to NCW short pieces are in work at once.
 // ------------------------------------------------------------------------------------------
-template <int D, int NT, int BS, int EB, bool WIN>
+template <int D, int NT, int BS, int EB, bool WIN, bool MOD>
 __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanParams& pp, Ctrl* ctrl, uint32_t ring,
                                               uint32_t qbuf, uint8_t* handoff, int warp, int lane) {
   using C = Cfg<D, NT, BS, EB>;
@@ -368,6 +368,18 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
       // fp8 cache: the K scale of this KV head joins the softmax scale
       const float sl2 = EB == 1 ? P.scale_log2 * __ldg(P.k_scale + pc.g) : P.scale_log2;
       (void)sl2;
+      TileMod<NT> md;
+      if constexpr (MOD) {
+        md.cap2 = P.cap2;
+        md.cap_k = sl2 * P.cap_r;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int row = nt * 8 + qcol + e;
+            md.slope2[nt][e] = P.slopes && row < R ? -1.4426950408889634f * __ldg(P.slopes + pc.g * P.G + row) : 0.f;
+          }
+      }
       // ---- this class's tiles
       for (int its = it0 + pos; its < it0 + n_piece; its += NCW) {
         const int slot = its % NST;
@@ -380,6 +392,8 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
         const uint32_t sV = sK + C::KV_BYTES;
         const uint32_t badmask = ctrl->meta[slot];
         const int n_left = pc.L - (pc.t0 + t) * TILE;
+        if constexpr (MOD) md.head = pc.lo - (pc.t0 + t) * TILE;
+        const bool whole = n_left - (P.T - 1) >= TILE && !(MOD && md.head > 0);   // every query token sees the whole tile
         if constexpr (EB == 2) {
           // split stage halves: the K half goes back to the producers as soon as the scores are computed, and
           // the V half is waited for only when the probabilities are ready
@@ -390,10 +404,12 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
           auto before_v = [&]() {
             if (!mbar_wait(smem_u32(&ctrl->full_v[slot]), (its / NST) & 1)) fail();
           };
-          if (n_left - (P.T - 1) >= TILE) {   // every query token sees the whole tile
-            compute_tile<D, NT, BS, false>(sK, sV, qf, acc, m, l, P.scale_log2, TILE, badmask, lane, lag, after_k, before_v);
+          if (whole) {
+            compute_tile<D, NT, BS, false, MOD>(sK, sV, qf, acc, m, l, P.scale_log2, MOD ? n_left : TILE, badmask, lane, lag, md,
+                                                after_k, before_v);
           } else {
-            compute_tile<D, NT, BS, true>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, after_k, before_v);
+            compute_tile<D, NT, BS, true, MOD>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, md, after_k,
+                                               before_v);
             fence_proxy_async();   // our zero-fill stores must be ordered before the next TMA write
           }
           if (aborted) break;
@@ -401,10 +417,10 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
           if (lane == 0) mbar_arrive(smem_u32(&ctrl->empty_v[slot]));
           continue;
         } else {
-          if (n_left - (P.T - 1) >= TILE) {
-            compute_tile_f8<D, NT, BS, false>(sK, sV, qf, acc, m, l, sl2, TILE, badmask, lane, lag);
+          if (whole) {
+            compute_tile_f8<D, NT, BS, false, MOD>(sK, sV, qf, acc, m, l, sl2, MOD ? n_left : TILE, badmask, lane, lag, md);
           } else {
-            compute_tile_f8<D, NT, BS, true>(sK, sV, qf, acc, m, l, sl2, n_left, badmask, lane, lag);
+            compute_tile_f8<D, NT, BS, true, MOD>(sK, sV, qf, acc, m, l, sl2, n_left, badmask, lane, lag, md);
           }
         }
         __syncwarp();
@@ -483,7 +499,7 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
       }
 
       // ---- finish the piece from registers (one-class piece, or last class of the chain)
-      if (complete && pc.t0 > 0) {
+      if (!MOD && complete && pc.t0 > 0) {
         // the unit's leading tiles were handled elsewhere (shared prefix): fold that partial in
         const float* pfx = P.pfx_partials + (static_cast<int64_t>(pc.s) * P.Hkv + pc.g) * C::SLOT_FLOATS;
 #pragma unroll
@@ -638,7 +654,8 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
         }
       }
     } else {
-      Walker walk{P.context_lens, P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile, sp_end - sp.flat};
+      WalkerT<MOD> walk{P.context_lens, MOD ? P.key_begin : P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile, sp_end - sp.flat,
+                        P.window};
       Piece pc;
       while (walk.next(pc)) {
         const int n_piece = pc.te - pc.tb;
@@ -684,12 +701,14 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
 // ------------------------------------------------------------------------------------------
 // WIN: the instantiation for batches of mostly one-tile pieces (chained merge, 8-row tiles, no in-kernel merge):
 // every warp walks the spans 32 units at a time (WindowWalker) and the tenth warp stages the query rows.
-template <int D, int NT, int BS, bool PROBE = false, bool CHAIN = false, int EB = 2, bool WIN = false>
+// MOD: modified scores and a first key per sequence (pdattn_decode_scored; chained merge, one query token).
+template <int D, int NT, int BS, bool PROBE = false, bool CHAIN = false, int EB = 2, bool WIN = false, bool MOD = false>
 __global__ void __launch_bounds__(Cfg<D, NT, BS, EB>::NTHREADS, 1)
 decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const __grid_constant__ DecodeParams P) {
   using C = Cfg<D, NT, BS, EB>;
   static_assert(EB == 2 || CHAIN, "the fp8 cache path uses the chained merge");
+  static_assert(!MOD || (CHAIN && !PROBE && !WIN), "modified scores use the chained merge");
   constexpr int NST = C::NSTAGES;
   constexpr int NCW = C::NCW;
   constexpr int NCT = C::NCT;
@@ -913,7 +932,8 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           it = it_end;
         }
       } else {
-        Walker walk{P.context_lens, P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile, sp_end - sp.flat};
+        WalkerT<MOD> walk{P.context_lens, MOD ? P.key_begin : P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile, sp_end - sp.flat,
+                          P.window};
         Piece pc;
         while (!aborted && walk.next(pc)) {
           if (!PROBE && pw == 0) {
@@ -970,9 +990,10 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   // ================= consumer warps =================
   const int ct = threadIdx.x;   // 0..NCT-1
   if (!PROBE) {
-    // sequences with no context produce zeros
+    // sequences with no context (or none that their token sees) produce zeros
     for (int s = cta; s < P.S; s += gridDim.x) {
-      if (__ldg(P.context_lens + s) <= 0) {
+      const int L = __ldg(P.context_lens + s);
+      if (L <= 0 || (MOD && first_key(L, P.key_begin ? __ldg(P.key_begin + s) : 0, P.window) >= L)) {
         uint32_t* o = reinterpret_cast<uint32_t*>(P.out + static_cast<int64_t>(s) * P.T * P.Hq * D);
         for (int i = ct; i < P.T * P.Hq * D / 2; i += NCT) o[i] = 0u;
       }
@@ -982,7 +1003,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   const int qcol = (lane & 3) * 2;
 
   if constexpr (CHAIN) {
-    consume_chain<D, NT, BS, EB, WIN>(P, pp, ctrl, ring, qbuf,
+    consume_chain<D, NT, BS, EB, WIN, MOD>(P, pp, ctrl, ring, qbuf,
                              smem + NST * C::STAGE_BYTES + C::QSLOTS * C::Q_BYTES + C::ML_BYTES + C::CTRL_BYTES, warp,
                              lane);
     return;
@@ -1080,9 +1101,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         if (PROBE) {
           // ceiling probe: no math
         } else if (n_left - (P.T - 1) >= TILE) {   // every query token sees the whole tile
-          compute_tile<D, NT, BS, false>(sK, sV, qf, acc, m, l, P.scale_log2, TILE, badmask, lane, lag, [] {}, [] {});
+          compute_tile<D, NT, BS, false, false>(sK, sV, qf, acc, m, l, P.scale_log2, TILE, badmask, lane, lag, TileMod<NT>{}, [] {}, [] {});
         } else {
-          compute_tile<D, NT, BS, true>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, [] {}, [] {});
+          compute_tile<D, NT, BS, true, false>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, TileMod<NT>{}, [] {}, [] {});
           fence_proxy_async();   // our zero-fill stores must be ordered before the next TMA write
         }
         __syncwarp();

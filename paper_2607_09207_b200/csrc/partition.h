@@ -142,6 +142,14 @@ PDATTN_HD inline void locate_in_seq(int64_t r, int64_t nt, int* k, int* tile) {
 bool plan_spans(const int32_t* context_lens, const int32_t* start_tiles, int num_seqs, int num_kv_heads,
                 int n_static, int dyn_per_cta, int max_spans, SpanStart* spans, PlanParams* plan);
 
+// First key that the single token at the end of a context sees: its document's first key, or the window's.  key_begin < 0
+// and window <= 0 stand for none.
+PDATTN_HD inline int first_key(int context_len, int key_begin, int window) {
+  int lo = key_begin > 0 ? key_begin : 0;
+  if (window > 0 && context_len - window > lo) lo = context_len - window;
+  return lo;
+}
+
 // tiles of one sequence that a plan covers
 PDATTN_HD inline int64_t seq_tiles(int64_t context_len, int64_t start_tile) {
   const int64_t all = context_len > 0 ? (context_len + kTileTokens - 1) / kTileTokens : 0;

@@ -4,6 +4,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -14,6 +15,7 @@
 #include "host_common.h"
 #include "kernels.cuh"
 #include "prefix_umma.cuh"
+#include "scored.h"
 #include "partition.h"
 
 namespace {
@@ -47,6 +49,7 @@ struct CallDesc {
   int group_size = 0;                           // pdattn_decode_grouped: > 0, with the shared tiles per group
   const int32_t* prefix_tiles = nullptr;        //   device copy
   const int32_t* prefix_tiles_host = nullptr;   //   host copy
+  const pdattn_score_args* score = nullptr;     // pdattn_decode_scored: modified scores and masks
   bool static_scratch = false;                  // pdattn_decode_static_scratch: scratch is the built-in array
   int32_t* status_out = nullptr;                //   device word that receives the error word after the call
 };
@@ -55,6 +58,7 @@ struct CallDesc {
 struct LaunchCtx {
   int block_size;
   bool chain, probe, fp8;
+  bool scored;              // modified scores and masks
   bool win;                 // the short-piece instantiation of the chained-merge kernel (8-row tiles, bf16 cache)
   DevInfo* di;
   cudaStream_t stream;
@@ -115,7 +119,10 @@ pdattn_status launch_bs(const CUtensorMap& mk, const CUtensorMap& mv, const Deco
   // the kernel may be set up while its predecessor on the stream drains (and waits for it inside)
   const bool dependent = g_prof_start == nullptr;
   if (g_prof_start) cudaEventRecord(g_prof_start, stream);
-  if (lc.fp8) {
+  if (lc.scored) {
+    const pdattn_status ss = launch_scored_decode(mk, mv, P, D, BS, NT == 2, lc.fp8, grid, stream, dependent);
+    if (ss != PDATTN_OK) return ss;
+  } else if (lc.fp8) {
     using C8 = Cfg<D, NT, BS, 1>;
     auto k8 = decode_kernel<D, NT, BS, false, true, 1>;
     bool& fdone = di->fp8_attr_set[D == 128][NT == 2][BS / 32];
@@ -621,6 +628,29 @@ pdattn_status pdattn_decode_grouped_fp8(const pdattn_args* args, int group_size,
   return decode_common(&a, cd, stream);
 }
 
+pdattn_status pdattn_decode_scored(const pdattn_args* args, const pdattn_score_args* score, pdattn_stream_t stream) {
+  if (!args || !score) return PDATTN_INVALID_ARG;
+  CallDesc cd;
+  cd.score = score;
+  return decode_common(args, cd, stream);
+}
+
+pdattn_status pdattn_decode_scored_fp8(const pdattn_args* args, const pdattn_score_args* score, const float* k_scale,
+                                       const float* v_scale, pdattn_stream_t stream) {
+  if (!args || !score || !k_scale || !v_scale) return PDATTN_INVALID_ARG;
+  pdattn_args a = *args;
+  // dense pools of one-byte codes; the stride fields are not used by this variant
+  a.kv_token_stride = a.head_dim;
+  a.kv_head_stride = static_cast<int64_t>(a.block_size) * a.head_dim;
+  a.kv_block_stride = static_cast<int64_t>(a.num_kv_heads) * a.block_size * a.head_dim;
+  CallDesc cd;
+  cd.score = score;
+  cd.fp8 = true;
+  cd.k_scale = k_scale;
+  cd.v_scale = v_scale;
+  return decode_common(&a, cd, stream);
+}
+
 pdattn_status pdattn_check(void* workspace, pdattn_stream_t stream_) {
   if (!workspace) return PDATTN_INVALID_ARG;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
@@ -700,6 +730,11 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
   if (fp8 && cd.probe) return PDATTN_UNSUPPORTED;
   if (fp8 && (!cd.k_scale || !cd.v_scale)) return PDATTN_INVALID_ARG;
   if (cd.static_scratch && (grouped || fp8 || T != 1 || cd.probe)) return PDATTN_UNSUPPORTED;
+  const pdattn_score_args* score = cd.score;
+  if (score) {
+    if (!(score->logit_cap >= 0.f) || std::isinf(score->logit_cap) || score->window < 0) return PDATTN_INVALID_ARG;
+    if (a->context_lens_host && score->key_begin && !score->key_begin_host) return PDATTN_INVALID_ARG;
+  }
   // a context longer than its block_table row can describe is refused here when the host knows the lengths;
   // without a host copy the kernel treats the tokens past the row as a bad page
   if (a->context_lens_host) {
@@ -770,6 +805,14 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     start_tiles_host = g_start_tiles_host.data();
   }
 
+  if (score && a->context_lens_host && (score->key_begin || score->window > 0)) {
+    g_start_tiles_host.resize(a->num_seqs);
+    for (int sq = 0; sq < a->num_seqs; ++sq)
+      g_start_tiles_host[sq] =
+          first_key(a->context_lens_host[sq], score->key_begin ? score->key_begin_host[sq] : 0, score->window) / kTileTokens;
+    start_tiles_host = g_start_tiles_host.data();
+  }
+
   static_assert(sizeof(DecodeParams) + 2 * sizeof(CUtensorMap) <= 32000, "kernel parameters");
   DecodeParams P{};
   P.q = static_cast<const __nv_bfloat16*>(a->q);
@@ -794,6 +837,15 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
   P.box5d = 0;
   P.k_scale = fp8 ? cd.k_scale : nullptr;
   P.v_scale = fp8 ? cd.v_scale : nullptr;
+  if (score) {
+    P.key_begin = score->key_begin;
+    P.slopes = score->bias_slopes;
+    P.window = score->window;
+    if (score->logit_cap > 0.f) {
+      P.cap2 = score->logit_cap * 1.4426950408889634f;
+      P.cap_r = 2.f / score->logit_cap;
+    }
+  }
   P.tickets = reinterpret_cast<int32_t*>(ws + WS_TICKETS_OFFSET);
   // the final merge of cut units: inside the decode kernel with the chained merge (modes -1 and 1) and 8-row
   // tiles, in combine_kernel alone with the barrier merge (0), with 16-row tiles or when asked for (2)
@@ -826,7 +878,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
       P.inkernel_max = 0;
     // Batches of mostly one-tile pieces (below 1.5 tiles per unit on average) take the short-piece instantiation:
     // every warp walks the spans 32 units at a time and the tenth warp stages the query rows instead of merging.
-    if (chain && !fp8 && !cd.probe && G * T <= 8 &&
+    if (chain && !fp8 && !cd.probe && !score && G * T <= 8 &&
         (g_short_path == 1 ||
          (g_short_path == -1 && 2 * static_cast<int64_t>(P.plan.total) <
                                     static_cast<int64_t>(kAutoShortTilesX2) * a->num_seqs * a->num_kv_heads))) {
@@ -848,7 +900,8 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     cudaError_t e = launch_dependent(plan_kernel, 1, 1024, 0, stream, true, a->context_lens,
                                      static_cast<const int32_t*>(nullptr), a->num_seqs, a->num_kv_heads, n_ctas, n_dyn_max,
                                      reinterpret_cast<int32_t*>(ws + wl.prefix),
-                                     reinterpret_cast<SpanStart*>(ws + wl.spans), P.hdr, P.inkernel_max > 0 ? 1 : 0);
+                                     reinterpret_cast<SpanStart*>(ws + wl.spans), P.hdr, P.inkernel_max > 0 ? 1 : 0,
+                                     P.key_begin, P.window);
     if (e != cudaSuccess) return cuda_fail("plan_kernel launch", e);
     g_last_launches += 1;
     combine_grid = n_ctas + n_dyn_max;
@@ -872,7 +925,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
                a->kv_head_stride, a->kv_token_stride, fp8 ? kMapV8 : rank, &mv);
   if (s != PDATTN_OK) return s;
   P.box5d = rank == 5;
-  const LaunchCtx lc{a->block_size, chain, cd.probe, fp8, win, di, stream};
+  const LaunchCtx lc{a->block_size, chain, cd.probe, fp8, score != nullptr, win, di, stream};
 
   if (grouped) {
     // shared prompt tiles first: one pass per (group, kv head) for the query rows of all samples

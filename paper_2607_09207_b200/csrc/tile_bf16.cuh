@@ -10,11 +10,13 @@ namespace pdattn {
 // ------------------------------------------------------------------------------------------
 // after_k() is called right after the last read of the K tile, before_v() right before the first access to the V
 // tile (with split stage halves the caller releases K in the one and waits for V in the other).
-template <int D, int NT, int BS, bool TAIL, class AfterK, class BeforeV>
+// MOD: modified scores and a first token (TileMod); its masked instantiation (TAIL) also masks the tokens before that one.
+template <int D, int NT, int BS, bool TAIL, bool MOD, class AfterK, class BeforeV>
 __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uint32_t (&qf)[NT][D / 16][2],
                                              float (&acc)[NT][D / 16][4], float (&m)[NT][2], float (&l)[NT][2],
                                              float sl2, int n_left, uint32_t badmask, int lane,
-                                             const int (&lag)[NT][2], AfterK after_k, BeforeV before_v) {
+                                             const int (&lag)[NT][2], const TileMod<NT>& md, AfterK after_k,
+                                             BeforeV before_v) {
   // n_left: tokens of the sequence from this tile's first one on (>= TILE unless TAIL)
   const int n_valid = n_left < TILE ? n_left : TILE;
   using C = Cfg<D, NT, BS>;
@@ -65,12 +67,15 @@ __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uin
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float v = sc[j][nt][r] * sl2;
+        float v;
+        if constexpr (MOD) v = md.score(sc[j][nt][r], sl2, nt, r & 1, n_left - 1 - (j * 16 + trow + ((r & 2) ? 8 : 0)));
+        else v = sc[j][nt][r] * sl2;
         if (TAIL) {
           // lag: tokens at the end of the context that this column's query token must not see (it sits
           // that many positions before the last one; 0 for plain decode)
           const int tok = j * 16 + trow + ((r & 2) ? 8 : 0);
           if (tok >= n_left - lag[nt][r & 1]) v = NEG_INF;
+          if (MOD && tok < md.head) v = NEG_INF;
         }
         if (dead_page) v = NEG_INF;
         sc[j][nt][r] = v;
@@ -148,6 +153,14 @@ __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uin
       const int page = tok / BS, row = tok % BS;
       const uint32_t a = sV + page * C::PAGE_BYTES + (ch >> 3) * C::HALF_BYTES + row * 128 + ((ch & 7) << 4);
       asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+    }
+    if constexpr (MOD) {     // the rows before the first token, for the same reason
+      for (int idx = lane; idx < min(md.head, n_valid) * (D / 8); idx += 32) {
+        const int tok = idx / (D / 8), ch = idx % (D / 8);
+        const int page = tok / BS, row = tok % BS;
+        const uint32_t a = sV + page * C::PAGE_BYTES + (ch >> 3) * C::HALF_BYTES + row * 128 + ((ch & 7) << 4);
+        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+      }
     }
     __syncwarp();
   }

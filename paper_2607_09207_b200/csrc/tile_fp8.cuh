@@ -22,11 +22,11 @@ namespace pdattn {
 // the score MMA holds token pi(rho) of its 16-token group -- a matter of the row addresses handed to
 // ldmatrix for K.
 // ------------------------------------------------------------------------------------------
-template <int D, int NT, int BS, bool TAIL>
+template <int D, int NT, int BS, bool TAIL, bool MOD>
 __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const uint32_t (&qf)[NT][D / 16][2],
                                                 float (&acc)[NT][D / 16][4], float (&m)[NT][2], float (&l)[NT][2],
                                                 float sl2, int n_left, uint32_t badmask, int lane,
-                                                const int (&lag)[NT][2]) {
+                                                const int (&lag)[NT][2], const TileMod<NT>& md) {
   constexpr int GROUPS = TILE / 16;
   const float NEG_INF = __int_as_float(0xff800000);
   const int n_valid = n_left < TILE ? n_left : TILE;
@@ -79,10 +79,13 @@ __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const 
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float v = sc[j][nt][r] * sl2;
+        float v;
+        if constexpr (MOD) v = md.score(sc[j][nt][r], sl2, nt, r & 1, n_left - 1 - (j * 16 + tok0 + ((r & 2) ? 2 : 0)));
+        else v = sc[j][nt][r] * sl2;
         if (TAIL) {
           const int tok = j * 16 + tok0 + ((r & 2) ? 2 : 0);
           if (tok >= n_left - lag[nt][r & 1]) v = NEG_INF;
+          if (MOD && tok < md.head) v = NEG_INF;
         }
         if (dead_page) v = NEG_INF;
         sc[j][nt][r] = v;
@@ -148,6 +151,10 @@ __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const 
       if (TAIL) {
         const int keep = n_valid - (j * 16 + (lane & 3) * 4);   // of this lane's four tokens
         keep_mask = keep >= 4 ? 0xffffffffu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
+        if constexpr (MOD) {                                    // and those before the first token
+          const int drop = md.head - (j * 16 + (lane & 3) * 4);
+          keep_mask &= drop <= 0 ? 0xffffffffu : (drop >= 4 ? 0u : ~((1u << (8 * drop)) - 1u));
+        }
       }
 #pragma unroll
       for (int jp = 0; jp < D / 32; ++jp) {

@@ -39,6 +39,7 @@ EXPORTS = [
     "pdattn_grouped_workspace_size", "pdattn_decode_grouped",
     "pdattn_multi_workspace_size", "pdattn_decode_multi", "pdattn_decode_fp8", "pdattn_append_kv_fp8", "pdattn_decode_fp8_multi",
     "pdattn_rope_append", "pdattn_rope_append_fp8", "pdattn_prefill_workspace_size", "pdattn_prefill",
+    "pdattn_decode_scored", "pdattn_decode_scored_fp8",
     "pdattn_pages_workspace_size", "pdattn_pages_init", "pdattn_pages_reserve", "pdattn_pages_fork", "pdattn_pages_free",
     "pdattn_pages_compact", "pdattn_pages_copy",
 ]
@@ -139,6 +140,8 @@ def lib():
         L.pdattn_check.argtypes = [vp, vp]
         L.pdattn_rope_append.argtypes = [ctypes.POINTER(RopeArgs), vp]
         L.pdattn_rope_append_fp8.argtypes = [ctypes.POINTER(RopeArgs), vp, vp, vp]
+        L.pdattn_decode_scored.argtypes = [ctypes.POINTER(Args), ctypes.POINTER(ScoreArgs), vp]
+        L.pdattn_decode_scored_fp8.argtypes = [ctypes.POINTER(Args), ctypes.POINTER(ScoreArgs), vp, vp, vp]
         L.pdattn_prefill_workspace_size.argtypes = [i32] * 6 + [ctypes.POINTER(sz)]
         L.pdattn_prefill.argtypes = [ctypes.POINTER(Args), vp, i32, ctypes.POINTER(ScoreArgs), vp]
         pool = ctypes.POINTER(PoolArgs)
@@ -612,6 +615,53 @@ def prefill(q, k_cache, v_cache, block_table, context_lens, cu_tokens, scale, ou
         score.fits(where, a.num_q_heads, q.shape[0], a.num_seqs)
     st = lib().pdattn_prefill(ctypes.byref(a), cu_tokens.data_ptr(), q.shape[0],
                               ctypes.byref(score.args) if score is not None else None, _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def _lens_host(where, a: Args, context_lens_host):
+    """Puts the host copy of the lengths into the argument block; the array must outlive the call."""
+    if context_lens_host is None:
+        return None
+    lens = np.ascontiguousarray(context_lens_host, dtype=np.int32)
+    if lens.size != a.num_seqs:
+        raise ValueError(f"{where}: context_lens_host has {lens.size} entries for {a.num_seqs} sequences")
+    a.context_lens_host = lens.ctypes.data
+    return lens
+
+
+def decode_scored(q, k_cache, v_cache, block_table, context_lens, scale, out, workspace, score: Score,
+                  context_lens_host: Optional[np.ndarray] = None, stream=None, check: bool = True) -> int:
+    """pdattn_decode_scored: decode_ex with the modified scores and masks of `score`."""
+    where = "pdattn_decode_scored"
+    _expect(where, torch.bfloat16, k_cache, v_cache)
+    _same_cache(where, k_cache, v_cache)
+    a = _step_args(where, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace)
+    if q.shape[0] != a.num_seqs:
+        raise ValueError(f"{where}: {q.shape[0]} query rows for {a.num_seqs} sequences")
+    score.fits(where, a.num_q_heads, a.num_seqs, a.num_seqs)
+    keep = _lens_host(where, a, context_lens_host)
+    st = lib().pdattn_decode_scored(ctypes.byref(a), ctypes.byref(score.args), _stream_ptr(stream))
+    del keep
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def decode_scored_fp8(q, k8, v8, k_scale, v_scale, block_table, context_lens, scale, out, workspace, score: Score,
+                      context_lens_host: Optional[np.ndarray] = None, stream=None, check: bool = True) -> int:
+    """pdattn_decode_scored_fp8: decode_scored over the e4m3 code pools of decode_fp8."""
+    where = "pdattn_decode_scored_fp8"
+    _code_pools(where, k8, v8, k_scale, v_scale)
+    a = _step_args(where, q, k8, v8, block_table, context_lens, scale, out, workspace)
+    if q.shape[0] != a.num_seqs:
+        raise ValueError(f"{where}: {q.shape[0]} query rows for {a.num_seqs} sequences")
+    score.fits(where, a.num_q_heads, a.num_seqs, a.num_seqs)
+    keep = _lens_host(where, a, context_lens_host)
+    st = lib().pdattn_decode_scored_fp8(ctypes.byref(a), ctypes.byref(score.args), k_scale.data_ptr(), v_scale.data_ptr(),
+                                        _stream_ptr(stream))
+    del keep
     if check and st != OK:
         raise PdattnError(st, where)
     return st

@@ -142,3 +142,27 @@ def test_prefill_refusals():
     assert pdattn.prefill_workspace_size(3, 9, 4, 2, 64) >= 8448
     with pytest.raises(pdattn.PdattnError):
         pdattn.prefill_workspace_size(3, -1, 4, 2, 64)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_decode_scored_refusals(fp8):
+    L = pdattn.lib()
+
+    def call(score=pdattn.ScoreArgs(), **kw):
+        a, s = ctypes.byref(step(**kw)), None if score is None else ctypes.byref(score)
+        return L.pdattn_decode_scored_fp8(a, s, P, P, None) if fp8 else L.pdattn_decode_scored(a, s, None)
+    assert call(score=None) == pdattn.INVALID_ARG
+    assert call(num_seqs=0) == pdattn.OK
+    for kw, why in BAD_STEPS:
+        if not (fp8 and any("stride" in k for k in kw)):
+            assert call(**kw) == why, kw
+    for cap, window in BAD_SCORES:
+        assert call(pdattn.ScoreArgs(cap, None, window, None, None, None)) == pdattn.INVALID_ARG
+    lens = (ctypes.c_int32 * 3)(5, 6, 64)
+    host = ctypes.cast(lens, ctypes.c_void_p).value
+    assert call(pdattn.ScoreArgs(0.0, None, 0, P, None, None), context_lens_host=host) == pdattn.INVALID_ARG
+    lens[2] = 65                                                                 # longer than its table row
+    assert call(context_lens_host=host) == pdattn.INVALID_ARG
+    if fp8:
+        a, s = ctypes.byref(step()), ctypes.byref(pdattn.ScoreArgs())
+        assert L.pdattn_decode_scored_fp8(a, s, None, P, None) == L.pdattn_decode_scored_fp8(a, s, P, None, None) == pdattn.INVALID_ARG
