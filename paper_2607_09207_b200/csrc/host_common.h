@@ -52,7 +52,7 @@ PDATTN_HIDDEN pdattn_status make_map(const void* ptr, int d, int bs, int hkv, in
 // kernel itself waits (griddepcontrol.wait) before it touches global memory.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_dependent(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t stream, bool dependent,
-                             Args... args) {
+                             const Args&... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(block);

@@ -118,7 +118,7 @@ pdattn_status pdattn_prefill(const pdattn_args* a, const int32_t* cu_tokens, int
     P.window = score->window;
     if (cap) {
       P.cap2 = score->logit_cap * kLog2e;
-      P.cap_k = 2.f * a->scale / score->logit_cap * kLog2e;
+      P.cap_x = a->scale / score->logit_cap;
     }
   }
   // scores are brought to base-2 units one by one for a bias, and for a scale that is not positive (the other form takes the

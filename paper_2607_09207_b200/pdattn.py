@@ -167,7 +167,7 @@ def lib():
 
 def _stream_ptr(stream) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return int(stream.cuda_stream)
 
 
@@ -441,66 +441,73 @@ def _ptr(t) -> Optional[int]:
 
 def _expect(where: str, dtype, *tensors):
     """dtype and device checks of the tensors a call takes (None is passed over): the library sees plain pointers."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is None:
-            continue
-        if t.dtype != dtype:
-            raise TypeError(f"{where}: a tensor of {dtype} is wanted, got {t.dtype}")
-        if t.device.type != "cuda" or t.device.index != here:
+        if t is not None and (t.dtype is not dtype or t.get_device() != here):
+            if t.dtype is not dtype:
+                raise TypeError(f"{where}: a tensor of {dtype} is wanted, got {t.dtype}")
             raise ValueError(f"{where}: a tensor lives on {t.device}, the current device is cuda:{here}")
 
 
-def _dense(where: str, *tensors):
+def _expect_dense(where: str, dtype, *tensors):
+    """_expect, and no gaps between the elements."""
+    here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and not t.is_contiguous():
+        if t is not None and (t.dtype is not dtype or t.get_device() != here or not t.is_contiguous()):
+            _expect(where, dtype, t)
             raise ValueError(f"{where}: a dense tensor is wanted, got strides {t.stride()} for shape {tuple(t.shape)}")
 
 
-def _same_cache(where: str, k_cache, v_cache):
+def _expect_caches(where: str, k_cache, v_cache):
+    """bf16 caches [page, kv_head, slot, dim] that can share one set of strides."""
+    _expect(where, torch.bfloat16, k_cache, v_cache)
     if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.stride(3) != 1:
         raise ValueError(f"{where}: k_cache and v_cache need the same shape and strides, head_dim contiguous")
 
 
-def _code_pools(where: str, k8, v8, k_scale, v_scale):
+def _expect_codes(where: str, k8, v8, k_scale, v_scale):
+    """The code pools of decode_fp8 and their scales."""
+    _expect_dense(where, torch.uint8, k8, v8)
+    _expect_dense(where, torch.float32, k_scale, v_scale)
     NB, Hkv, bs, d = k8.shape
-    _expect(where, torch.uint8, k8, v8)
-    _expect(where, torch.float32, k_scale, v_scale)
-    _dense(where, k8, v8, k_scale, v_scale)
-    if tuple(v8.shape) != (NB, Hkv, d, bs) or k_scale.numel() != Hkv or v_scale.numel() != Hkv:
+    if v8.shape != (NB, Hkv, d, bs) or k_scale.numel() != Hkv or v_scale.numel() != Hkv:
         raise ValueError(f"{where}: code pools {tuple(k8.shape)} and {tuple(v8.shape)} with {k_scale.numel()} and "
                          f"{v_scale.numel()} scales do not belong together")
 
 
-def _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, cu_tokens,
+def _token_stride(where, t, shape) -> int:
+    """Elements between two tokens of t [N, heads, d], whose heads lie densely."""
+    N, H, d = shape
+    st = t.stride()
+    if t.shape != shape or (N and (st[2] != 1 or (H > 1 and st[1] != d))):
+        raise ValueError(f"{where}: {N} rows of {H} dense heads of {d} are wanted, got shape {tuple(t.shape)}, strides {st}")
+    return st[0] if N > 1 else H * d
+
+
+def _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, kv_strides, block_table, context_lens, inv_freq, cu_tokens,
                rotary_dim, interleaved, magnitude, workspace) -> RopeArgs:
-    N, Hkv, d = k_new.shape
-    NB, bs = k_cache.shape[0], k_cache.shape[2]
-    Hq = 0 if q is None else q.shape[1]
-    _expect(where, torch.bfloat16, q, q_out, k_new, v_new)
-    _expect(where, torch.int32, block_table, context_lens, cu_tokens)
-    _expect(where, torch.float32, inv_freq)
-    _dense(where, q_out, block_table, context_lens, cu_tokens, inv_freq)
-    for t in (q, k_new, v_new):
-        if t is not None and N and (t.shape[0] != N or t.shape[2] != d or t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != d)):
-            raise ValueError(f"{where}: rows of dense heads are wanted, got strides {t.stride()} for shape {tuple(t.shape)}")
-    S = context_lens.numel()
+    shape = k_new.shape
+    N, Hkv, d = shape
+    NB, heads, bs, dim = k_cache.shape
+    _expect(where, torch.bfloat16, q, k_new, v_new)
+    _expect_dense(where, torch.bfloat16, q_out)
+    _expect_dense(where, torch.int32, block_table, context_lens, cu_tokens)
+    _expect_dense(where, torch.float32, inv_freq)
+    S, MB = block_table.shape
     rotary = d if rotary_dim is None else int(rotary_dim)
-    if (v_new.shape != k_new.shape or tuple(k_cache.shape[1::2]) != (Hkv, d) or block_table.shape[0] != S
-            or (cu_tokens is not None and cu_tokens.numel() != S + 1) or inv_freq.numel() * 2 != rotary
-            or (q is not None and (q_out is None or tuple(q_out.shape) != tuple(q.shape)))):
+    if (heads != Hkv or dim != d or context_lens.numel() != S or inv_freq.numel() * 2 != rotary
+            or (cu_tokens is not None and cu_tokens.numel() != S + 1)):
         raise ValueError(f"{where}: shapes do not belong together")
-    a = RopeArgs()
-    a.q, a.q_out, a.k_new, a.v_new = _ptr(q), _ptr(q_out) if q is not None else None, k_new.data_ptr(), v_new.data_ptr()
-    a.q_token_stride = 0 if q is None else q.stride(0) if N > 1 else Hq * d
-    a.k_token_stride, a.v_token_stride = (k_new.stride(0), v_new.stride(0)) if N > 1 else (Hkv * d, Hkv * d)
-    a.k_cache, a.v_cache, a.block_table = k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr()
-    a.context_lens, a.cu_tokens, a.inv_freq = context_lens.data_ptr(), _ptr(cu_tokens), inv_freq.data_ptr()
-    a.magnitude, a.rotary_dim, a.interleaved = float(magnitude), rotary, int(bool(interleaved))
-    a.num_tokens, a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = N, S, Hq, Hkv, d, bs
-    a.max_blocks_per_seq, a.num_blocks = block_table.shape[1], NB
-    a.workspace = _ptr(workspace)
-    return a
+    Hq, q_stride = 0, 0
+    if q is not None:
+        Hq = q.shape[1]
+        q_stride = _token_stride(where, q, (N, Hq, d))
+        if q_out is None or q_out.shape != (N, Hq, d):
+            raise ValueError(f"{where}: q_out has the shape of q")
+    return RopeArgs(_ptr(q), _ptr(q_out) if Hq else None, k_new.data_ptr(), v_new.data_ptr(), q_stride,
+                    _token_stride(where, k_new, shape), _token_stride(where, v_new, shape), k_cache.data_ptr(), v_cache.data_ptr(),
+                    block_table.data_ptr(), context_lens.data_ptr(), _ptr(cu_tokens), inv_freq.data_ptr(), magnitude, rotary,
+                    1 if interleaved else 0, N, S, Hq, Hkv, d, bs, MB, NB, *kv_strides, _ptr(workspace))
 
 
 def rope_append(q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, *, cu_tokens=None,
@@ -510,11 +517,9 @@ def rope_append(q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_l
     the paged cache beside v_new ([N, Hkv, d]).  context_lens counts the new tokens; cu_tokens [S + 1] (None: one new
     token per sequence)."""
     where = "pdattn_rope_append"
-    _expect(where, torch.bfloat16, k_cache, v_cache)
-    _same_cache(where, k_cache, v_cache)
-    a = _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, cu_tokens,
-                   rotary_dim, interleaved, magnitude, workspace)
-    a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = k_cache.stride(0), k_cache.stride(1), k_cache.stride(2)
+    _expect_caches(where, k_cache, v_cache)
+    a = _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, inv_freq,
+                   cu_tokens, rotary_dim, interleaved, magnitude, workspace)
     st = lib().pdattn_rope_append(ctypes.byref(a), _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
@@ -526,8 +531,8 @@ def rope_append_fp8(q, k_new, v_new, q_out, k8, v8, k_scale, v_scale, block_tabl
                     stream=None, check: bool = True) -> int:
     """pdattn_rope_append_fp8: rope_append into the e4m3 code pools of decode_fp8."""
     where = "pdattn_rope_append_fp8"
-    _code_pools(where, k8, v8, k_scale, v_scale)
-    a = _rope_args(where, q, k_new, v_new, q_out, k8, v8, block_table, context_lens, inv_freq, cu_tokens, rotary_dim,
+    _expect_codes(where, k8, v8, k_scale, v_scale)
+    a = _rope_args(where, q, k_new, v_new, q_out, k8, v8, (0, 0, 0), block_table, context_lens, inv_freq, cu_tokens, rotary_dim,
                    interleaved, magnitude, workspace)
     st = lib().pdattn_rope_append_fp8(ctypes.byref(a), k_scale.data_ptr(), v_scale.data_ptr(), _stream_ptr(stream))
     if check and st != OK:
@@ -541,9 +546,8 @@ class Score:
 
     def __init__(self, logit_cap: float = 0.0, bias_slopes=None, window: int = 0, key_begin=None, prefix_lens=None,
                  key_begin_host: Optional[np.ndarray] = None):
-        _expect("Score", torch.float32, bias_slopes)
-        _expect("Score", torch.int32, key_begin, prefix_lens)
-        _dense("Score", bias_slopes, key_begin, prefix_lens)
+        _expect_dense("Score", torch.float32, bias_slopes)
+        _expect_dense("Score", torch.int32, key_begin, prefix_lens)
         host = None if key_begin_host is None else np.ascontiguousarray(key_begin_host, dtype=np.int32)
         self.keep = (bias_slopes, key_begin, prefix_lens, host)
         self.args = ScoreArgs(float(logit_cap), _ptr(bias_slopes), int(window), _ptr(key_begin), _ptr(prefix_lens),
@@ -551,32 +555,36 @@ class Score:
 
     def fits(self, where: str, num_q_heads: int, num_tokens: int, num_seqs: int):
         slopes, begin, prefix, host = self.keep
-        for what, t, n in (("bias_slopes", slopes, num_q_heads), ("key_begin", begin, num_tokens),
-                           ("prefix_lens", prefix, num_seqs)):
-            if t is not None and t.numel() != n:
-                raise ValueError(f"{where}: {what} has {t.numel()} entries, {n} are wanted")
+        if slopes is not None and slopes.numel() != num_q_heads:
+            raise ValueError(f"{where}: bias_slopes has {slopes.numel()} entries for {num_q_heads} query heads")
+        if begin is not None and begin.numel() != num_tokens:
+            raise ValueError(f"{where}: key_begin has {begin.numel()} entries for {num_tokens} query tokens")
         if host is not None and host.size != num_tokens:
-            raise ValueError(f"{where}: key_begin_host has {host.size} entries, {num_tokens} are wanted")
+            raise ValueError(f"{where}: key_begin_host has {host.size} entries for {num_tokens} query tokens")
+        if prefix is not None and prefix.numel() != num_seqs:
+            raise ValueError(f"{where}: prefix_lens has {prefix.numel()} entries for {num_seqs} sequences")
 
 
-def _step_args(where, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace) -> Args:
+def _step_args(where, q, k_cache, v_cache, kv_strides, block_table, context_lens, scale, out, workspace,
+               context_lens_host=None) -> Args:
     """The argument block of a call over bf16 or code caches whose q and out are [rows, Hq, d]."""
-    N, Hq, d = q.shape
-    NB, Hkv, bs = k_cache.shape[:3]
-    _expect(where, torch.bfloat16, q, out)
-    _expect(where, torch.int32, block_table, context_lens)
-    _dense(where, q, out, block_table, context_lens)
-    S = context_lens.numel()
-    if k_cache.shape[3] != d or tuple(out.shape) != (N, Hq, d) or block_table.dim() != 2 or block_table.shape[0] != S:
+    _expect_dense(where, torch.bfloat16, q, out)
+    _expect_dense(where, torch.int32, block_table, context_lens)
+    shape = q.shape
+    _, Hq, d = shape
+    NB, Hkv, bs, dim = k_cache.shape
+    S, MB = block_table.shape
+    if dim != d or out.shape != shape or context_lens.numel() != S:
         raise ValueError(f"{where}: shapes do not belong together")
-    a = Args()
-    a.q, a.k_cache, a.v_cache, a.out = q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr()
-    a.block_table, a.context_lens = block_table.data_ptr(), context_lens.data_ptr()
-    a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = S, Hq, Hkv, d, bs
-    a.max_blocks_per_seq, a.num_blocks = block_table.shape[1], NB
-    a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = k_cache.stride(0), k_cache.stride(1), k_cache.stride(2)
-    a.scale = float(scale)
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    host = None
+    if context_lens_host is not None:
+        host = np.ascontiguousarray(context_lens_host, dtype=np.int32)
+        if host.size != S:
+            raise ValueError(f"{where}: context_lens_host has {host.size} entries for {S} sequences")
+    a = Args(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), block_table.data_ptr(),
+             context_lens.data_ptr(), None if host is None else host.ctypes.data, S, Hq, Hkv, d, bs, MB, NB, *kv_strides, scale,
+             workspace.data_ptr(), workspace.numel())
+    a.keep = host                                  # lives as long as the block
     return a
 
 
@@ -604,11 +612,9 @@ def prefill(q, k_cache, v_cache, block_table, context_lens, cu_tokens, scale, ou
     """pdattn_prefill: q and out [N, Hq, d]; the tokens cu_tokens[s] .. cu_tokens[s + 1] are the last ones of sequence s's
     context_lens[s] (their K and V are in the caches); each attends by the rules of `score` (None: plain causal)."""
     where = "pdattn_prefill"
-    _expect(where, torch.bfloat16, k_cache, v_cache)
-    _expect(where, torch.int32, cu_tokens)
-    _dense(where, cu_tokens)
-    _same_cache(where, k_cache, v_cache)
-    a = _step_args(where, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace)
+    _expect_caches(where, k_cache, v_cache)
+    _expect_dense(where, torch.int32, cu_tokens)
+    a = _step_args(where, q, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, scale, out, workspace)
     if cu_tokens.numel() != a.num_seqs + 1:
         raise ValueError(f"{where}: cu_tokens has {cu_tokens.numel()} entries for {a.num_seqs} sequences")
     if score is not None:
@@ -620,48 +626,30 @@ def prefill(q, k_cache, v_cache, block_table, context_lens, cu_tokens, scale, ou
     return st
 
 
-def _lens_host(where, a: Args, context_lens_host):
-    """Puts the host copy of the lengths into the argument block; the array must outlive the call."""
-    if context_lens_host is None:
-        return None
-    lens = np.ascontiguousarray(context_lens_host, dtype=np.int32)
-    if lens.size != a.num_seqs:
-        raise ValueError(f"{where}: context_lens_host has {lens.size} entries for {a.num_seqs} sequences")
-    a.context_lens_host = lens.ctypes.data
-    return lens
-
-
 def decode_scored(q, k_cache, v_cache, block_table, context_lens, scale, out, workspace, score: Score,
                   context_lens_host: Optional[np.ndarray] = None, stream=None, check: bool = True) -> int:
     """pdattn_decode_scored: decode_ex with the modified scores and masks of `score`."""
     where = "pdattn_decode_scored"
-    _expect(where, torch.bfloat16, k_cache, v_cache)
-    _same_cache(where, k_cache, v_cache)
-    a = _step_args(where, q, k_cache, v_cache, block_table, context_lens, scale, out, workspace)
-    if q.shape[0] != a.num_seqs:
-        raise ValueError(f"{where}: {q.shape[0]} query rows for {a.num_seqs} sequences")
-    score.fits(where, a.num_q_heads, a.num_seqs, a.num_seqs)
-    keep = _lens_host(where, a, context_lens_host)
-    st = lib().pdattn_decode_scored(ctypes.byref(a), ctypes.byref(score.args), _stream_ptr(stream))
-    del keep
-    if check and st != OK:
-        raise PdattnError(st, where)
-    return st
+    _expect_caches(where, k_cache, v_cache)
+    a = _step_args(where, q, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, scale, out, workspace,
+                   context_lens_host)
+    return _scored(where, lib().pdattn_decode_scored, q, a, score, (), stream, check)
 
 
 def decode_scored_fp8(q, k8, v8, k_scale, v_scale, block_table, context_lens, scale, out, workspace, score: Score,
                       context_lens_host: Optional[np.ndarray] = None, stream=None, check: bool = True) -> int:
     """pdattn_decode_scored_fp8: decode_scored over the e4m3 code pools of decode_fp8."""
     where = "pdattn_decode_scored_fp8"
-    _code_pools(where, k8, v8, k_scale, v_scale)
-    a = _step_args(where, q, k8, v8, block_table, context_lens, scale, out, workspace)
+    _expect_codes(where, k8, v8, k_scale, v_scale)
+    a = _step_args(where, q, k8, v8, (0, 0, 0), block_table, context_lens, scale, out, workspace, context_lens_host)
+    return _scored(where, lib().pdattn_decode_scored_fp8, q, a, score, (k_scale.data_ptr(), v_scale.data_ptr()), stream, check)
+
+
+def _scored(where, call, q, a: Args, score: Score, scales, stream, check) -> int:
     if q.shape[0] != a.num_seqs:
         raise ValueError(f"{where}: {q.shape[0]} query rows for {a.num_seqs} sequences")
     score.fits(where, a.num_q_heads, a.num_seqs, a.num_seqs)
-    keep = _lens_host(where, a, context_lens_host)
-    st = lib().pdattn_decode_scored_fp8(ctypes.byref(a), ctypes.byref(score.args), k_scale.data_ptr(), v_scale.data_ptr(),
-                                        _stream_ptr(stream))
-    del keep
+    st = call(ctypes.byref(a), ctypes.byref(score.args), *scales, _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
     return st
@@ -672,8 +660,7 @@ class PagePool:
     free_count [1]."""
 
     def __init__(self, ref_counts, free_list, free_count):
-        _expect("PagePool", torch.int32, ref_counts, free_list, free_count)
-        _dense("PagePool", ref_counts, free_list, free_count)
+        _expect_dense("PagePool", torch.int32, ref_counts, free_list, free_count)
         if free_list.numel() != ref_counts.numel() or free_count.numel() != 1:
             raise ValueError("PagePool: ref_counts and free_list have one entry per page, free_count has one")
         self.ref_counts, self.free_list, self.free_count = ref_counts, free_list, free_count
@@ -708,8 +695,7 @@ def alloc_pages_workspace(num_blocks: int, num_seqs: int, device="cuda", stream=
 
 
 def _pages_check(where, block_table, context_lens, *lists):
-    _expect(where, torch.int32, block_table, context_lens, *lists)
-    _dense(where, block_table, context_lens, *lists)
+    _expect_dense(where, torch.int32, block_table, context_lens, *lists)
     if block_table.dim() != 2 or context_lens.numel() != block_table.shape[0]:
         raise ValueError(f"{where}: block_table [S, MB] and context_lens [S] do not belong together")
 
@@ -782,22 +768,19 @@ def pages_copy(k_cache, v_cache, copy_src, copy_dst, workspace=None, stream=None
     """pdattn_pages_copy: page copy_src[i] to page copy_dst[i] in both caches ([page, kv_head, slot, dim] bf16, or the
     uint8 code pools of decode_fp8)."""
     where = "pdattn_pages_copy"
-    _expect(where, torch.int32, copy_src, copy_dst)
-    _dense(where, copy_src, copy_dst)
+    _expect_dense(where, torch.int32, copy_src, copy_dst)
     if copy_src.numel() != copy_dst.numel():
         raise ValueError(f"{where}: copy_src and copy_dst have the same length")
     NB, Hkv, bs, d = k_cache.shape
     if k_cache.dtype == torch.uint8:
-        _expect(where, torch.uint8, k_cache, v_cache)
-        _dense(where, k_cache, v_cache)
+        _expect_dense(where, torch.uint8, k_cache, v_cache)
         if tuple(v_cache.shape) != (NB, Hkv, d, bs):
             raise ValueError(f"{where}: code pools {tuple(k_cache.shape)} and {tuple(v_cache.shape)} do not belong together")
     else:
-        _expect(where, torch.bfloat16, k_cache, v_cache)
-        _same_cache(where, k_cache, v_cache)
+        _expect_caches(where, k_cache, v_cache)
     st = lib().pdattn_pages_copy(k_cache.data_ptr(), v_cache.data_ptr(), copy_src.data_ptr(), copy_dst.data_ptr(),
-                                 copy_src.numel(), Hkv, d, bs, NB, k_cache.element_size(), k_cache.stride(0),
-                                 k_cache.stride(1), k_cache.stride(2), _ptr(workspace), _stream_ptr(stream))
+                                 copy_src.numel(), Hkv, d, bs, NB, k_cache.element_size(), *k_cache.stride()[:3],
+                                 _ptr(workspace), _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
     return st
