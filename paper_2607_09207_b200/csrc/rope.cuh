@@ -12,6 +12,8 @@
 //     sine and cosine of the reduced turn in 32.  pos * inv_freq in 32 bits would be off by up to 0.03 rad at 10^6.
 //   - A thread owns two 16-byte chunks of a row that rotate into each other (half layout: R/2 elements apart;
 //     interleaved and pass-through: neighbours), so every load and store is 16 bytes wide and q_out may be q.
+//   - 512 threads a block, three blocks an SM: measured on 17,492 prompt tokens of 40 + 8 + 8 heads, 91 us (5.5 TB/s; 256
+//     threads with a deeper unroll 95), and on one token of 256 sequences, 28 + 4 + 4 heads, 3.4 us (3.6).
 //   - Products and sums in fp32, one rounding per element (bf16 nearest even; e4m3 of value / scale for the fp8 cache).
 #pragma once
 
@@ -19,7 +21,7 @@
 
 namespace pdattn {
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 512;
 constexpr int kRopeMaxTokens = 8;      // tokens of a block (one warp each looks its token up)
 
 struct RopeParams {
@@ -53,7 +55,7 @@ __device__ __forceinline__ int find_sequence(const int32_t* __restrict__ cu, int
 }
 
 template <int D, bool FP8>
-__global__ void __launch_bounds__(kRopeThreads)
+__global__ void __launch_bounds__(kRopeThreads, 3)
 rope_append_kernel(const __grid_constant__ RopeParams P) {
   constexpr int TPR = D / 16;          // threads per row: two 16-byte chunks each
   __shared__ float2 cs[kRopeMaxTokens][D / 2];
@@ -98,7 +100,7 @@ rope_append_kernel(const __grid_constant__ RopeParams P) {
   const int rows = P.Hq + 2 * P.Hkv;
   const int rot = P.R / 16;            // chunk pairs of a row that rotate
   const int items = nt * rows * TPR;
-#pragma unroll 2
+#pragma unroll 1
   for (int i = tid; i < items; i += kRopeThreads) {
     const int p = i % TPR, tr = i / TPR;
     const int k = tr / rows, r = tr - k * rows;
