@@ -300,7 +300,9 @@ typedef struct {
  * The softmax weights are rounded to bf16 for the second product; fp32 otherwise.
  *   - Bad page ids, slots past the end and pages that no row references: as in pdattn_decode_ex.
  *   - Rows of out at or past cu_tokens[num_seqs] are left as they were.  A token before position 0 gets zeros.
- *   - args->workspace holds pdattn_prefill_workspace_size() bytes.
+ *   - args->workspace holds pdattn_prefill_workspace_size() bytes.  Calls of few tokens are cut along the keys so that long
+ *     contexts keep every SM busy; that takes room for the parts' results.  A smaller workspace (8448 bytes at least) is taken
+ *     too: such calls are then cut into fewer parts, or not at all (another order of summation: other rounding).
  */
 pdattn_status pdattn_prefill_workspace_size(int num_seqs, int num_tokens, int num_q_heads, int num_kv_heads, int head_dim,
                                             int block_size, size_t* device_bytes);

@@ -51,10 +51,10 @@ PDATTN_HIDDEN pdattn_status make_map(const void* ptr, int d, int bs, int hkv, in
 // Launch that may begin while the kernel before it on the stream drains (programmatic dependent launch); the
 // kernel itself waits (griddepcontrol.wait) before it touches global memory.
 template <typename... KArgs, typename... Args>
-cudaError_t launch_dependent(void (*kernel)(KArgs...), int grid, int block, size_t smem, cudaStream_t stream, bool dependent,
+cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, int block, size_t smem, cudaStream_t stream, bool dependent,
                              const Args&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

@@ -31,11 +31,27 @@ pdattn_status launch_prefill_kernel(const CUtensorMap& mq, const CUtensorMap& mk
     if (e != cudaSuccess) return cuda_fail("cudaFuncSetAttribute", e);
     attr_set[dev] = true;
   }
-  const int grid = P.n_items < sms ? P.n_items : sms;
+  const int units = P.n_items * P.splits;
+  const int grid = units < sms ? units : sms;
   const cudaError_t e = launch_dependent(kern, grid, PF_NTHREADS, C::DYN_BYTES, stream, true, mq, mk, mv, P);
   if (e != cudaSuccess) return cuda_fail("prefill_kernel launch", e);
+  if (P.splits > 1) {
+    const cudaError_t j = launch_dependent(prefill_join_kernel<D>, dim3(P.n_items, 2, D / 8), 128, 0, stream, true, P);
+    if (j != cudaSuccess) return cuda_fail("prefill_join_kernel launch", j);
+  }
   return PDATTN_OK;
 }
+
+// Items of a call (pair slots x KV heads), and the parts each may be cut into along the keys: as many as fill PF_UNITS CTAs.
+constexpr int PF_UNITS = 148;
+int64_t prefill_items(int num_seqs, int num_tokens, int Hq, int Hkv) {
+  return (static_cast<int64_t>(num_tokens) / (2 * (128 / (Hq / Hkv))) + num_seqs) * Hkv;
+}
+int prefill_splits(int64_t items) { return items > 0 && items <= PF_UNITS / 2 ? static_cast<int>(PF_UNITS / items) : 1; }
+size_t prefill_part_bytes(int head_dim) { return static_cast<size_t>(2) * (head_dim + 2) * 128 * 4; }
+constexpr size_t kPrefillParts = WS_CLEARED_BYTES;             // [items] int32
+constexpr size_t kPrefillPartials = WS_CLEARED_BYTES + 1024;   // 256-byte aligned
+static_assert(kPrefillPartials % 256 == 0 && PF_UNITS / 2 * 4 <= 1024, "workspace layout");
 
 }  // namespace
 
@@ -46,7 +62,9 @@ pdattn_status pdattn_prefill_workspace_size(int num_seqs, int num_tokens, int nu
   if (!device_bytes || num_tokens < 0) return PDATTN_INVALID_ARG;
   const pdattn_status s = check_shape(num_seqs, num_q_heads, num_kv_heads, head_dim, block_size);
   if (s != PDATTN_OK) return s;
-  *device_bytes = align_up(WS_CLEARED_BYTES, 256);
+  const int64_t items = prefill_items(num_seqs, num_tokens, num_q_heads, num_kv_heads);
+  const int splits = prefill_splits(items);
+  *device_bytes = splits > 1 ? kPrefillPartials + static_cast<size_t>(items) * splits * prefill_part_bytes(head_dim) : WS_CLEARED_BYTES;
   return PDATTN_OK;
 }
 
@@ -65,14 +83,18 @@ pdattn_status pdattn_prefill(const pdattn_args* a, const int32_t* cu_tokens, int
   auto mis = [](const void* p, size_t al) { return (reinterpret_cast<uintptr_t>(p) & (al - 1)) != 0; };
   if (mis(a->q, 16) || mis(a->k_cache, 16) || mis(a->v_cache, 16) || mis(a->out, 16) || mis(a->workspace, 256))
     return PDATTN_MISALIGNED;
-  size_t need = 0;
-  s = pdattn_prefill_workspace_size(a->num_seqs, num_tokens, a->num_q_heads, a->num_kv_heads, a->head_dim, a->block_size, &need);
-  if (s != PDATTN_OK) return s;
-  if (a->workspace_bytes < need) return PDATTN_WORKSPACE_TOO_SMALL;
+  if (a->workspace_bytes < WS_CLEARED_BYTES) return PDATTN_WORKSPACE_TOO_SMALL;
   const int G = a->num_q_heads / a->num_kv_heads;
   const int TQ = 128 / G;
-  const int64_t items = (static_cast<int64_t>(num_tokens) / (2 * TQ) + a->num_seqs) * a->num_kv_heads;
+  const int64_t items = prefill_items(a->num_seqs, num_tokens, a->num_q_heads, a->num_kv_heads);
   if (items > INT32_MAX / 2) return PDATTN_UNSUPPORTED;
+  // a workspace without room for the parts' results is taken too: the items then stay whole
+  int splits = prefill_splits(items);
+  if (splits > 1) {
+    const int64_t room = a->workspace_bytes > kPrefillPartials
+                             ? static_cast<int64_t>((a->workspace_bytes - kPrefillPartials) / prefill_part_bytes(a->head_dim)) / items : 0;
+    if (splits > room) splits = room > 1 ? static_cast<int>(room) : 1;
+  }
   int dev = 0;
   DevInfo* di = nullptr;
   s = device_info(&dev, &di);
@@ -109,6 +131,9 @@ pdattn_status pdattn_prefill(const pdattn_args* a, const int32_t* cu_tokens, int
   P.bs_log2 = a->block_size == 64 ? 6 : a->block_size == 32 ? 5 : 4;
   P.TQ = TQ;
   P.n_items = static_cast<int>(items);
+  P.splits = splits;
+  P.parts = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(a->workspace) + kPrefillParts);
+  P.partials = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + kPrefillPartials);
   P.scale_log2 = a->scale * kLog2e;
   const bool cap = score && score->logit_cap > 0.f;
   if (score) {

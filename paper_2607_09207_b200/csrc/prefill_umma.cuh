@@ -18,6 +18,9 @@
 // thread, in order, so the buffer that P_t occupies needs no further wait, and scores that have arrived say that the product
 // before them is done.
 //
+// Few rows over long contexts.  Items that would leave most SMs idle are cut along the keys into up to P.splits parts of at
+// least PF_MIN_TILES key tiles; each writes its (m, l, O) and prefill_join_kernel puts them together in order.
+//
 // Masks are intervals per row.  A key tile that every row of a tile sees whole takes no mask at all; the others ("edge" tiles)
 // are masked by select.  A masked weight is 0, and 0 * inf or 0 * NaN would still poison the row, so in edge tiles the guards set
 // the non-finite elements of V to 0 before the product and note the keys; a row that does see such a key adds those elements
@@ -56,6 +59,9 @@ struct PrefillParams {
   int N, S, Hq, Hkv, G, MB, NB, bs_log2;
   int TQ;                        // tokens of a tile: 128 / G
   int n_items;                   // pair slots x KV heads
+  int splits;                    // parts an item may be cut into
+  int32_t* parts;                // [n_items] parts it was cut into (splits > 1 only)
+  float* partials;               // [n_items * splits][2 tiles][O columns, m, l][128 rows]
   int window;
   float scale_log2;              // scale * log2(e)
   float cap2;                    // cap * log2(e)
@@ -63,6 +69,7 @@ struct PrefillParams {
 };
 
 constexpr int PF_KEYS = 128;     // keys of a tile
+constexpr int PF_MIN_TILES = 4;  // key tiles of a part, at least
 constexpr int PF_ITEMS = 3;      // items in flight between the warps
 constexpr int PF_GUARDS = 2;     // warps that guard V
 constexpr int PF_NTHREADS = 512;
@@ -85,6 +92,7 @@ struct PrefillCfg {
 struct PrefillItem {
   int s, g, tok0, n;             // sequence, KV head, first token of the pair within the sequence, new tokens of the sequence
   int L, row0;                   // context length; cu_tokens[s]
+  int part;                      // slot of its partial result, or -1: the item is whole
   int begin[2], end[2];          // key tiles [begin, end) of each tile; begin == end: none
   int plain, edges;              // key tiles [plain, edges) are seen whole by every row of both tiles
   int rows[2];                   // tokens of each tile
@@ -105,6 +113,26 @@ struct PrefillCtrl {
   uint32_t abort, tmem_base;
 };
 static_assert(sizeof(PrefillCtrl) <= 1024, "control block");
+
+// The tokens of a pair slot: sequence s (whose rows begin at row0, row1 - row0 of them), first token tok0.  false: none.  One
+// warp; 32 probes per round.
+__device__ __forceinline__ bool prefill_slot(const PrefillParams& P, int slot, int lane, int& s, int& row0, int& row1, int& tok0) {
+  const int TP = 2 * P.TQ;
+  int lo = 0, len = P.S;                                // the last sequence whose first slot is at or before this one
+  while (len > 1) {
+    const int step = (len + 31) / 32, i = lane * step;
+    const bool below = i < len && __ldg(P.cu_tokens + lo + i) / TP + lo + i <= slot;
+    const uint32_t m = __ballot_sync(0xffffffffu, below);
+    const int b = m ? 31 - __clz(m) : 0;
+    lo += b * step;
+    len = min(step, len - b * step);
+  }
+  s = lo;
+  row0 = __ldg(P.cu_tokens + lo);
+  row1 = __ldg(P.cu_tokens + lo + 1);
+  tok0 = (slot - (row0 / TP + lo)) * TP;
+  return row0 >= 0 && row1 <= P.N && tok0 >= 0 && tok0 < row1 - row0;
+}
 
 // first and one-past-last key that token j of a sequence sees
 __device__ __forceinline__ int2 prefill_interval(const PrefillParams& P, int L, int n, int row0, int prefix, int j) {
@@ -297,44 +325,34 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
     if (warp == 12) {
       // ================= items: found one or two ahead of their use
       int next = blockIdx.x;
+      const int n_units = P.n_items * P.splits;
       for (int k = 0;; ++k) {
         PrefillItem it;
         it.s = -1;
-        while (next < P.n_items) {
+        while (next < n_units) {
           const int slots = P.n_items / P.Hkv;
-          const int slot = slots - 1 - next / P.Hkv;      // the late pairs of a sequence, which see most keys, first
-          it.g = next % P.Hkv;
+          const int unit = next, item = unit / P.splits, split = unit - item * P.splits;
+          const int slot = slots - 1 - item / P.Hkv;      // the late pairs of a sequence, which see most keys, first
+          it.g = item % P.Hkv;
           int drawn = 0;
           if (lane == 0) drawn = atomicAdd(&P.hdr->counter, 1);
           next = static_cast<int>(gridDim.x) + __shfl_sync(0xffffffffu, drawn, 0);
-          // the last sequence whose first slot is at or before this one
-          const int TP = 2 * P.TQ;
-          int lo = 0, len = P.S;
-          while (len > 1) {
-            const int step = (len + 31) / 32, i = lane * step;
-            const bool below = i < len && __ldg(P.cu_tokens + lo + i) / TP + lo + i <= slot;
-            const uint32_t m = __ballot_sync(0xffffffffu, below);
-            const int b = m ? 31 - __clz(m) : 0;
-            lo += b * step;
-            len = min(step, len - b * step);
+          int s, row1;
+          if (!prefill_slot(P, slot, lane, s, it.row0, row1, it.tok0)) {
+            if (P.splits > 1 && split == 0 && lane == 0) P.parts[item] = 0;
+            continue;
           }
-          const int row0 = __ldg(P.cu_tokens + lo), row1 = __ldg(P.cu_tokens + lo + 1);
-          const int tok0 = (slot - (row0 / TP + lo)) * TP;
-          if (row0 < 0 || row1 > P.N || tok0 < 0 || tok0 >= row1 - row0) continue;   // a slot without tokens
-          it.s = lo;
-          it.tok0 = tok0;
-          it.row0 = row0;
-          it.n = row1 - row0;
-          it.L = max(0, __ldg(P.context_lens + lo));
+          it.n = row1 - it.row0;
+          it.L = max(0, __ldg(P.context_lens + s));
           it.plain = 0;
           it.edges = INT_MAX;
-          const int prefix = P.prefix_lens ? __ldg(P.prefix_lens + lo) : 0;
+          const int prefix = P.prefix_lens ? __ldg(P.prefix_lens + s) : 0;
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            it.rows[t] = min(P.TQ, max(0, it.n - tok0 - t * P.TQ));
+            it.rows[t] = min(P.TQ, max(0, it.n - it.tok0 - t * P.TQ));
             int lo_min = INT_MAX, lo_max = 0, hi_min = INT_MAX, hi_max = 0;
             for (int j = lane; j < it.rows[t]; j += 32) {
-              const int2 v = prefill_interval(P, it.L, it.n, row0, prefix, tok0 + t * P.TQ + j);
+              const int2 v = prefill_interval(P, it.L, it.n, it.row0, prefix, it.tok0 + t * P.TQ + j);
               if (v.y > 0) lo_min = min(lo_min, v.x);
               lo_max = max(lo_max, v.x);
               hi_max = max(hi_max, v.y);
@@ -351,6 +369,24 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
               it.edges = min(it.edges, hi_min / PF_KEYS);
             }
           }
+          it.part = -1;
+          if (P.splits > 1) {
+            // this unit's share of the item's key tiles
+            const int k0 = tiles_from(it), n = max(0, tiles_to(it) - k0);
+            const int parts = max(1, min(P.splits, n / PF_MIN_TILES));
+            if (split == 0 && lane == 0) P.parts[item] = parts;
+            if (split >= parts) continue;
+            if (parts > 1) it.part = unit;
+            const int a = k0 + static_cast<int>(static_cast<int64_t>(n) * split / parts);
+            const int b = k0 + static_cast<int>(static_cast<int64_t>(n) * (split + 1) / parts);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              it.begin[t] = max(it.begin[t], a);
+              it.end[t] = min(it.end[t], b);
+              if (it.begin[t] >= it.end[t]) it.begin[t] = it.end[t] = 0;
+            }
+          }
+          it.s = s;
           break;
         }
         const int e = k % PF_ITEMS;
@@ -775,7 +811,13 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           ++no;
           tc_fence_after();
         }
-        const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+        // a part of an item leaves its sums as they are
+        float* part = it.part >= 0 ? P.partials + (static_cast<int64_t>(it.part) * 2 + t) * ((D + 2) * 128) + r : nullptr;
+        const float inv = part ? 1.f : l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+        if (part) {
+          part[D * 128] = m;
+          part[(D + 1) * 128] = l;
+        }
         // A thread holds a row; written like that, every store of a warp would touch 32 lines.  Groups of four lanes transpose
         // 4 x 4 chunks of 16 bytes among themselves, so that a store writes 64 bytes of each of eight rows.
         __nv_bfloat16* out0 = P.out + (static_cast<int64_t>(it.row0 + it.tok0 + t * P.TQ) * P.Hq + it.g * P.G) * D;
@@ -791,6 +833,11 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = any && inv != 0.f ? __uint_as_float(o[i]) * inv : 0.f;
           if (poison_to >= 0) add_guarded<D>(P, it.s, it.g, max(lo, poison_from * PF_KEYS), min(hi, (poison_to + 1) * PF_KEYS), q, v);
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) part[(q * 32 + i) * 128] = v[i];
+            continue;
+          }
           uint4 w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -825,6 +872,48 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   tc_fence_before();
   __syncthreads();
   if (warp == 8) tmem_dealloc(tbase, C::TMEM_COLS);
+}
+
+// The parts of the items that were cut along the keys, put together in order: block (item, tile, 8 columns), a thread per row.
+//   M = max m_j;  out = sum O_j 2^(m_j - M) / sum l_j 2^(m_j - M)
+// Bound by the latency of its loads (neighbouring rows are neighbours in memory): four parts are fetched at a time.
+template <int D>
+__global__ void __launch_bounds__(128)
+prefill_join_kernel(const __grid_constant__ PrefillParams P) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int item = blockIdx.x, t = blockIdx.y, q = blockIdx.z, r = threadIdx.x;
+  const int parts = P.parts[item];
+  if (parts <= 1) return;
+  int s, row0, row1, tok0;
+  prefill_slot(P, P.n_items / P.Hkv - 1 - item / P.Hkv, r & 31, s, row0, row1, tok0);
+  const int g = item % P.Hkv, rj = r / P.G, rh = r - rj * P.G, j = tok0 + t * P.TQ + rj;
+  if (rj >= P.TQ || j >= row1 - row0) return;
+  const float* first = P.partials + (static_cast<int64_t>(item) * P.splits * 2 + t) * ((D + 2) * 128) + r;
+  constexpr int64_t STEP = 2 * (D + 2) * 128;
+  const float NEG_INF = __int_as_float(0xff800000);
+  float M = NEG_INF, L = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) M = fmaxf(M, first[p * STEP + D * 128]);
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const float* part = first + p * STEP;
+    const float m = part[D * 128], l = part[(D + 1) * 128];
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = part[(q * 8 + i) * 128];
+    const float f = m == NEG_INF ? 0.f : fast_exp2(m - M);        // 0: saw nothing
+    L += l * f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      // infinities and NaN of V stand whatever the weight
+      const bool odd = (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u;
+      o[i] += odd ? x[i] : x[i] * f;
+    }
+  }
+  const float inv = L > 0.f ? 1.f / L : (L != L ? L : 0.f);
+  *reinterpret_cast<uint4*>(P.out + (static_cast<int64_t>(row0 + j) * P.Hq + g * P.G + rh) * D + q * 8) =
+      make_uint4(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
+                 pack_bf16x2(o[6] * inv, o[7] * inv));
 }
 
 }  // namespace pdattn

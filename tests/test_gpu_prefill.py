@@ -319,3 +319,42 @@ def test_wrapper_refuses_what_the_library_cannot_see():
         pdattn.prefill(**good, score=pdattn.Score(key_begin=torch.zeros(5, dtype=torch.int32, device="cuda")))
     with pytest.raises(pdattn.PdattnError):
         pdattn.prefill(**good, score=pdattn.Score(logit_cap=-1.0))
+
+
+@pytest.mark.parametrize("n,L,Hq,Hkv,d", [([1], [20000], 4, 1, 128), ([40], [30000], 28, 4, 128), ([5, 0, 17], [9000, 77, 600], 8, 2, 64),
+                                         ([100, 3], [100, 15000], 16, 1, 128), ([300], [4000], 2, 2, 64)])
+@pytest.mark.parametrize("what", ["causal", "window", "documents", "capped"])
+def test_few_tokens_over_long_contexts(n, L, Hq, Hkv, d, what):
+    """Cut along the keys: parts of very different worth, some without a visible key."""
+    c = make(n, L, Hq, Hkv, d, 16, seed=Hq + d, sharp=2.0)
+    score, ref = {}, {}
+    if what == "window":
+        score["window"] = ref["window"] = 3000
+    if what == "documents":
+        r = np.random.default_rng(1)
+        pos = np.concatenate([np.arange(b - a, b) for a, b in zip(n, L)])
+        ref["begin"] = np.maximum(0, pos - r.integers(0, 12000, len(pos))).astype(np.int32)
+        ref["begin"][-1] = 30000                             # the last token sees nothing
+        score["key_begin"] = torch.from_numpy(ref["begin"]).cuda()
+    if what == "capped":
+        score["logit_cap"] = ref["cap"] = 8.0
+        score["bias_slopes"] = ref["slopes"] = torch.full((Hq,), 0.001, device="cuda")
+    want, size = reference(c, **ref)
+    out = run(c, **score)
+    close(out, want, size)
+    assert torch.equal(run(c, **score), out)
+    # without room for the parts' results the items stay whole
+    small = torch.zeros(8448, dtype=torch.uint8, device="cuda")
+    close(run(c, ws=small, **score), want, size)
+    some = torch.zeros(8448 + 1024 + 10 * 2 * (d + 2) * 512 + 77, dtype=torch.uint8, device="cuda")
+    close(run(c, ws=some, **score), want, size)
+
+
+def test_cut_items_with_values_that_are_not_finite():
+    c = make([20], [12000], 4, 1, 128, 16)
+    v, tab = c["vc"], c["tab"]
+    for t, j, x in ((50, 3, math.inf), (6000, 3, -math.inf), (7000, 9, math.inf), (11990, 77, math.nan), (11999, 100, -math.inf)):
+        v[tab[0, t // 16], 0, t % 16, j] = x
+    close(run(c), *reference(c))
+    begin = np.linspace(0, 11000, 20).astype(np.int32)
+    close(run(c, key_begin=torch.from_numpy(begin).cuda()), *reference(c, begin=begin))
