@@ -261,7 +261,8 @@ typedef struct {
   int num_seqs, num_q_heads;        /* num_q_heads 0: only k and v (q, q_out may be NULL)             */
   int num_kv_heads, head_dim, block_size, max_blocks_per_seq, num_blocks;
   int64_t kv_block_stride, kv_head_stride, kv_token_stride;
-  void* workspace;                  /* DEVICE, may be NULL: its sticky error word (see pdattn_check)  */
+  void* workspace;                  /* DEVICE, may be NULL: its sticky error word.  pdattn_check clears 8448 bytes, so one
+                                       that is checked has them and was given to pdattn_workspace_init */
 } pdattn_rope_args;
 pdattn_status pdattn_rope_append(const pdattn_rope_args* args, pdattn_stream_t stream);
 /* The same into the fp8 cache of pdattn_decode_fp8 (its layouts; the stride fields of the caches are ignored): rotated
@@ -281,14 +282,15 @@ pdattn_status pdattn_rope_append_fp8(const pdattn_rope_args* args, const float* 
  * All members zero / NULL: plain causal attention.
  */
 typedef struct {
-  float logit_cap;                  /* 0: none                                                        */
+  float logit_cap;                  /* 0: none; else 1e-6 .. 1e6                                      */
   const float* bias_slopes;         /* DEVICE fp32 [num_q_heads], or NULL                             */
   int window;                       /* 0: none                                                        */
   const int32_t* key_begin;         /* DEVICE int32, one per query token, or NULL                     */
   const int32_t* prefix_lens;       /* DEVICE int32 [num_seqs], or NULL.  pdattn_decode_scored ignores it: a single
                                        token sees all keys up to itself in any case                   */
-  const int32_t* key_begin_host;    /* HOST copy of key_begin.  pdattn_decode_scored: required with key_begin when
-                                       context_lens_host is given; else ignored                       */
+  const int32_t* key_begin_host;    /* HOST copy of key_begin (read during the call only; must equal the device array).
+                                       pdattn_decode_scored: required with key_begin when context_lens_host is
+                                       given; else ignored                                            */
 } pdattn_score_args;
 
 /*
@@ -298,11 +300,13 @@ typedef struct {
  * new tokens; cu_tokens DEVICE int32 [num_seqs + 1].  Each token attends by the rules of pdattn_score_args (score NULL:
  * plain causal).  Takes no host copies: the launch does not depend on the lengths (args->context_lens_host is not read).
  * The softmax weights are rounded to bf16 for the second product; fp32 otherwise.
- *   - Bad page ids, slots past the end and pages that no row references: as in pdattn_decode_ex.
+ *   - Bad page ids, slots past the end, pages that no row references and contexts longer than their table row (without a
+ *     host copy of the lengths): as in pdattn_decode_ex.
  *   - Rows of out at or past cu_tokens[num_seqs] are left as they were.  A token before position 0 gets zeros.
  *   - args->workspace holds pdattn_prefill_workspace_size() bytes.  Calls of few tokens are cut along the keys so that long
  *     contexts keep every SM busy; that takes room for the parts' results.  A smaller workspace (8448 bytes at least) is taken
- *     too: such calls are then cut into fewer parts, or not at all (another order of summation: other rounding).
+ *     too: such calls are then cut into fewer parts, or not at all (another order of summation: other rounding).  As for
+ *     the decode calls, pdattn_workspace_init comes before its first use, and calls that share it must not overlap.
  */
 pdattn_status pdattn_prefill_workspace_size(int num_seqs, int num_tokens, int num_q_heads, int num_kv_heads, int head_dim,
                                             int block_size, size_t* device_bytes);
@@ -338,9 +342,9 @@ pdattn_status pdattn_pages_workspace_size(int num_blocks, int num_seqs, size_t* 
 pdattn_status pdattn_pages_init(const pdattn_page_pool* pool, pdattn_stream_t stream);
 /*
  * Pages for new_tokens[s] >= 0 (DEVICE int32 [num_seqs]) further tokens of every sequence, lowest ids first, in sequence
- * order; context_lens[s] += new_tokens[s].  A sequence whose row cannot hold them (or with a negative number) is left as
- * it is: PDATTN_BAD_SEQUENCE from pdattn_check.  Too few free pages for all the others: nothing changes,
- * PDATTN_OUT_OF_PAGES.
+ * order; context_lens[s] += new_tokens[s].  A partial last page must be the sequence's own (pdattn_pages_fork sees to that).
+ * A sequence whose row cannot hold them (or with a negative number) is left as it is: PDATTN_BAD_SEQUENCE from
+ * pdattn_check.  Too few free pages for all the others: nothing changes, PDATTN_OUT_OF_PAGES.
  */
 pdattn_status pdattn_pages_reserve(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
                                    const int32_t* new_tokens, int num_seqs, int max_blocks_per_seq, int block_size,
@@ -377,7 +381,7 @@ pdattn_status pdattn_pages_compact(const pdattn_page_pool* pool, int32_t* block_
  * Copies page copy_src[i] to page copy_dst[i] of both caches, i < num_copies; a pair with a negative entry is skipped.  No page
  * that is written may be another pair's (the pairs of fork and compact never are).  element_bytes 2: bf16 caches with the
  * strides of pdattn_args; 1: the dense code pools of pdattn_decode_fp8 (strides ignored).  A page outside [0, num_blocks) is
- * not copied and sets the error word of `workspace` (may be NULL).
+ * not copied and sets the error word of `workspace` (may be NULL; as in pdattn_rope_args).
  */
 pdattn_status pdattn_pages_copy(void* k_cache, void* v_cache, const int32_t* copy_src, const int32_t* copy_dst,
                                 int num_copies, int num_kv_heads, int head_dim, int block_size, int num_blocks,

@@ -79,7 +79,7 @@ struct DecodeParams {
   const float* slopes;        // per query head, or null
   int window;                 // 0: none
   float cap2;                 // cap * log2(e); 0: none
-  float cap_r;                // 2 / cap
+  float cap_r;                // 1 / (cap * log2(e)): base-2 scores to multiples of the cap
   int inkernel_max;         // > 0: a cut unit whose followers all lie within this many spans after its first one is
                             // merged by the CTA that writes its last partial; 0: every cut unit is left to combine_kernel
   SpanStart spans[MAX_PARAM_SPANS + 1];
@@ -366,22 +366,28 @@ struct WalkerT {
 };
 using Walker = WalkerT<false>;
 
+// tanh to 2^-22: up to 3/4 the odd polynomial of degree 9 with the smallest largest error there (1.9e-7, found by Remez
+// exchange; leading coefficient first), past it 1 - 2 / (1 + exp(2 t)), which cancels for small t.
+__device__ constexpr float kTanh[5] = {0.0123188357f, -0.0492804514f, 0.132260918f, -0.333230765f, 0.999997228f};
+__device__ __forceinline__ float tanh_any(float t) {
+  const float u = t * t;
+  const float small = t * fmaf(fmaf(fmaf(fmaf(kTanh[0], u, kTanh[1]), u, kTanh[2]), u, kTanh[3]), u, kTanh[4]);
+  float rc;
+  const float e = fast_exp2(t * 2.8853900817779268f) + 1.f;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(e));
+  return fabsf(t) <= 0.75f ? small : fmaf(-2.f, rc, 1.f);
+}
+
 // Modified scores of one tile on one warp (compute_tile and compute_tile_f8 with MOD).
 template <int NT>
 struct TileMod {
-  float cap2, cap_k;        // cap tanh(s / cap) in base-2 units: cap2 - 2 cap2 / (1 + 2^(s cap_k)); cap2 == 0: none
+  float cap2, cap_x;        // cap tanh(x / cap) in base-2 units: cap2 tanh(s cap_x); cap2 == 0: none
   float slope2[NT][2];      // per score column of this lane: -slope * log2(e)
   int head;                 // tokens of the tile before the first one seen (<= 0: none)
   // score of a token `dist` positions before the current one
   __device__ __forceinline__ float score(float s, float sl2, int nt, int e, int dist) const {
     float v = s * sl2;
-    if (cap2 != 0.f) {
-      // exact to 2^-21 of the cap, at both ends of the range too
-      float rc;
-      const float ex = fast_exp2(s * cap_k) + 1.f;
-      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(ex));
-      v = fmaf(-2.f * cap2, rc, cap2);
-    }
+    if (cap2 != 0.f) v = cap2 * tanh_any(s * cap_x);
     return fmaf(slope2[nt][e], static_cast<float>(dist), v);
   }
 };

@@ -371,7 +371,7 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
       TileMod<NT> md;
       if constexpr (MOD) {
         md.cap2 = P.cap2;
-        md.cap_k = sl2 * P.cap_r;
+        md.cap_x = sl2 * P.cap_r;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

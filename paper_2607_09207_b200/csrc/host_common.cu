@@ -109,7 +109,7 @@ pdattn_status make_map(const void* ptr, int d, int bs, int hkv, int nb, int64_t 
                        CUtensorMap* out) {
   MapKey key{ptr, d, bs, hkv, nb, rank, sb, sh, st};
   for (auto& e : g_maps)
-    if (e.valid && e.key == key) {
+    if (rank != kMapQ && e.valid && e.key == key) {
       *out = e.map;
       return PDATTN_OK;
     }
@@ -177,12 +177,13 @@ pdattn_status make_map(const void* ptr, int d, int bs, int hkv, int nb, int64_t 
              static_cast<int>(r));
     return PDATTN_CUDA_ERROR;
   }
+  *out = m;
+  if (rank == kMapQ) return PDATTN_OK;
   MapCacheEntry& e = g_maps[g_map_next];
   g_map_next = (g_map_next + 1) % 16;
   e.valid = true;
   e.key = key;
   e.map = m;
-  *out = m;
   return PDATTN_OK;
 }
 

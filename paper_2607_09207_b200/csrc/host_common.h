@@ -24,6 +24,9 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // The head shapes and page sizes every attention entry point takes.
 PDATTN_HIDDEN pdattn_status check_shape(int num_seqs, int Hq, int Hkv, int d, int bs);
 
+// A cap of pdattn_score_args: none (0), or one whose reciprocal and whose multiples fp32 holds.
+inline bool valid_cap(float cap) { return cap == 0.f || (cap >= 1e-6f && cap <= 1e6f); }
+
 // ---- per-device facts ------------------------------------------------------------------------
 struct DevInfo {
   bool ready = false;
@@ -43,7 +46,8 @@ PDATTN_HIDDEN pdattn_status device_info(int* dev_out, DevInfo** info);
 // ---- TMA tensor maps ---------------------------------------------------------------------------
 constexpr int kMapK8 = 81, kMapV8 = 82;   // "ranks" of the two fp8 views in make_map
 constexpr int kMapQ = 83;                 // ... and of the packed query rows of pdattn_prefill
-// View of a cache as a tensor for TMA (see host_common.cu); cached per thread, pointer and shape.
+// View of a cache as a tensor for TMA (see host_common.cu).  The caches' views are kept per thread, pointer and shape; that of
+// the query rows, which are new memory in every call, is not.
 PDATTN_HIDDEN pdattn_status make_map(const void* ptr, int d, int bs, int hkv, int nb, int64_t sb, int64_t sh, int64_t st,
                                      int rank, CUtensorMap* out);
 

@@ -4,7 +4,6 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
-#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -732,7 +731,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
   if (cd.static_scratch && (grouped || fp8 || T != 1 || cd.probe)) return PDATTN_UNSUPPORTED;
   const pdattn_score_args* score = cd.score;
   if (score) {
-    if (!(score->logit_cap >= 0.f) || std::isinf(score->logit_cap) || score->window < 0) return PDATTN_INVALID_ARG;
+    if (!valid_cap(score->logit_cap) || score->window < 0) return PDATTN_INVALID_ARG;
     if (a->context_lens_host && score->key_begin && !score->key_begin_host) return PDATTN_INVALID_ARG;
   }
   // a context longer than its block_table row can describe is refused here when the host knows the lengths;
@@ -843,7 +842,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     P.window = score->window;
     if (score->logit_cap > 0.f) {
       P.cap2 = score->logit_cap * 1.4426950408889634f;
-      P.cap_r = 2.f / score->logit_cap;
+      P.cap_r = 1.f / P.cap2;
     }
   }
   P.tickets = reinterpret_cast<int32_t*>(ws + WS_TICKETS_OFFSET);

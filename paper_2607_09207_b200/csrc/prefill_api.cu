@@ -1,5 +1,4 @@
 // Host side of pdattn_prefill: argument checks, tensor maps, launch.
-#include <cmath>
 #include <cstdio>
 #include <type_traits>
 
@@ -79,7 +78,7 @@ pdattn_status pdattn_prefill(const pdattn_args* a, const int32_t* cu_tokens, int
   if (a->max_blocks_per_seq <= 0 || a->num_blocks <= 0) return PDATTN_INVALID_ARG;
   if (a->kv_block_stride <= 0 || a->kv_head_stride <= 0 || a->kv_token_stride < a->head_dim) return PDATTN_INVALID_ARG;
   if ((a->kv_block_stride | a->kv_head_stride | a->kv_token_stride) % 8 != 0) return PDATTN_UNSUPPORTED;
-  if (score && (!(score->logit_cap >= 0.f) || std::isinf(score->logit_cap) || score->window < 0)) return PDATTN_INVALID_ARG;
+  if (score && (!valid_cap(score->logit_cap) || score->window < 0)) return PDATTN_INVALID_ARG;
   auto mis = [](const void* p, size_t al) { return (reinterpret_cast<uintptr_t>(p) & (al - 1)) != 0; };
   if (mis(a->q, 16) || mis(a->k_cache, 16) || mis(a->v_cache, 16) || mis(a->out, 16) || mis(a->workspace, 256))
     return PDATTN_MISALIGNED;

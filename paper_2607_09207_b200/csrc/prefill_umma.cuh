@@ -92,6 +92,7 @@ struct PrefillCfg {
 struct PrefillItem {
   int s, g, tok0, n;             // sequence, KV head, first token of the pair within the sequence, new tokens of the sequence
   int L, row0;                   // context length; cu_tokens[s]
+  int keys;                      // tokens of the context that the table row can describe
   int part;                      // slot of its partial result, or -1: the item is whole
   int begin[2], end[2];          // key tiles [begin, end) of each tile; begin == end: none
   int plain, edges;              // key tiles [plain, edges) are seen whole by every row of both tiles
@@ -135,12 +136,12 @@ __device__ __forceinline__ bool prefill_slot(const PrefillParams& P, int slot, i
 }
 
 // first and one-past-last key that token j of a sequence sees
-__device__ __forceinline__ int2 prefill_interval(const PrefillParams& P, int L, int n, int row0, int prefix, int j) {
+__device__ __forceinline__ int2 prefill_interval(const PrefillParams& P, int L, int keys, int n, int row0, int prefix, int j) {
   const int pos = L - n + j;
   int lo = 0;
   if (P.window > 0) lo = max(lo, pos - P.window + 1);
   if (P.key_begin) lo = max(lo, __ldg(P.key_begin + row0 + j));
-  const int hi = pos < 0 ? 0 : min(L, max(pos + 1, prefix));
+  const int hi = pos < 0 ? 0 : min(keys, max(pos + 1, prefix));
   return lo < hi ? make_int2(lo, hi) : make_int2(0, 0);
 }
 
@@ -184,22 +185,16 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   return d;
 }
 
-// x <- tanh(x k), 32 values, to 2^-22.  Capped scores mostly lie well inside the cap: up to 3/4 of it an odd polynomial of degree
-// 9 (the one with the smallest largest error there, 1.9e-7, found by Remez exchange) does it on the FMA pipe; the exponential
-// unit, which the softmax needs, would be asked three times per score otherwise.  A warp that holds a larger one takes
-// 1 - 2 / (1 + exp(2 x k)) for all its 32.
+// x <- tanh(x k), 32 values, to 2^-22.  Capped scores mostly lie well inside the cap: up to 3/4 of it an odd polynomial (see
+// kTanh) does it on the FMA pipe; the exponential unit, which the softmax needs, would be asked three times per score
+// otherwise.  A warp that holds a larger one takes the way that serves both.
 __device__ __forceinline__ void tanh_columns(uint32_t (&x)[32], float k) {
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < 32; i += 2) top = max3(top, fabsf(__uint_as_float(x[i])), fabsf(__uint_as_float(x[i + 1])));
   if (__any_sync(0xffffffffu, top * fabsf(k) > 0.75f)) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      float rc;
-      const float e = fast_exp2(__uint_as_float(x[i]) * (k * 2.8853900817779268f)) + 1.f;
-      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(e));
-      x[i] = __float_as_uint(fmaf(-2.f, rc, 1.f));
-    }
+    for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(tanh_any(__uint_as_float(x[i]) * k));
     return;
   }
   const uint64_t kk = pack_f32x2(k, k);
@@ -207,10 +202,10 @@ __device__ __forceinline__ void tanh_columns(uint32_t (&x)[32], float k) {
   for (int i = 0; i < 32; i += 2) {
     const uint64_t t = mul_f32x2(pack_f32x2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), kk);
     const uint64_t u = mul_f32x2(t, t);
-    uint64_t p = fma_f32x2(pack_f32x2(0.0123188357f, 0.0123188357f), u, pack_f32x2(-0.0492804514f, -0.0492804514f));
-    p = fma_f32x2(p, u, pack_f32x2(0.132260918f, 0.132260918f));
-    p = fma_f32x2(p, u, pack_f32x2(-0.333230765f, -0.333230765f));
-    p = fma_f32x2(p, u, pack_f32x2(0.999997228f, 0.999997228f));
+    uint64_t p = fma_f32x2(pack_f32x2(kTanh[0], kTanh[0]), u, pack_f32x2(kTanh[1], kTanh[1]));
+    p = fma_f32x2(p, u, pack_f32x2(kTanh[2], kTanh[2]));
+    p = fma_f32x2(p, u, pack_f32x2(kTanh[3], kTanh[3]));
+    p = fma_f32x2(p, u, pack_f32x2(kTanh[4], kTanh[4]));
     float a, b;
     unpack_f32x2(mul_f32x2(p, t), a, b);
     x[i] = __float_as_uint(a);
@@ -329,7 +324,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       for (int k = 0;; ++k) {
         PrefillItem it;
         it.s = -1;
-        while (next < n_units) {
+        while (static_cast<unsigned>(next) < static_cast<unsigned>(n_units)) {
           const int slots = P.n_items / P.Hkv;
           const int unit = next, item = unit / P.splits, split = unit - item * P.splits;
           const int slot = slots - 1 - item / P.Hkv;      // the late pairs of a sequence, which see most keys, first
@@ -344,6 +339,9 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           }
           it.n = row1 - it.row0;
           it.L = max(0, __ldg(P.context_lens + s));
+          // tokens past the end of the table row are left out like those of a bad page
+          it.keys = static_cast<int>(min(static_cast<int64_t>(it.L), static_cast<int64_t>(P.MB) << P.bs_log2));
+          if (it.keys < it.L && lane == 0) atomicOr(&P.hdr->err, ERR_BAD_PAGE);
           it.plain = 0;
           it.edges = INT_MAX;
           const int prefix = P.prefix_lens ? __ldg(P.prefix_lens + s) : 0;
@@ -352,7 +350,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
             it.rows[t] = min(P.TQ, max(0, it.n - it.tok0 - t * P.TQ));
             int lo_min = INT_MAX, lo_max = 0, hi_min = INT_MAX, hi_max = 0;
             for (int j = lane; j < it.rows[t]; j += 32) {
-              const int2 v = prefill_interval(P, it.L, it.n, it.row0, prefix, it.tok0 + t * P.TQ + j);
+              const int2 v = prefill_interval(P, it.L, it.keys, it.n, it.row0, prefix, it.tok0 + t * P.TQ + j);
               if (v.y > 0) lo_min = min(lo_min, v.x);
               lo_max = max(lo_max, v.x);
               hi_max = max(hi_max, v.y);
@@ -421,10 +419,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       for (int k = 0; ok && get_item(k, ip); ++k) {
         const PrefillItem& it = *ip;
         const int32_t* row = P.block_table + static_cast<int64_t>(it.s) * P.MB;
-        const int npages = (it.L + (1 << P.bs_log2) - 1) >> P.bs_log2;
+        const int npages = static_cast<int>((static_cast<int64_t>(it.keys) + (1 << P.bs_log2) - 1) >> P.bs_log2);
         auto page_id = [&](int kt) {
           const int i = kt * ppt + j;
-          return i >= npages ? -2 : i < P.MB ? __ldg(row + i) : -1;     // -2: past the end, filled with zeros; -1: bad
+          return i < npages ? __ldg(row + i) : -2;             // -2: past the end, filled with zeros
         };
         const int k0 = tiles_from(it), k1 = tiles_to(it);
         int id_next = k0 < k1 ? page_id(k0) : 0;
@@ -662,7 +660,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       int lo = 0, hi = 0;
       const int pos = it.L - it.n + j;
       if (valid) {
-        const int2 v = prefill_interval(P, it.L, it.n, it.row0, P.prefix_lens ? __ldg(P.prefix_lens + it.s) : 0, j);
+        const int2 v = prefill_interval(P, it.L, it.keys, it.n, it.row0, P.prefix_lens ? __ldg(P.prefix_lens + it.s) : 0, j);
         lo = v.x;
         hi = v.y;
       }

@@ -358,3 +358,60 @@ def test_cut_items_with_values_that_are_not_finite():
     close(run(c), *reference(c))
     begin = np.linspace(0, 11000, 20).astype(np.int32)
     close(run(c, key_begin=torch.from_numpy(begin).cuda()), *reference(c, begin=begin))
+
+
+@pytest.mark.parametrize("cap", [1e-6, 0.5, 300.0, 1e4, 1e6])
+def test_caps_far_from_the_scores(cap):
+    """A cap far above the scores leaves them as they are to fp32 (tanh good to 2^-18 of small values: 2^-14 for scores
+    up to 16), one far below makes them all alike."""
+    c = make([90, 3], [200, 900], 4, 2, 128, 16, sharp=2.0)
+    close(run(c, logit_cap=cap), *reference(c, cap=cap))
+
+
+def test_lengths_that_no_table_row_can_hold():
+    """The largest length there is: the work is bounded by the row, whose tokens all count."""
+    c = make([40, 5], [128, 160], 4, 2, 128, 16)
+    c["tab"] = c["tab"][:, :8].copy()
+    want, size = reference(dict(c, n=np.array([40, 5]), L=np.array([128, 128])), prefix=[128, 128])
+    lens = torch.tensor([2 ** 31 - 1, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    ws = pdattn.alloc_prefill_workspace(2, 45, 4, 2, 128)
+    out = torch.empty_like(c["q"])
+    pdattn.prefill(c["q"], c["kc"], c["vc"], c["table"][:, :8].contiguous(), lens, c["cu"], c["scale"], out, ws)
+    assert pdattn.check(ws) == pdattn.BAD_PAGE_INDEX
+    close(out, want, size)
+
+
+def test_cut_items_start_from_any_workspace_contents_and_keep_a_key_of_nan_to_those_who_see_it():
+    c = make([30], [9000], 4, 2, 128, 16)
+    ws = pdattn.alloc_prefill_workspace(1, 30, 4, 2, 128)
+    ws[8448:] = 255                                          # NaN in every part's result
+    begin = np.linspace(0, 8990, 30).astype(np.int32)
+    dev = torch.from_numpy(begin).cuda()
+    want, size = reference(c, begin=begin)
+    close(run(c, ws=ws, key_begin=dev), want, size)
+    c["kc"][c["tab"][0, 4000 // 16], 0, 4000 % 16] = math.nan
+    out = run(c, ws=ws, key_begin=dev)
+    sees = begin <= 4000
+    close(out[~torch.from_numpy(sees).cuda()], want[~sees], size[~sees])
+    close(out[:, 2:], want[:, 2:], size[:, 2:])
+    assert bool(out[torch.from_numpy(sees).cuda(), :2].isnan().all())
+
+
+def test_cut_calls_captured_and_replayed_on_one_workspace():
+    """Two graphs that share a workspace, replayed in turn, and a call with other tokens between them."""
+    c, e = make([12], [7000], 4, 1, 128, 16), make([50, 2], [900, 5000], 4, 1, 128, 16)
+    ws = max((pdattn.alloc_prefill_workspace(len(x["n"]), int(x["n"].sum()), 4, 1, 128) for x in (c, e)), key=len)
+    outs, graphs = [run(c, ws=ws), run(e, ws=ws)], []
+    keep = [o.clone() for o in outs]
+    for x, o in zip((c, e), outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            pdattn.prefill(x["q"], x["kc"], x["vc"], x["table"], x["lens"], x["cu"], x["scale"], o, ws)
+        graphs.append(graph)
+    for _ in range(3):
+        for o in outs:
+            o.fill_(7.0)
+        graphs[1].replay()
+        graphs[0].replay()
+        assert torch.equal(outs[0], keep[0]) and torch.equal(outs[1], keep[1])
+        assert torch.equal(run(e, ws=ws), keep[1])

@@ -189,3 +189,12 @@ def test_wrapper_refuses_what_the_library_cannot_see():
         pdattn.decode_scored(w.q[:1], *args[1:], pdattn.Score())
     with pytest.raises(TypeError):
         pdattn.Score(bias_slopes=torch.zeros(8, device="cuda", dtype=torch.double))
+
+
+@pytest.mark.parametrize("cap", [1e-6, 0.5, 300.0, 1e4, 1e6])
+def test_caps_far_from_the_scores(cap):
+    """A cap far above the scores leaves them as they are to fp32 (tanh good to 2^-18 of small values: 2^-14 for scores
+    up to 16), one far below makes them all alike."""
+    w = W.make_custom([300, 64, 700], 8, 2, 128, 16, device="cuda:0")
+    w.q.mul_(2.0)
+    close(run(w, cap=cap), *reference(w, cap=cap), BF16_WEIGHTS)

@@ -166,3 +166,12 @@ def test_decode_scored_refusals(fp8):
     if fp8:
         a, s = ctypes.byref(step()), ctypes.byref(pdattn.ScoreArgs())
         assert L.pdattn_decode_scored_fp8(a, s, None, P, None) == L.pdattn_decode_scored_fp8(a, s, P, None, None) == pdattn.INVALID_ARG
+
+
+@pytest.mark.parametrize("cap", [1e-7, 1.5e6, 1e-44])
+def test_caps_out_of_range(cap):
+    L = pdattn.lib()
+    score = ctypes.byref(pdattn.ScoreArgs(cap, None, 0, None, None, None))
+    assert L.pdattn_prefill(ctypes.byref(step()), P, 9, score, None) == pdattn.INVALID_ARG
+    assert L.pdattn_decode_scored(ctypes.byref(step()), score, None) == pdattn.INVALID_ARG
+    assert L.pdattn_decode_scored_fp8(ctypes.byref(step()), score, P, P, None) == pdattn.INVALID_ARG
