@@ -35,7 +35,9 @@
 // 2500 (128 exponentials a thread, two warps to a quadrant), weights to the next scores 1300 (barrier, half of P.V, Q.K^T,
 // barrier).  Tried and not faster: two threads a row (16 softmax warps), the scores in registers throughout (the code then
 // outgrows the instruction caches), a share of the exponentials on the FMA pipe, one MMA warp per tile (the tiles fall into step
-// and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 532 us, 0.90 PFLOP/s; a null softmax takes 430 us.
+// and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 474-510 us, 0.94-1.01 PFLOP/s (the spread is
+// the clock under the power cap); with a cap 690, with a distance bias 625.  Also tried for those two: the bias as packed
+// multiply-adds (no gain), worked out again in the second pass in place of the write-back (+13 %), tanh in unpacked operations (+10 %).
 //
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA thread drains, tensor memory
 // is freed and the CTA returns.
@@ -71,6 +73,7 @@ struct PrefillParams {
 constexpr int PF_KEYS = 128;     // keys of a tile
 constexpr int PF_MIN_TILES = 4;  // key tiles of a part, at least
 constexpr int PF_ITEMS = 3;      // items in flight between the warps
+constexpr int PF_AHEAD = 2;      // a CTA draws its next item when the loads of the present one come to its last two key tiles
 constexpr int PF_GUARDS = 2;     // warps that guard V
 constexpr int PF_NTHREADS = 512;
 constexpr int PF_LAUNCH_REGS = 128, PF_SOFTMAX_REGS = 184, PF_OTHER_REGS = 72;   // a thread
@@ -106,7 +109,7 @@ struct PrefillCtrl {
   uint64_t q_full[2], q_free[2], s_full[2];
   uint64_t p_part[2][2];                         // per tile: the weights of its first, of its second 64 keys are stored
   uint64_t o_full[2];                            // the item's last product into O is done
-  uint64_t item_full[PF_ITEMS], item_free[PF_ITEMS];
+  uint64_t item_full[PF_ITEMS], item_free[PF_ITEMS], item_ask;
   uint64_t drained;
   PrefillItem item[PF_ITEMS];
   uint32_t page_bad[8];                          // per key tile (mod 8): bit j set = its page j had a bad id
@@ -188,7 +191,7 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
 // x <- tanh(x k), 32 values, to 2^-22.  Capped scores mostly lie well inside the cap: up to 3/4 of it an odd polynomial (see
 // kTanh) does it on the FMA pipe; the exponential unit, which the softmax needs, would be asked three times per score
 // otherwise.  A warp that holds a larger one takes 1 - 2 / (1 + exp(2 x k)) for all its 32: what that loses in small values, 2^-22
-// of the cap, is at most 2^-21 of the largest score there (choosing value by value costs 645 us where this takes 416: prompts of
+// of the cap, is at most 2^-21 of the largest score there (choosing value by value costs 645 us where this took 416: prompts of
 // 28/4 heads of 128 with a cap of 50).
 __device__ __forceinline__ void tanh_columns(uint32_t (&x)[32], float k) {
   float top = 0.f;
@@ -264,6 +267,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
 
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&ctrl->drained), 1);
+    mbar_init(smem_u32(&ctrl->item_ask), 1);
     for (int i = 0; i < 8; ++i) {
       mbar_init(smem_u32(&ctrl->k_full[i]), 1);
       mbar_init(smem_u32(&ctrl->v_full[i]), 1);
@@ -325,20 +329,30 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PF_OTHER_REGS));
     if (warp == 12) {
-      // ================= items: found one or two ahead of their use
+      // ================= items.  Each is drawn no earlier than its loads can begin: what a CTA draws ahead, one that is
+      // idle cannot have (37 sequences of 36 tokens over 2048 keys, 28/4 heads, an item per SM: 82 us drawn three ahead, 51 so)
       int next = blockIdx.x;
       const int n_units = P.n_items * P.splits;
       for (int k = 0;; ++k) {
         PrefillItem it;
         it.s = -1;
-        while (static_cast<unsigned>(next) < static_cast<unsigned>(n_units)) {
+        auto draw = [&]() {
+          int drawn = 0;
+          if (lane == 0) drawn = atomicAdd(&P.hdr->counter, 1);
+          next = static_cast<int>(gridDim.x) + __shfl_sync(0xffffffffu, drawn, 0);
+        };
+        if (k > 0) {
+          if (!__all_sync(0xffffffffu, prefill_wait(smem_u32(&ctrl->item_ask), (k - 1) & 1, abort_flag))) {
+            if (lane == 0) fail();
+            break;
+          }
+          draw();
+        }
+        for (; static_cast<unsigned>(next) < static_cast<unsigned>(n_units); draw()) {   // (slots without tokens are passed over)
           const int slots = P.n_items / P.Hkv;
           const int unit = next, item = unit / P.splits, split = unit - item * P.splits;
           const int slot = slots - 1 - item / P.Hkv;      // the late pairs of a sequence, which see most keys, first
           it.g = item % P.Hkv;
-          int drawn = 0;
-          if (lane == 0) drawn = atomicAdd(&P.hdr->counter, 1);
-          next = static_cast<int>(gridDim.x) + __shfl_sync(0xffffffffu, drawn, 0);
           int s, row1;
           if (!prefill_slot(P, slot, lane, s, it.row0, row1, it.tok0)) {
             if (P.splits > 1 && split == 0 && lane == 0) P.parts[item] = 0;
@@ -433,6 +447,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         };
         const int k0 = tiles_from(it), k1 = tiles_to(it);
         int id_next = k0 < k1 ? page_id(k0) : 0;
+        bool asked = isV;                                 // for the next item; the K loads ask
         if (!isV) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
@@ -452,6 +467,10 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         for (int kt = k0; kt < k1 && ok; ++kt) {
           int id = id_next;
           if (kt + 1 < k1) id_next = page_id(kt + 1);
+          if (!asked && kt >= k1 - PF_AHEAD) {
+            if (lane == 0) mbar_arrive(smem_u32(&ctrl->item_ask));
+            asked = true;
+          }
           if (!active(it, 0, kt) && !active(it, 1, kt)) continue;
           const bool bad = id != -2 && (id < 0 || id >= P.NB);
           const uint32_t badmask = __ballot_sync(0xffffffffu, bad && h == 0);
@@ -473,6 +492,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           if (++slot == ring) slot = 0;
           ++c;
         }
+        if (!asked && lane == 0) mbar_arrive(smem_u32(&ctrl->item_ask));
         done_item(k);
       }
       if (lane == 0) {
