@@ -415,3 +415,13 @@ def test_cut_calls_captured_and_replayed_on_one_workspace():
         graphs[0].replay()
         assert torch.equal(outs[0], keep[0]) and torch.equal(outs[1], keep[1])
         assert torch.equal(run(e, ws=ws), keep[1])
+
+
+def test_items_of_very_different_length():
+    """One long sequence among many of a token or none: what a CTA draws next is settled while others still work."""
+    n = [1] * 150 + [0] * 40 + [700] + [2] * 90 + [0] * 30
+    L = [1 + i % 300 for i in range(150)] + [0] * 40 + [20000] + [2 + 40 * i for i in range(90)] + [5] * 30
+    c = make(n, L, 14, 2, 128, 16, seed=4)
+    close(run(c), *reference(c))
+    begin = begins(c, 128)
+    close(run(c, key_begin=torch.from_numpy(begin).cuda()), *reference(c, begin=begin))

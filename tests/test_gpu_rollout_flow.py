@@ -152,3 +152,47 @@ def test_rollout(fp8, Hq, Hkv, d, bs):
     pdattn.pages_free(e.pool, e.table, e.lens, e.i32(alive), bs, e.pages_ws)
     assert pdattn.check(e.pages_ws) == pdattn.OK
     assert int(e.pool.free_count) == 200 and not e.pool.ref_counts.any()
+
+
+def test_calls_that_overlap_on_streams_of_their_own():
+    """Prompt attention of one batch beside the decode steps of another, each with a workspace of its own: the same bits as
+    one after the other."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    Hq, Hkv, d, bs = 8, 2, 128, 16
+
+    def batch(n, L):
+        pages = -(-L // bs)
+        NB = int(pages.sum())
+        table = np.full((len(n), int(pages.max())), -1, np.int32)
+        at = 0
+        for s, p in enumerate(pages):
+            table[s, :p] = np.arange(at, at + p)
+            at += p
+        kc, vc = (torch.randn(NB, Hkv, bs, d, device="cuda", generator=g).bfloat16() for _ in range(2))
+        q = torch.randn(int(n.sum()), Hq, d, device="cuda", generator=g).bfloat16()
+        i32 = lambda x: torch.from_numpy(np.asarray(x, np.int32)).cuda()  # noqa: E731
+        return q, kc, vc, i32(table), i32(L), i32(np.concatenate([[0], np.cumsum(n)]))
+    a = batch(np.array([900, 40, 300]), np.array([900, 3000, 1200]))
+    b = batch(np.ones(60, np.int64), np.arange(1, 61) * 50)
+    e = batch(np.array([30]), np.array([9000]))               # cut along the keys
+    wa, we = pdattn.alloc_prefill_workspace(3, 1240, Hq, Hkv, d, bs), pdattn.alloc_prefill_workspace(1, 30, Hq, Hkv, d, bs)
+    wb = pdattn.alloc_workspace(60, Hq, Hkv, d, bs)
+    score = pdattn.Score(logit_cap=20.0, window=700)
+
+    def calls(outs, streams):
+        for x, ws, out, st in ((a, wa, outs[0], streams[0]), (e, we, outs[2], streams[2])):
+            pdattn.prefill(*x[:6], 0.09, out, ws, score=score, stream=st)
+        q, kc, vc, table, lens, _ = b
+        pdattn.decode_scored(q, kc, vc, table, lens, 0.09, outs[1], wb, score, stream=streams[1])
+    want = [torch.empty_like(x[0]) for x in (a, b, e)]
+    calls(want, [None] * 3)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for _ in range(5):
+        got = [torch.full_like(x, 7.0) for x in want]
+        torch.cuda.synchronize()
+        for _ in range(4):
+            calls(got, streams)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert pdattn.check(wa) == pdattn.check(wb) == pdattn.check(we) == pdattn.OK
