@@ -458,6 +458,19 @@ def _expect_dense(where: str, dtype, *tensors):
             raise ValueError(f"{where}: a dense tensor is wanted, got strides {t.stride()} for shape {tuple(t.shape)}")
 
 
+def _expect_workspace(where: str, workspace):
+    """A dense tensor of bytes on the current device, one that can hold the error word at least."""
+    _expect_dense(where, torch.uint8, workspace)
+    if workspace.numel() < 4:
+        raise ValueError(f"{where}: a workspace of {workspace.numel()} bytes")
+
+
+def _expect_device(where: str, device: int):
+    here = torch._C._cuda_getDevice()
+    if device != here:
+        raise ValueError(f"{where}: tensors on cuda:{device}, the current device is cuda:{here}")
+
+
 def _expect_caches(where: str, k_cache, v_cache):
     """bf16 caches [page, kv_head, slot, dim] that can share one set of strides."""
     _expect(where, torch.bfloat16, k_cache, v_cache)
@@ -493,6 +506,8 @@ def _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, kv_strides, bloc
     _expect_dense(where, torch.bfloat16, q_out)
     _expect_dense(where, torch.int32, block_table, context_lens, cu_tokens)
     _expect_dense(where, torch.float32, inv_freq)
+    if workspace is not None:
+        _expect_workspace(where, workspace)
     S, MB = block_table.shape
     rotary = d if rotary_dim is None else int(rotary_dim)
     if (heads != Hkv or dim != d or context_lens.numel() != S or inv_freq.numel() * 2 != rotary
@@ -550,11 +565,14 @@ class Score:
         _expect_dense("Score", torch.int32, key_begin, prefix_lens)
         host = None if key_begin_host is None else np.ascontiguousarray(key_begin_host, dtype=np.int32)
         self.keep = (bias_slopes, key_begin, prefix_lens, host)
+        self.device = next((t.get_device() for t in self.keep[:3] if t is not None), None)
         self.args = ScoreArgs(float(logit_cap), _ptr(bias_slopes), int(window), _ptr(key_begin), _ptr(prefix_lens),
                               None if host is None else host.ctypes.data)
 
     def fits(self, where: str, num_q_heads: int, num_tokens: int, num_seqs: int):
         slopes, begin, prefix, host = self.keep
+        if self.device is not None:
+            _expect_device(where, self.device)
         if slopes is not None and slopes.numel() != num_q_heads:
             raise ValueError(f"{where}: bias_slopes has {slopes.numel()} entries for {num_q_heads} query heads")
         if begin is not None and begin.numel() != num_tokens:
@@ -570,6 +588,7 @@ def _step_args(where, q, k_cache, v_cache, kv_strides, block_table, context_lens
     """The argument block of a call over bf16 or code caches whose q and out are [rows, Hq, d]."""
     _expect_dense(where, torch.bfloat16, q, out)
     _expect_dense(where, torch.int32, block_table, context_lens)
+    _expect_workspace(where, workspace)
     shape = q.shape
     _, Hq, d = shape
     NB, Hkv, bs, dim = k_cache.shape
@@ -665,6 +684,7 @@ class PagePool:
             raise ValueError("PagePool: ref_counts and free_list have one entry per page, free_count has one")
         self.ref_counts, self.free_list, self.free_count = ref_counts, free_list, free_count
         self.num_blocks = ref_counts.numel()
+        self.device = ref_counts.get_device()
         self.args = PoolArgs(ref_counts.data_ptr(), free_list.data_ptr(), free_count.data_ptr(), self.num_blocks)
 
     @classmethod
@@ -694,8 +714,10 @@ def alloc_pages_workspace(num_blocks: int, num_seqs: int, device="cuda", stream=
     return ws
 
 
-def _pages_check(where, block_table, context_lens, *lists):
+def _pages_check(where, pool, workspace, block_table, context_lens, *lists):
     _expect_dense(where, torch.int32, block_table, context_lens, *lists)
+    _expect_workspace(where, workspace)
+    _expect_device(where, pool.device)
     if block_table.dim() != 2 or context_lens.numel() != block_table.shape[0]:
         raise ValueError(f"{where}: block_table [S, MB] and context_lens [S] do not belong together")
 
@@ -704,7 +726,7 @@ def pages_reserve(pool: PagePool, block_table, context_lens, new_tokens, block_s
                   check: bool = True) -> int:
     """pdattn_pages_reserve: pages for new_tokens[s] further tokens of every sequence; context_lens advances (in place)."""
     where = "pdattn_pages_reserve"
-    _pages_check(where, block_table, context_lens, new_tokens)
+    _pages_check(where, pool, workspace, block_table, context_lens, new_tokens)
     S, MB = block_table.shape
     if new_tokens.numel() != S:
         raise ValueError(f"{where}: new_tokens has one entry per row")
@@ -721,7 +743,7 @@ def pages_fork(pool: PagePool, block_table, context_lens, parents, children, cop
     """pdattn_pages_fork: the empty rows children[i] become copies of the rows parents[i]; the partial pages to copy are
     written to (copy_src, copy_dst)."""
     where = "pdattn_pages_fork"
-    _pages_check(where, block_table, context_lens, parents, children, copy_src, copy_dst)
+    _pages_check(where, pool, workspace, block_table, context_lens, parents, children, copy_src, copy_dst)
     n = parents.numel()
     if children.numel() != n or copy_src.numel() < n or copy_dst.numel() < n:
         raise ValueError(f"{where}: {n} parents, {children.numel()} children, room for {copy_src.numel()} and {copy_dst.numel()} copies")
@@ -738,7 +760,7 @@ def pages_free(pool: PagePool, block_table, context_lens, seqs, block_size: int,
                check: bool = True) -> int:
     """pdattn_pages_free: rows seqs give their pages back and become empty."""
     where = "pdattn_pages_free"
-    _pages_check(where, block_table, context_lens, seqs)
+    _pages_check(where, pool, workspace, block_table, context_lens, seqs)
     S, MB = block_table.shape
     st = lib().pdattn_pages_free(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(), seqs.data_ptr(),
                                  seqs.numel(), S, MB, block_size, workspace.data_ptr(), workspace.numel(),
@@ -752,7 +774,7 @@ def pages_compact(pool: PagePool, block_table, context_lens, copy_src, copy_dst,
                   check: bool = True) -> int:
     """pdattn_pages_compact: renumber the referenced pages densely; the moves are written to (copy_src, copy_dst)."""
     where = "pdattn_pages_compact"
-    _pages_check(where, block_table, context_lens, copy_src, copy_dst)
+    _pages_check(where, pool, workspace, block_table, context_lens, copy_src, copy_dst)
     if copy_src.numel() != copy_dst.numel():
         raise ValueError(f"{where}: copy_src and copy_dst have the same length")
     S, MB = block_table.shape
@@ -769,6 +791,8 @@ def pages_copy(k_cache, v_cache, copy_src, copy_dst, workspace=None, stream=None
     uint8 code pools of decode_fp8)."""
     where = "pdattn_pages_copy"
     _expect_dense(where, torch.int32, copy_src, copy_dst)
+    if workspace is not None:
+        _expect_workspace(where, workspace)
     if copy_src.numel() != copy_dst.numel():
         raise ValueError(f"{where}: copy_src and copy_dst have the same length")
     NB, Hkv, bs, d = k_cache.shape

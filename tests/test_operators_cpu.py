@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2607_09207_b200 import build as pd_build
 from paper_2607_09207_b200 import pdattn
@@ -175,3 +176,77 @@ def test_caps_out_of_range(cap):
     assert L.pdattn_prefill(ctypes.byref(step()), P, 9, score, None) == pdattn.INVALID_ARG
     assert L.pdattn_decode_scored(ctypes.byref(step()), score, None) == pdattn.INVALID_ARG
     assert L.pdattn_decode_scored_fp8(ctypes.byref(step()), score, P, P, None) == pdattn.INVALID_ARG
+
+
+class Elsewhere:
+    """Stands for a tensor of bytes on another device."""
+    dtype, device, shape = torch.uint8, "cuda:7", (1 << 20,)
+
+    def get_device(self):
+        return 7
+
+    def is_contiguous(self):
+        return True
+
+    def stride(self):
+        return (1,)
+
+    def numel(self):
+        return 1 << 20
+
+    def data_ptr(self):
+        return P
+
+
+def test_what_lives_on_another_device_is_refused_before_the_library_is_called(monkeypatch):
+    """Host tensors take the part of the current device's."""
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0, raising=False)
+
+    class Library:
+        reached = 0
+
+        def __getattr__(self, name):
+            def call(*a):
+                Library.reached += 1
+                return pdattn.OK
+            return call
+    monkeypatch.setattr(pdattn, "_lib", Library())
+    bf, i32 = torch.bfloat16, torch.int32
+    q, kv, cache = torch.zeros(3, 4, 64, dtype=bf), torch.zeros(3, 2, 64, dtype=bf), torch.zeros(6, 2, 16, 64, dtype=bf)
+    table, lens, cu = torch.zeros(3, 4, dtype=i32), torch.ones(3, dtype=i32), torch.arange(4, dtype=i32)
+    freq, ws = torch.zeros(32), torch.zeros(1 << 16, dtype=torch.uint8)
+    codes, scales = torch.zeros(6, 2, 16, 64, dtype=torch.uint8), torch.ones(2)
+    vcodes = codes.transpose(2, 3).contiguous()
+    pool = pdattn.PagePool(torch.zeros(6, dtype=i32), torch.zeros(6, dtype=i32), torch.zeros(1, dtype=i32))
+    score = pdattn.Score(bias_slopes=torch.zeros(4))
+    pairs = torch.zeros(3, dtype=i32)
+    calls = {
+        "rope": lambda w, s, p: pdattn.rope_append(q, kv, kv, q, cache, cache, table, lens, freq, workspace=w),
+        "rope fp8": lambda w, s, p: pdattn.rope_append_fp8(q, kv, kv, q, codes, vcodes, scales, scales, table, lens, freq, workspace=w),
+        "prefill": lambda w, s, p: pdattn.prefill(q, cache, cache, table, lens, cu, 1.0, q, w, score=s),
+        "decode": lambda w, s, p: pdattn.decode_scored(q, cache, cache, table, lens, 1.0, q, w, s),
+        "decode fp8": lambda w, s, p: pdattn.decode_scored_fp8(q, codes, vcodes, scales, scales, table, lens, 1.0, q, w, s),
+        "reserve": lambda w, s, p: pdattn.pages_reserve(p, table, lens, lens, 16, w),
+        "fork": lambda w, s, p: pdattn.pages_fork(p, table, lens, pairs, pairs, pairs, pairs, 16, w),
+        "free": lambda w, s, p: pdattn.pages_free(p, table, lens, pairs, 16, w),
+        "compact": lambda w, s, p: pdattn.pages_compact(p, table, lens, pairs, pairs, 16, w),
+        "copy": lambda w, s, p: pdattn.pages_copy(cache, cache, pairs, pairs, workspace=w),
+    }
+    for name, call in calls.items():
+        Library.reached = 0
+        call(ws, score, pool)
+        assert Library.reached == 1, name
+        with pytest.raises(ValueError):
+            call(Elsewhere(), score, pool)
+        with pytest.raises(TypeError):
+            call(ws.view(torch.int32), score, pool)
+        with pytest.raises(ValueError):
+            call(ws[:2], score, pool)
+        assert Library.reached == 1, name
+    monkeypatch.setattr(score, "device", 7)
+    monkeypatch.setattr(pool, "device", 7)
+    for name in ("prefill", "decode", "decode fp8", "reserve", "fork", "free", "compact"):
+        with pytest.raises(ValueError):
+            calls[name](ws, score, pool)
+    assert Library.reached == 1
