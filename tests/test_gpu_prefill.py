@@ -425,3 +425,15 @@ def test_items_of_very_different_length():
     close(run(c), *reference(c))
     begin = begins(c, 128)
     close(run(c, key_begin=torch.from_numpy(begin).cuda()), *reference(c, begin=begin))
+
+
+@pytest.mark.parametrize("n,L", [([8] * 16, [4000 - 200 * i for i in range(16)]), ([700], [3000]), ([30, 0, 1] * 6, [900, 50, 7000] * 6)])
+def test_items_that_need_part_of_a_second_round(n, L):
+    """Between half and two thirds as many items as CTAs: three parts each, short ones fewer."""
+    c = make(n, L, 28, 4, 128, 16, seed=len(n))
+    slopes = torch.linspace(0, 0.1, 28, device="cuda")
+    out = run(c, bias_slopes=slopes, window=2500)
+    close(out, *reference(c, slopes=slopes, window=2500))
+    assert torch.equal(run(c, bias_slopes=slopes, window=2500), out)
+    small = torch.zeros(8448, dtype=torch.uint8, device="cuda")
+    close(run(c, ws=small), *reference(c))
