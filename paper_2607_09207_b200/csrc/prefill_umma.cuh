@@ -26,7 +26,7 @@
 // the non-finite elements of V to 0 before the product and note the keys; a row that does see such a key adds those elements
 // to its output at the end (whatever the weight, infinity and NaN are absorbing).
 //
-// Numbers: scores, maxima, sums and O in fp32; the weights are rounded to bf16 for the second product (relative 2^-9 each,
+// Numbers: scores, maxima, sums and O in fp32; the weights are rounded to bf16 for the second product (at most 2^-8 of each,
 // independent: the same size as the final rounding of the output; two terms, as in the decode kernel, would cost half as much
 // tensor work again).  The reference of the online softmax follows the running maximum only when that grew by more than 2^8,
 // so O is rarely rescaled.
