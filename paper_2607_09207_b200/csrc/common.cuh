@@ -369,13 +369,17 @@ using Walker = WalkerT<false>;
 // tanh to 2^-22: up to 3/4 the odd polynomial of degree 9 with the smallest largest error there (1.9e-7, found by Remez
 // exchange; leading coefficient first), past it 1 - 2 / (1 + exp(2 t)), which cancels for small t.
 __device__ constexpr float kTanh[5] = {0.0123188357f, -0.0492804514f, 0.132260918f, -0.333230765f, 0.999997228f};
-__device__ __forceinline__ float tanh_any(float t) {
-  const float u = t * t;
-  const float small = t * fmaf(fmaf(fmaf(fmaf(kTanh[0], u, kTanh[1]), u, kTanh[2]), u, kTanh[3]), u, kTanh[4]);
+constexpr float kTanhNear = 0.75f;
+__device__ __forceinline__ float tanh_far(float t) {
   float rc;
   const float e = fast_exp2(t * 2.8853900817779268f) + 1.f;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(e));
-  return fabsf(t) <= 0.75f ? small : fmaf(-2.f, rc, 1.f);
+  return fmaf(-2.f, rc, 1.f);
+}
+__device__ __forceinline__ float tanh_any(float t) {
+  const float u = t * t;
+  const float small = t * fmaf(fmaf(fmaf(fmaf(kTanh[0], u, kTanh[1]), u, kTanh[2]), u, kTanh[3]), u, kTanh[4]);
+  return fabsf(t) <= kTanhNear ? small : tanh_far(t);
 }
 
 // Modified scores of one tile on one warp (compute_tile and compute_tile_f8 with MOD).

@@ -36,7 +36,7 @@
 // barrier).  Tried and not faster: two threads a row (16 softmax warps), the scores in registers throughout (the code then
 // outgrows the instruction caches), a share of the exponentials on the FMA pipe, one MMA warp per tile (the tiles fall into step
 // and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 474-510 us, 0.94-1.01 PFLOP/s (the spread is
-// the clock under the power cap); with a cap 690, with a distance bias 625.  Also tried for those two: the bias as packed
+// the clock under the power cap); with a cap 683, with a distance bias 625.  Also tried for those two: the bias as packed
 // multiply-adds (no gain), worked out again in the second pass in place of the write-back (+13 %), tanh in unpacked operations (+10 %).
 //
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA thread drains, tensor memory
@@ -190,36 +190,37 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
 
 // x <- tanh(x k), 32 values, to 2^-22.  Capped scores mostly lie well inside the cap: up to 3/4 of it an odd polynomial (see
 // kTanh) does it on the FMA pipe; the exponential unit, which the softmax needs, would be asked three times per score
-// otherwise.  A warp that holds a larger one takes 1 - 2 / (1 + exp(2 x k)) for all its 32: what that loses in small values, 2^-22
-// of the cap, is at most 2^-21 of the largest score there (choosing value by value costs 645 us where this took 416: prompts of
-// 28/4 heads of 128 with a cap of 50).
-__device__ __forceinline__ void tanh_columns(uint32_t (&x)[32], float k) {
+// otherwise.  A warp that holds a larger one works out both forms and chooses value by value, as tanh_any does: a score's tanh has
+// the same bits whatever else its warp holds.  Rows that no token owns (`valid`; they hold what an earlier kernel left) do not count.
+__device__ __forceinline__ void tanh_columns(uint32_t (&x)[32], float k, bool valid) {
   float top = 0.f;
 #pragma unroll
   for (int i = 0; i < 32; i += 2) top = max3(top, fabsf(__uint_as_float(x[i])), fabsf(__uint_as_float(x[i + 1])));
-  if (__any_sync(0xffffffffu, top * fabsf(k) > 0.75f)) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      float rc;
-      const float e = fast_exp2(__uint_as_float(x[i]) * (k * 2.8853900817779268f)) + 1.f;
-      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rc) : "f"(e));
-      x[i] = __float_as_uint(fmaf(-2.f, rc, 1.f));
-    }
-    return;
-  }
   const uint64_t kk = pack_f32x2(k, k);
-#pragma unroll
-  for (int i = 0; i < 32; i += 2) {
+  auto pair = [&](int i, auto far_) {
     const uint64_t t = mul_f32x2(pack_f32x2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), kk);
     const uint64_t u = mul_f32x2(t, t);
     uint64_t p = fma_f32x2(pack_f32x2(kTanh[0], kTanh[0]), u, pack_f32x2(kTanh[1], kTanh[1]));
     p = fma_f32x2(p, u, pack_f32x2(kTanh[2], kTanh[2]));
     p = fma_f32x2(p, u, pack_f32x2(kTanh[3], kTanh[3]));
     p = fma_f32x2(p, u, pack_f32x2(kTanh[4], kTanh[4]));
-    float a, b;
-    unpack_f32x2(mul_f32x2(p, t), a, b);
-    x[i] = __float_as_uint(a);
-    x[i + 1] = __float_as_uint(b);
+    float y[2];
+    unpack_f32x2(mul_f32x2(p, t), y[0], y[1]);
+    if constexpr (decltype(far_)::value) {
+      float tt[2];
+      unpack_f32x2(t, tt[0], tt[1]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) y[e] = fabsf(tt[e]) <= kTanhNear ? y[e] : tanh_far(tt[e]);
+    }
+    x[i] = __float_as_uint(y[0]);
+    x[i + 1] = __float_as_uint(y[1]);
+  };
+  if (__any_sync(0xffffffffu, valid && top * fabsf(k) > kTanhNear)) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) pair(i, std::true_type{});
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) pair(i, std::false_type{});
   }
 }
 
@@ -714,7 +715,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           float m4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
           auto columns = [&](uint32_t (&x)[32], int q) {
             const int k0 = kt * PF_KEYS + q * 32;
-            if (CAP) tanh_columns(x, P.cap_x);
+            if (CAP) tanh_columns(x, P.cap_x, valid);
             if (GEN) {
               const float d0 = static_cast<float>(k0 - pos);
 #pragma unroll
@@ -760,7 +761,7 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
         const float mu = m_new == NEG_INF ? 0.f : m_new;
         const float alpha = grow ? fast_exp2(m - mu) : 1.f;
         m = m_new;
-        if (__any_sync(0xffffffffu, !first && alpha != 1.f)) {
+        if (__any_sync(0xffffffffu, valid && !first && alpha != 1.f)) {
           // new reference: scale this row of O (the product before this one was done when the scores came)
 #pragma unroll 1
           for (int q = 0; q < D / 16; ++q) {

@@ -437,3 +437,46 @@ def test_items_that_need_part_of_a_second_round(n, L):
     assert torch.equal(run(c, bias_slopes=slopes, window=2500), out)
     small = torch.zeros(8448, dtype=torch.uint8, device="cuda")
     close(run(c, ws=small), *reference(c))
+
+
+def capped_neighbours(G, cap):
+    """Two sequences whose rows share tiles with what nobody may notice: unused slots, a neighbour's queries, padding rows."""
+    c = make([9, 40], [150, 300], 2 * G, 2, 128, 16, seed=G, sharp=2.0)
+    for x in (c["kc"], c["vc"]):
+        x.nan_to_num_(0.0)                               # unused slots: 0 in place of NaN
+    return c, dict(logit_cap=cap)
+
+
+@pytest.mark.parametrize("G", [2, 7])
+@pytest.mark.parametrize("cap", [50.0, 1e4, 1e5, 1e6])
+@pytest.mark.parametrize("junk", [1e30, math.inf])
+def test_capped_scores_do_not_depend_on_what_the_row_does_not_see(G, cap, junk):
+    """The same bits whatever lies in unused slots, behind key_begin, in the next sequence's queries, or was left in shared
+    memory by an earlier kernel."""
+    c, score = capped_neighbours(G, cap)
+    begin = np.zeros(49, np.int32)
+    begin[:9] = 70
+    dev = torch.from_numpy(begin).cuda()
+    plain = run(c, key_begin=dev, **score)
+    want, size = reference(c, cap=cap, begin=begin)
+    close(plain, want, size)
+    bs, tab = c["bs"], c["tab"]
+    for s, L in ((0, 150), (1, 300)):                    # past the end of each context
+        c["kc"][tab[s, (L - 1) // bs], :, L % bs:] = junk
+        c["vc"][tab[s, (L - 1) // bs], :, L % bs:] = junk
+    c["kc"][tab[0, :4]] = junk                           # keys 0 .. 63: before the first sequence's first key
+    c["q"][9:] *= 1e4
+    run(make([300], [300], 2 * G, 2, 128, 16, sharp=1e5), logit_cap=1.0)       # large queries in every tile of shared memory
+    out = run(c, key_begin=dev, **score)
+    assert torch.equal(out[:9], plain[:9])
+    close(out[:9], want[:9], size[:9])
+
+
+@pytest.mark.parametrize("cap", [1e4, 1e5, 1e6])
+def test_large_and_small_capped_scores_in_one_tile(cap):
+    """A row's small scores keep their precision beside another row's scores past the cap."""
+    c = make([64], [300], 4, 2, 128, 16, sharp=2.0)
+    c["q"][::5] *= 2e6                                   # every fifth token: scores far past the cap
+    want, size = reference(c, cap=cap)
+    small = np.arange(64) % 5 != 0
+    close(run(c, logit_cap=cap)[torch.from_numpy(small).cuda()], want[small], size[small])
