@@ -366,10 +366,11 @@ struct WalkerT {
 };
 using Walker = WalkerT<false>;
 
-// tanh to 2^-22: up to 3/4 the odd polynomial of degree 9 with the smallest largest error there (1.9e-7, found by Remez
-// exchange; leading coefficient first), past it 1 - 2 / (1 + exp(2 t)), which cancels for small t.
-__device__ constexpr float kTanh[5] = {0.0123188357f, -0.0492804514f, 0.132260918f, -0.333230765f, 0.999997228f};
-constexpr float kTanhNear = 0.75f;
+// tanh to 2^-21 of its value.  Up to 0.6 an odd polynomial whose leading coefficient is 1: t (1 + u q(u)), u = t^2, with the
+// q of degree 3 that has the smallest largest RELATIVE error there (2^-23.5, found by Remez exchange; with fp32 rounding
+// 2^-22.4; leading coefficient first).  Past it 1 - 2 / (1 + exp(2 t)), which cancels for small t.
+__device__ constexpr float kTanh[4] = {0.015612634f, -0.052211806f, 0.13313116f, -0.33332598f};
+constexpr float kTanhNear = 0.6f;
 __device__ __forceinline__ float tanh_far(float t) {
   float rc;
   const float e = fast_exp2(t * 2.8853900817779268f) + 1.f;
@@ -378,7 +379,7 @@ __device__ __forceinline__ float tanh_far(float t) {
 }
 __device__ __forceinline__ float tanh_any(float t) {
   const float u = t * t;
-  const float small = t * fmaf(fmaf(fmaf(fmaf(kTanh[0], u, kTanh[1]), u, kTanh[2]), u, kTanh[3]), u, kTanh[4]);
+  const float small = t * fmaf(fmaf(fmaf(fmaf(kTanh[0], u, kTanh[1]), u, kTanh[2]), u, kTanh[3]), u, 1.f);
   return fabsf(t) <= kTanhNear ? small : tanh_far(t);
 }
 

@@ -36,7 +36,7 @@
 // barrier).  Tried and not faster: two threads a row (16 softmax warps), the scores in registers throughout (the code then
 // outgrows the instruction caches), a share of the exponentials on the FMA pipe, one MMA warp per tile (the tiles fall into step
 // and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 474-510 us, 0.94-1.01 PFLOP/s (the spread is
-// the clock under the power cap); with a cap 683, with a distance bias 625.  Also tried for those two: the bias as packed
+// the clock under the power cap); with a cap 682 (1055 where every score lies past it), with a distance bias 625.  Also tried for those two: the bias as packed
 // multiply-adds (no gain), worked out again in the second pass in place of the write-back (+13 %), tanh in unpacked operations (+10 %).
 //
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA thread drains, tensor memory
@@ -188,7 +188,7 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   return d;
 }
 
-// x <- tanh(x k), 32 values, to 2^-22.  Capped scores mostly lie well inside the cap: up to 3/4 of it an odd polynomial (see
+// x <- tanh(x k), 32 values, to 2^-21 of each.  Capped scores mostly lie well inside the cap: up to 0.6 of it an odd polynomial (see
 // kTanh) does it on the FMA pipe; the exponential unit, which the softmax needs, would be asked three times per score
 // otherwise.  A warp that holds a larger one works out both forms and chooses value by value, as tanh_any does: a score's tanh has
 // the same bits whatever else its warp holds.  Rows that no token owns (`valid`; they hold what an earlier kernel left) do not count.
@@ -203,7 +203,7 @@ __device__ __forceinline__ void tanh_columns(uint32_t (&x)[32], float k, bool va
     uint64_t p = fma_f32x2(pack_f32x2(kTanh[0], kTanh[0]), u, pack_f32x2(kTanh[1], kTanh[1]));
     p = fma_f32x2(p, u, pack_f32x2(kTanh[2], kTanh[2]));
     p = fma_f32x2(p, u, pack_f32x2(kTanh[3], kTanh[3]));
-    p = fma_f32x2(p, u, pack_f32x2(kTanh[4], kTanh[4]));
+    p = fma_f32x2(p, u, pack_f32x2(1.f, 1.f));
     float y[2];
     unpack_f32x2(mul_f32x2(p, t), y[0], y[1]);
     if constexpr (decltype(far_)::value) {

@@ -480,3 +480,20 @@ def test_large_and_small_capped_scores_in_one_tile(cap):
     want, size = reference(c, cap=cap)
     small = np.arange(64) % 5 != 0
     close(run(c, logit_cap=cap)[torch.from_numpy(small).cuda()], want[small], size[small])
+
+
+@pytest.mark.parametrize("cap", [1e4, 3e4, 1e5, 1e6])
+@pytest.mark.parametrize("X", [8192.0, -8192.0])
+def test_large_caps_keep_large_scores(cap, X):
+    """Two keys whose logits agree: a score of X whose bias takes the capped score away, and a score of 0.  With v = 1 and -1 the
+    output is tanh of half the logits' error.  Roundings of the first logit, in units of 2^-24 of it: tanh 8 (2^-21), its argument
+    2, cap and product 3, slope 2, their sum 1; 24 are allowed for.  The weights are rounded to bf16: 2^-9 of each at most."""
+    d = 128
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, kc, vc = (torch.zeros(s, device="cuda", dtype=BF16) for s in ((1, 2, d), (1, 1, 16, d), (1, 1, 16, d)))
+    q[..., 3], kc[0, 0, 0, 3] = X / 64, 64.0
+    vc[0, 0, 0], vc[0, 0, 1] = 1.0, -1.0
+    c = dict(q=q, kc=kc, vc=vc, table=i32([[0]]), lens=i32([2]), cu=i32([0, 1]), n=[1], L=[2], bs=16, scale=1.0)
+    capped = cap * math.tanh(X / cap)
+    out = run(c, logit_cap=cap, bias_slopes=torch.full((2,), capped, device="cuda"))
+    assert float(out.float().abs().max()) <= 12 * 2.0 ** -24 * abs(X) + 2.0 ** -8

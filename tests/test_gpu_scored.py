@@ -198,3 +198,28 @@ def test_caps_far_from_the_scores(cap):
     w = W.make_custom([300, 64, 700], 8, 2, 128, 16, device="cuda:0")
     w.q.mul_(2.0)
     close(run(w, cap=cap), *reference(w, cap=cap), BF16_WEIGHTS)
+
+
+@pytest.mark.parametrize("cap", [1e4, 3e4, 1e5, 1e6])
+@pytest.mark.parametrize("X", [8192.0, -8192.0])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_large_caps_keep_large_scores(cap, X, fp8):
+    """Two keys whose logits agree: a score of X whose bias takes the capped score away, and a score of 0.  With v = 1 and -1 the
+    output is tanh of half the logits' error.  Roundings of the first logit, in units of 2^-24 of it: tanh 8 (2^-21), its argument
+    7, cap and product 3, slope 2, their sum 1; 24 are allowed for.  The weights: 2^-15, fp8 2^-11."""
+    d = 128
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    q, kc, vc = (torch.zeros(s, device="cuda", dtype=BF16) for s in ((1, 2, d), (1, 1, 16, d), (1, 1, 16, d)))
+    q[..., 3], kc[0, 0, 0, 3] = X / 64, 64.0
+    vc[0, 0, 0], vc[0, 0, 1] = 1.0, -1.0
+    out, ws = torch.empty_like(q), pdattn.alloc_workspace(1, 2, 1, d)
+    sc = pdattn.Score(logit_cap=cap, bias_slopes=torch.full((2,), cap * math.tanh(X / cap), device="cuda"))
+    if fp8:
+        one = torch.ones(1, device="cuda")
+        k8, v8 = kc.to(F8).view(torch.uint8), vc.to(F8).view(torch.uint8).transpose(2, 3).contiguous()
+        pdattn.decode_scored_fp8(q, k8, v8, one, one, i32([[0]]), i32([2]), 1.0, out, ws, sc)
+    else:
+        pdattn.decode_scored(q, kc, vc, i32([[0]]), i32([2]), 1.0, out, ws, sc)
+    assert pdattn.check(ws) == pdattn.OK
+    # (the output is rounded once more, 2^-8 of a value below 0.01)
+    assert float(out.float().abs().max()) <= (12 * 2.0 ** -24 * abs(X) + 2.0 ** -11) * (1 + 2.0 ** -8)
