@@ -371,7 +371,8 @@ pdattn_status pdattn_pages_free(const pdattn_page_pool* pool, int32_t* block_tab
 /*
  * Makes the referenced pages dense: with n of them, those at or past n move, in ascending order, into the unreferenced
  * pages below n, in ascending order.  Tables and books are renumbered; the pairs are written to copy_src / copy_dst
- * [max_copies >= num_blocks / 2], the rest of which becomes -1.
+ * [max_copies >= num_blocks / 2], the rest of which becomes -1.  An entry of a row that names no referenced page stays as it
+ * is and is reported as PDATTN_BAD_PAGE_INDEX.
  */
 pdattn_status pdattn_pages_compact(const pdattn_page_pool* pool, int32_t* block_table, const int32_t* context_lens,
                                    int num_seqs, int max_blocks_per_seq, int block_size, int32_t* copy_src,

@@ -23,10 +23,10 @@ struct PagePool {
 // Scratch behind the cleared part of the workspace
 struct PagesScratch {
   int32_t* err;        // the workspace's sticky error word
-  int32_t* head;       // [0]: fork accepted, [1]: live pages
+  int32_t* head;       // [0]: fork accepted
   int32_t* lens;       // [S] fork: parent lengths
   int32_t* tails;      // [S] fork: page of the child's partial tail, -1 = none
-  int32_t* map;        // [NB] compact: new id of page p
+  int32_t* map;        // [NB] compact: new id of page p, -1: nothing references it
 };
 
 constexpr int kPagesThreads = 1024;
@@ -389,7 +389,7 @@ pages_books_kernel(PagePool pool, int32_t* __restrict__ copy_src, int32_t* __res
           const int k = id - at;
           if (k < max_copies) copy_dst[k] = id;
         }
-        if (COMPACT) X.map[id] = id < n_live ? id : -1;
+        if (COMPACT) X.map[id] = live[e] && id < n_live ? id : -1;   // (those that move: below)
       }
       at += live[e];
     }
@@ -411,7 +411,6 @@ pages_books_kernel(PagePool pool, int32_t* __restrict__ copy_src, int32_t* __res
       pool.ref[a] = 0;
       X.map[a] = b;
     }
-    if (g == 0) X.head[1] = n_live;
   }
   cluster.sync();                               // no block leaves while another may still write to its shared memory
 }
@@ -424,14 +423,12 @@ pages_remap_kernel(PagePool pool, int32_t* __restrict__ table, const int32_t* __
   const int s = blockIdx.x;
   const int64_t need = (static_cast<int64_t>(lens[s]) + bs - 1) / bs;
   const int np = static_cast<int>(need < 0 ? 0 : need < MB ? need : MB);
-  const int n_live = X.head[1];
   int32_t* row = table + static_cast<int64_t>(s) * MB;
   for (int b = threadIdx.x; b < np; b += blockDim.x) {
     const int id = row[b];
-    if (id >= 0 && id < n_live) continue;
     const int to = id >= 0 && id < pool.NB ? X.map[id] : -1;
-    if (to >= 0) row[b] = to;
-    else atomicOr(X.err, ERR_BAD_PAGE);         // an entry that names no live page stays as it is
+    if (to < 0) atomicOr(X.err, ERR_BAD_PAGE);  // an entry that names no live page stays as it is
+    else if (to != id) row[b] = to;
   }
 }
 

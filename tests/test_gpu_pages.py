@@ -283,3 +283,17 @@ def test_captured_and_replayed():
         graph.replay()
     assert pdattn.check(d.ws) == pdattn.OK
     d.same()                                            # everything was freed: the books of an empty pool
+
+
+@pytest.mark.parametrize("dead", [1, 2])
+def test_a_dead_page_below_the_live_ones_is_reported_by_compaction(dead):
+    """Rows 0 and 1 hold pages 0 and 3, pages 1 and 2 are free; an entry that names one of those is left and reported."""
+    m = Books(9, 4, 3, 16)
+    d = Device(m)
+    assert d.reserve([16, 32, 16, 16]) == m.reserve([16, 32, 16, 16])       # pages 0; 1, 2; 3; 4
+    assert d.free([1]) == m.free([1])
+    d.table[3, 0] = dead                                # page 4 of row 3 is now nobody's; pages 0, 3, 4 are live
+    pdattn.pages_compact(d.pool, d.table, d.lens, d.src[:4], d.dst[:4], 16, d.ws)
+    assert pdattn.check(d.ws) == pdattn.BAD_PAGE_INDEX
+    assert d.table[:, 0].tolist() == [0, -1, 1, dead]   # page 3 moved to 1, page 4 to 2
+    assert pdattn.check(d.ws) == pdattn.OK
