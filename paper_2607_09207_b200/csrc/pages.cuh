@@ -87,6 +87,7 @@ pages_reserve_kernel(PagePool pool, int32_t* __restrict__ table, int32_t* __rest
                      const int32_t* __restrict__ new_tokens, int S, int MB, int bs, int32_t* err) {
   __shared__ int warp_sums[32];
   __shared__ int first[kPagesThreads], from[kPagesThreads], count_of[kPagesThreads];
+  __shared__ unsigned long long wanted;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int64_t room = static_cast<int64_t>(MB) * bs;
@@ -100,20 +101,20 @@ pages_reserve_kernel(PagePool pool, int32_t* __restrict__ table, int32_t* __rest
     return static_cast<int>((static_cast<int64_t>(L) + n + bs - 1) / bs - (static_cast<int64_t>(L) + bs - 1) / bs);
   };
   const int count = *pool.free_count;
-  int64_t total = 0;
-  for (int base = 0; base < S; base += kPagesThreads) {
-    int L, n, need = 0;
-    if (base + tid < S) {
-      need = request(base + tid, L, n);
-      if (need < 0) {
-        atomicOr(err, ERR_BAD_SEQUENCE);          // left as it is; the others are served
-        need = 0;
-      }
-    }
-    int sum;
-    block_scan_excl(need, warp_sums, &sum);
-    total += sum;
+  // The request's total in 64 bits: 1024 rows of a wide table can ask for more pages than 32 hold.  What is granted below is at
+  // most the pool, so the sums there fit.
+  unsigned long long mine = 0;
+  for (int s = tid; s < S; s += kPagesThreads) {
+    int L, n;
+    const int need = request(s, L, n);
+    if (need < 0) atomicOr(err, ERR_BAD_SEQUENCE);   // left as it is; the others are served
+    else mine += need;
   }
+  if (tid == 0) wanted = 0;
+  __syncthreads();
+  if (mine > 0) atomicAdd(&wanted, mine);
+  __syncthreads();
+  const int64_t total = static_cast<int64_t>(wanted);
   if (total > count || count > pool.NB) {
     if (tid == 0) atomicOr(err, ERR_OUT_OF_PAGES);
     return;

@@ -297,3 +297,20 @@ def test_a_dead_page_below_the_live_ones_is_reported_by_compaction(dead):
     assert pdattn.check(d.ws) == pdattn.BAD_PAGE_INDEX
     assert d.table[:, 0].tolist() == [0, -1, 1, dead]   # page 3 moved to 1, page 4 to 2
     assert pdattn.check(d.ws) == pdattn.OK
+
+
+def test_requests_whose_total_passes_32_bits_are_refused():
+    """1024 rows of 2^21 pages each: 2^31 pages in all."""
+    NB, S, MB, bs = 64, 1025, 1 << 21, 16
+    pool = pdattn.PagePool.create(NB)
+    table = torch.full((S, MB), -1, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(S, dtype=torch.int32, device="cuda")
+    ws = pdattn.alloc_pages_workspace(NB, S)
+    for rows, new in ((1024, MB * bs), (1025, MB * bs), (1024, MB * bs - 15)):
+        ask = torch.zeros_like(lens)
+        ask[:rows] = new
+        pdattn.pages_reserve(pool, table, lens, ask, bs, ws)
+        assert pdattn.check(ws) == pdattn.OUT_OF_PAGES
+        assert int(pool.free_count) == NB and not lens.any() and not pool.ref_counts.any()
+        assert pool.free_list.tolist() == list(range(NB - 1, -1, -1))
+    assert bool((table[::100] == -1).all())
