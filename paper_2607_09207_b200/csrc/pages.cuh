@@ -90,7 +90,7 @@ pages_reserve_kernel(PagePool pool, int32_t* __restrict__ table, int32_t* __rest
   __shared__ unsigned long long wanted;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int64_t room = static_cast<int64_t>(MB) * bs;
+  const int64_t room = min(static_cast<int64_t>(MB) * bs, static_cast<int64_t>(INT32_MAX));   // (lengths are int32)
   auto request = [&](int s, int& L, int& n) {     // pages the sequence needs; n = tokens granted
     L = lens[s];
     n = new_tokens[s];

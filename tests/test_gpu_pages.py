@@ -314,3 +314,17 @@ def test_requests_whose_total_passes_32_bits_are_refused():
         assert int(pool.free_count) == NB and not lens.any() and not pool.ref_counts.any()
         assert pool.free_list.tolist() == list(range(NB - 1, -1, -1))
     assert bool((table[::100] == -1).all())
+
+
+def test_lengths_stay_within_32_bits():
+    """A row wide enough for 2^31 tokens: the request that would pass the largest length is refused, the one before it served."""
+    MB, bs, top = 1 << 27, 16, 2 ** 31 - 1
+    pool, ws = pdattn.PagePool.create(8), pdattn.alloc_pages_workspace(8, 1)
+    i32 = lambda x: torch.tensor([x], dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.full((1, MB), -1, dtype=torch.int32, device="cuda")
+    lens = i32(top - 40)
+    pdattn.pages_reserve(pool, table, lens, i32(41), bs, ws)
+    assert pdattn.check(ws) == pdattn.BAD_SEQUENCE and int(lens) == top - 40 and int(pool.free_count) == 8
+    pdattn.pages_reserve(pool, table, lens, i32(40), bs, ws)
+    assert pdattn.check(ws) == pdattn.OK and int(lens) == top and int(pool.free_count) == 6
+    assert table[0, -4:].tolist() == [-1, -1, 0, 1]
