@@ -211,7 +211,7 @@ pdattn_status pdattn_append_kv_fp8(const void* k_new, const void* v_new, void* k
  * pdattn_args), and context_lens[s] becomes t + 1 (DEVICE, updated in place).  The page must
  * already be in the table: page allocation stays with the caller.  A sequence whose target page id
  * is outside [0, num_blocks), or whose table row is full, is left untouched and, if `workspace`
- * (DEVICE, may be NULL) is given, its sticky error word is set (see pdattn_check).
+ * (DEVICE, may be NULL, 4-byte aligned) is given, its sticky error word is set (see pdattn_check).
  * Followed by pdattn_decode_ex with context_lens_host = NULL, a whole decode step needs no host
  * work that depends on the lengths.
  */
@@ -261,7 +261,7 @@ typedef struct {
   int num_seqs, num_q_heads;        /* num_q_heads 0: only k and v (q, q_out may be NULL)             */
   int num_kv_heads, head_dim, block_size, max_blocks_per_seq, num_blocks;
   int64_t kv_block_stride, kv_head_stride, kv_token_stride;
-  void* workspace;                  /* DEVICE, may be NULL: its sticky error word.  pdattn_check clears 8448 bytes, so one
+  void* workspace;                  /* DEVICE, may be NULL, 4-byte aligned: its sticky error word.  pdattn_check clears 8448 bytes, so one
                                        that is checked has them and was given to pdattn_workspace_init */
 } pdattn_rope_args;
 pdattn_status pdattn_rope_append(const pdattn_rope_args* args, pdattn_stream_t stream);

@@ -41,7 +41,7 @@ pdattn_status rope_common(const pdattn_rope_args* a, bool fp8, const float* k_sc
     return PDATTN_INVALID_ARG;
   }
   if (misaligned(a->k_new, 16) || misaligned(a->v_new, 16) || misaligned(a->k_cache, 16) || misaligned(a->v_cache, 16) ||
-      misaligned(a->q, 16) || misaligned(a->q_out, 16))
+      misaligned(a->q, 16) || misaligned(a->q_out, 16) || misaligned(a->workspace, 4))
     return PDATTN_MISALIGNED;
   // in place only row for row: a dense output over a strided input would overwrite rows that are still to be read
   if (a->num_q_heads > 0 && a->q_out == a->q && a->q_token_stride != q_row) return PDATTN_INVALID_ARG;
@@ -252,7 +252,7 @@ pdattn_status pdattn_pages_copy(void* k_cache, void* v_cache, const int32_t* cop
   }
   if (kv_block_stride <= 0 || kv_head_stride <= 0 || kv_token_stride < head_dim) return PDATTN_INVALID_ARG;
   if ((kv_block_stride | kv_head_stride | kv_token_stride) % 8 != 0) return PDATTN_UNSUPPORTED;
-  if (misaligned(k_cache, 16) || misaligned(v_cache, 16)) return PDATTN_MISALIGNED;
+  if (misaligned(k_cache, 16) || misaligned(v_cache, 16) || misaligned(workspace, 4)) return PDATTN_MISALIGNED;
   int dev = 0;
   DevInfo* di = nullptr;
   const pdattn_status s = device_info(&dev, &di);

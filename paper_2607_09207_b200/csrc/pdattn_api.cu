@@ -278,8 +278,8 @@ pdattn_status pdattn_append_kv(const void* k_new, const void* v_new, void* k_cac
   if (!k_new || !v_new || !k_cache || !v_cache || !block_table || !context_lens) return PDATTN_INVALID_ARG;
   if (kv_block_stride <= 0 || kv_head_stride <= 0 || kv_token_stride < head_dim) return PDATTN_INVALID_ARG;
   if ((kv_block_stride | kv_head_stride | kv_token_stride) % 8 != 0) return PDATTN_UNSUPPORTED;
-  auto mis = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; };
-  if (mis(k_new) || mis(v_new) || mis(k_cache) || mis(v_cache)) return PDATTN_MISALIGNED;
+  auto mis = [](const void* p, size_t al) { return (reinterpret_cast<uintptr_t>(p) & (al - 1)) != 0; };
+  if (mis(k_new, 16) || mis(v_new, 16) || mis(k_cache, 16) || mis(v_cache, 16) || mis(workspace, 4)) return PDATTN_MISALIGNED;
   cudaError_t e = launch_dependent(
       append_kernel, num_seqs, 32 * num_kv_heads, 0, reinterpret_cast<cudaStream_t>(stream), true,
       static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new),
@@ -308,8 +308,8 @@ pdattn_status pdattn_append_kv_fp8(const void* k_new, const void* v_new, void* k
   if (num_seqs == 0) return PDATTN_OK;
   if (!k_new || !v_new || !k_cache || !v_cache || !k_scale || !v_scale || !block_table || !context_lens)
     return PDATTN_INVALID_ARG;
-  auto mis = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; };
-  if (mis(k_new) || mis(v_new) || mis(k_cache) || mis(v_cache)) return PDATTN_MISALIGNED;
+  auto mis = [](const void* p, size_t al) { return (reinterpret_cast<uintptr_t>(p) & (al - 1)) != 0; };
+  if (mis(k_new, 16) || mis(v_new, 16) || mis(k_cache, 16) || mis(v_cache, 16) || mis(workspace, 4)) return PDATTN_MISALIGNED;
   cudaError_t e = launch_dependent(
       append_fp8_kernel, num_seqs, 32 * num_kv_heads, 0, reinterpret_cast<cudaStream_t>(stream), true,
       static_cast<const __nv_bfloat16*>(k_new), static_cast<const __nv_bfloat16*>(v_new),

@@ -250,3 +250,18 @@ def test_what_lives_on_another_device_is_refused_before_the_library_is_called(mo
         with pytest.raises(ValueError):
             calls[name](ws, score, pool)
     assert Library.reached == 1
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_an_error_word_that_is_not_aligned_is_refused(off):
+    """The kernels set bits of it atomically, so it has to be a whole word; any word will do."""
+    L = pdattn.lib()
+    ref = ctypes.byref
+
+    def calls(ws):
+        return [L.pdattn_rope_append(ref(rope(workspace=ws)), None), L.pdattn_rope_append_fp8(ref(rope(workspace=ws)), P, P, None),
+                L.pdattn_pages_copy(P, P, P, P, 4, 2, 64, 16, 12, 2, 2048, 1024, 64, ws, None),
+                L.pdattn_append_kv(P, P, P, P, P, P, 3, 2, 64, 16, 4, 12, 2048, 1024, 64, ws, None),
+                L.pdattn_append_kv_fp8(P, P, P, P, P, P, P, P, 3, 2, 64, 16, 4, 12, ws, None)]
+    assert calls(P + off) == [pdattn.MISALIGNED] * 5
+    assert pdattn.MISALIGNED not in calls(P + 4 * off) if not torch.cuda.is_available() else True
