@@ -150,6 +150,10 @@ PDATTN_HD inline int first_key(int context_len, int key_begin, int window) {
   return lo;
 }
 
+// Parts of an item of pdattn_prefill that were written, from the word its CTAs left in the workspace.  When a call's bounded waits
+// run out, units may never be drawn and the word is whatever the memory held: it must not lead past the parts' room.
+PDATTN_HD inline int join_parts(int word, int splits) { return word < 0 ? 0 : word < splits ? word : splits; }
+
 // tiles of one sequence that a plan covers
 PDATTN_HD inline int64_t seq_tiles(int64_t context_len, int64_t start_tile) {
   const int64_t all = context_len > 0 ? (context_len + kTileTokens - 1) / kTileTokens : 0;

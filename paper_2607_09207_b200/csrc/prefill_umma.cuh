@@ -908,7 +908,7 @@ __global__ void __launch_bounds__(128)
 prefill_join_kernel(const __grid_constant__ PrefillParams P) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int item = blockIdx.x, t = blockIdx.y, q = blockIdx.z, r = threadIdx.x;
-  const int parts = P.parts[item];
+  const int parts = join_parts(P.parts[item], P.splits);
   if (parts <= 1) return;
   int s, row0, row1, tok0;
   prefill_slot(P, P.n_items / P.Hkv - 1 - item / P.Hkv, r & 31, s, row0, row1, tok0);

@@ -265,3 +265,22 @@ def test_an_error_word_that_is_not_aligned_is_refused(off):
                 L.pdattn_append_kv_fp8(P, P, P, P, P, P, P, P, 3, 2, 64, 16, 4, 12, ws, None)]
     assert calls(P + off) == [pdattn.MISALIGNED] * 5
     assert pdattn.MISALIGNED not in calls(P + 4 * off) if not torch.cuda.is_available() else True
+
+
+def test_the_join_of_cut_prompt_items_stays_within_its_parts_whatever_the_workspace_holds(tmp_path):
+    """The word that says how many parts an item has is not written when a call's waits run out."""
+    import os
+    import shutil
+    import subprocess
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        pytest.skip("no C++ compiler")
+    here, exe = os.path.dirname(os.path.abspath(__file__)), str(tmp_path / "join_parts_check")
+    subprocess.check_call([cxx, "-std=c++17", "-Wall", "-Wextra", "-Werror", "-I", pd_build.CSRC,
+                           os.path.join(here, "c", "join_parts_check.cpp"), "-o", exe])
+    out = subprocess.run([exe], capture_output=True, text=True, timeout=60)
+    assert out.returncode == 0 and "join_parts_check: ok" in out.stdout, out.stdout + out.stderr
+    # and the kernel reads that word nowhere else
+    with open(os.path.join(pd_build.CSRC, "prefill_umma.cuh")) as f:
+        reads = [x for x in f.read().split("P.parts[item]")[1:] if not x.startswith(" = ")]
+    assert len(reads) == 1 and reads[0].startswith(", P.splits);")
