@@ -600,14 +600,30 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       // ================= guards of V: each takes its share of every 64 keys
       const int w = warp - (16 - PF_GUARDS);
       constexpr int WORDS = 4 / PF_GUARDS;                // 32 keys each
+      // A softmax warp reads v_bad of a tile after it has handed the tile's weights over, so the products do not hold the entry for
+      // it.  Within an item its next weights do, and the two tiles end at most 3 key tiles apart (hi grows by at most one a token);
+      // so what may still be unread when tile c comes is the entry of c - 8 where that belongs to an item before this one: its
+      // release says that it was read.  (Items three back are released, or this one could not have been published.  A read
+      // before the weights go would do too, and costs 4 % of 8191 causal tokens.)
       const PrefillItem* ip;
-      int c = 0, slot = 0;
+      int c = 0, slot = 0, start = 0, start1 = 0;         // first tiles of this item and of the one before it
+      int read = -1;                                      // items up to this one are known to be released
       bool ok = true;
       for (int k = 0; ok && get_item(k, ip); ++k) {
         const PrefillItem& it = *ip;
         const int k1 = tiles_to(it);
+        start1 = start;
+        start = c;
         for (int kt = tiles_from(it); kt < k1; ++kt) {
           if (!active(it, 0, kt) && !active(it, 1, kt)) continue;
+          const int owner = c - 8 >= start1 ? k - 1 : k - 2;
+          if (c >= 8 && c - 8 < start && owner > read) {
+            if (!__all_sync(0xffffffffu, prefill_wait(smem_u32(&ctrl->item_free[owner % PF_ITEMS]), (owner / PF_ITEMS) & 1, abort_flag))) {
+              ok = false;
+              break;
+            }
+            read = owner;
+          }
           if (!__all_sync(0xffffffffu, prefill_wait(smem_u32(&ctrl->v_full[c & 7]), (c >> 3) & 1, abort_flag))) {
             ok = false;
             break;

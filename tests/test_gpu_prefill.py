@@ -497,3 +497,22 @@ def test_large_caps_keep_large_scores(cap, X):
     capped = cap * math.tanh(X / cap)
     out = run(c, logit_cap=cap, bias_slopes=torch.full((2,), capped, device="cuda"))
     assert float(out.float().abs().max()) <= 12 * 2.0 ** -24 * abs(X) + 2.0 ** -8
+
+
+@pytest.mark.parametrize("d,Hq", [(64, 2), (128, 6)])
+def test_second_tiles_that_come_and_go_beside_values_that_are_not_finite(d, Hq):
+    """Items of one and of two tiles in turn, many to a CTA, masks and non-finite values in most of their key tiles."""
+    r = np.random.default_rng(11)
+    S = 420
+    n = np.where(np.arange(S) % 3 == 0, r.integers(1, 260, S), r.integers(1, 60, S))
+    L = n + r.integers(0, 1400, S)
+    c = make(n, L, Hq, 2, d, 16, seed=d)
+    for s in range(S):
+        for t in r.integers(0, L[s], 3):
+            c["vc"][c["tab"][s, t // 16], int(r.integers(0, 2)), t % 16, int(r.integers(0, d))] = float(r.choice([math.inf, -math.inf, math.nan]))
+    pos = np.concatenate([np.arange(b - a, b) for a, b in zip(n, L)])
+    begin = np.maximum(0, pos - r.integers(0, 1200, len(pos))).astype(np.int32)
+    want, size = reference(c, begin=begin)
+    dev = torch.from_numpy(begin).cuda()
+    for _ in range(3):
+        close(run(c, key_begin=dev), want, size)
