@@ -279,6 +279,8 @@ pdattn_status pdattn_rope_append_fp8(const pdattn_rope_args* args, const float* 
  * key_begin is a document mask (the first key of the token's own document); prefix_lens is a prefix mask (every token
  * of the sequence sees the first prefix_lens[s] keys, whatever its position); window is a sliding window.  A token that
  * sees no key gets zeros.  What a token does not see never reaches its output, infinities and NaN included.
+ * An infinity or NaN in an element of v that a token does see leaves that element of its output not finite: an infinity
+ * becomes an infinity, or NaN where its weight vanishes in 32 bits or where infinities of both signs meet.
  * All members zero / NULL: plain causal attention.
  */
 typedef struct {

@@ -516,3 +516,24 @@ def test_second_tiles_that_come_and_go_beside_values_that_are_not_finite(d, Hq):
     dev = torch.from_numpy(begin).cuda()
     for _ in range(3):
         close(run(c, key_begin=dev), want, size)
+
+
+@pytest.mark.parametrize("L,key", [(600, 5), (600, 560), (600, 300), (9000, 40), (9000, 8900)])
+def test_a_visible_infinity_of_vanishing_weight_is_never_lost(L, key):
+    """A steep bias: the weight of a far key is 0 in 32 bits.  Whatever tile it lies in, what sees it is not finite and nothing else
+    is touched."""
+    n = 90
+    c = make([n], [L], 4, 2, 128, 16)
+    c["vc"][c["tab"][0, key // 16], 0, key % 16, 9] = math.inf
+    slopes = torch.full((4,), 3.0, device="cuda")
+    out = run(c, bias_slopes=slopes)
+    c["vc"][c["tab"][0, key // 16], 0, key % 16, 9] = 0.0
+    want, size = reference(c, slopes=slopes)
+    sees = torch.arange(L - n, L) >= key
+    hit = torch.zeros(out.shape, dtype=torch.bool)
+    hit[sees, :2, 9] = True
+    assert not out.cpu()[hit].isfinite().any()
+    o = out.clone()
+    o[hit.cuda()] = 0.0
+    want[hit.numpy()] = 0.0
+    close(o, want, size)

@@ -223,3 +223,21 @@ def test_large_caps_keep_large_scores(cap, X, fp8):
     assert pdattn.check(ws) == pdattn.OK
     # (the output is rounded once more, 2^-8 of a value below 0.01)
     assert float(out.float().abs().max()) <= (12 * 2.0 ** -24 * abs(X) + 2.0 ** -11) * (1 + 2.0 ** -8)
+
+
+@pytest.mark.parametrize("L,key", [(600, 5), (600, 590), (9000, 40)])
+def test_a_visible_infinity_of_vanishing_weight_is_never_lost(L, key):
+    """A steep bias: the weight of a far key is 0 in 32 bits.  Its element is not finite all the same, the others are as ever."""
+    w = W.make_custom([L, 70], 8, 2, 128, 16, device="cuda:0")
+    slopes, page = torch.full((8,), 3.0, device="cuda"), int(w.block_table[0, key // 16])
+    keep = w.v_cache[page, 1, key % 16, 9].clone()
+    w.v_cache[page, 1, key % 16, 9] = math.inf
+    for host in (True, False):
+        out = run(w, host=host, slopes=slopes)
+        w.v_cache[page, 1, key % 16, 9] = keep
+        want, size = reference(w, slopes=slopes)
+        w.v_cache[page, 1, key % 16, 9] = math.inf
+        assert not out[0, 4:, 9].isfinite().any()
+        out[0, 4:, 9] = 0.0
+        want[0, 4:, 9] = 0.0
+        close(out, want, size, BF16_WEIGHTS)
