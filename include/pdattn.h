@@ -38,11 +38,13 @@ extern "C" {
 typedef int pdattn_status;
 #define PDATTN_OK                   0
 #define PDATTN_INVALID_ARG         (-1) /* null pointer, negative size, Hq % Hkv != 0, ...           */
-#define PDATTN_UNSUPPORTED         (-2) /* head_dim not in {64,128}, block_size not in {16,32,64}, G > 16, or a
-                                           cache stride that is not a multiple of 8 elements          */
+#define PDATTN_UNSUPPORTED         (-2) /* head_dim not in {64,128}, block_size not in {16,32,64}, G > 16, a cache
+                                           stride that is not a multiple of 8 elements, or no host memory for the
+                                           plan of this many sequences (text in pdattn_last_cuda_error()) */
 #define PDATTN_WORKSPACE_TOO_SMALL (-3)
 #define PDATTN_MISALIGNED          (-4) /* q / k_cache / v_cache / out not 16-byte aligned, or workspace /
-                                           staging not 256-byte aligned                              */
+                                           staging not 256-byte aligned (4 bytes where only the error
+                                           word is used)                                             */
 #define PDATTN_NOT_BOUND           (-5) /* pdattn_decode() without pdattn_bind() on this thread       */
 #define PDATTN_CUDA_ERROR          (-6) /* a CUDA call failed; text in pdattn_last_cuda_error()       */
 #define PDATTN_BAD_PAGE_INDEX      (-7) /* reported by pdattn_check(): a used block_table entry was

@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <vector>
 
@@ -35,7 +36,7 @@ int g_host_zero_copy = -1;                // pdattn_set_host_zero_copy: -1 defau
 int g_prefix_engine = -1;                 // pdattn_set_prefix_engine: -1 default (tcgen05), 0 warp MMAs, 1 tcgen05
 int g_short_path = -1;                    // pdattn_set_short_piece_path: -1 by batch shape, 0 never, 1 whenever it applies
 constexpr int kAutoShortTilesX2 = 3;      // mode -1: the short-piece kernel below 1.5 tiles per unit on average
-thread_local std::vector<int32_t> g_start_tiles_host;   // scratch of the grouped path (no call parameter lives here)
+thread_local std::vector<int32_t> g_start_tiles_host;   // scratch of the grouped and the scored path (no call parameter lives here)
 
 // What one decode call is, beyond the plain arguments: every entry point fills one of these and hands it to
 // decode_common.
@@ -706,6 +707,17 @@ pdattn_status static_scratch_address(int dev, uint8_t** out) {
 // ---- the one decode path -----------------------------------------------------------------------
 namespace {
 
+// Room for one start tile per sequence; false (with a text) when the host has no memory for it.
+bool start_tiles_room(int num_seqs) {
+  try {
+    g_start_tiles_host.resize(num_seqs);
+  } catch (const std::exception&) {
+    snprintf(cuda_error_text(), kCudaErrorTextBytes, "no host memory for the plan of %d sequences", num_seqs);
+    return false;
+  }
+  return true;
+}
+
 pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_stream_t stream_) {
   g_last_launches = 0;
   if (!a) return PDATTN_INVALID_ARG;
@@ -755,6 +767,15 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
   size_t need = scratch_need(wl, &off_start, &off_pfx);
   if (!cd.static_scratch && a->workspace_bytes < need) return PDATTN_WORKSPACE_TOO_SMALL;
 
+  const int32_t* start_tiles_host = nullptr;
+  if (score && a->context_lens_host && (score->key_begin || score->window > 0)) {
+    if (!start_tiles_room(a->num_seqs)) return PDATTN_UNSUPPORTED;
+    for (int sq = 0; sq < a->num_seqs; ++sq)
+      g_start_tiles_host[sq] =
+          first_key(a->context_lens_host[sq], score->key_begin ? score->key_begin_host[sq] : 0, score->window) / kTileTokens;
+    start_tiles_host = g_start_tiles_host.data();
+  }
+
   int dev = 0;
   DevInfo* di = nullptr;
   s = device_info(&dev, &di);
@@ -782,7 +803,6 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     if (e != cudaSuccess) return cuda_fail("cudaMemsetAsync(static scratch header)", e);
   }
 
-  const int32_t* start_tiles_host = nullptr;
   int n_groups = 0;
   const bool umma = g_prefix_engine != 0 && !fp8;   // which kernel takes the shared tiles of a grouped call
   if (grouped) {
@@ -793,7 +813,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     if (G > 8 || Gs * G > max_rows) return PDATTN_UNSUPPORTED;
     if (!a->context_lens_host || a->num_seqs % Gs != 0) return PDATTN_INVALID_ARG;
     n_groups = a->num_seqs / Gs;
-    g_start_tiles_host.resize(a->num_seqs);
+    if (!start_tiles_room(a->num_seqs)) return PDATTN_UNSUPPORTED;
     for (int sq = 0; sq < a->num_seqs; ++sq) {
       const int pt = cd.prefix_tiles_host[sq / Gs];
       // every member must own at least one token past the shared tiles
@@ -801,14 +821,6 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
       if (static_cast<int64_t>(pt) * kTileTokens / a->block_size > a->max_blocks_per_seq) return PDATTN_INVALID_ARG;
       g_start_tiles_host[sq] = pt;
     }
-    start_tiles_host = g_start_tiles_host.data();
-  }
-
-  if (score && a->context_lens_host && (score->key_begin || score->window > 0)) {
-    g_start_tiles_host.resize(a->num_seqs);
-    for (int sq = 0; sq < a->num_seqs; ++sq)
-      g_start_tiles_host[sq] =
-          first_key(a->context_lens_host[sq], score->key_begin ? score->key_begin_host[sq] : 0, score->window) / kTileTokens;
     start_tiles_host = g_start_tiles_host.data();
   }
 

@@ -284,3 +284,36 @@ def test_the_join_of_cut_prompt_items_stays_within_its_parts_whatever_the_worksp
     with open(os.path.join(pd_build.CSRC, "prefill_umma.cuh")) as f:
         reads = [x for x in f.read().split("P.parts[item]")[1:] if not x.startswith(" = ")]
     assert len(reads) == 1 and reads[0].startswith(", P.splits);")
+
+
+def test_a_scored_step_without_host_memory_for_its_plan_is_refused():
+    """Not an exception through the C boundary, which would end the process.  In a child, whose address space is limited."""
+    import subprocess
+    import sys
+    code = """
+import ctypes, resource, sys
+import numpy as np
+lib = ctypes.CDLL(sys.argv[1])
+sys.path.insert(0, sys.argv[2])
+from paper_2607_09207_b200 import pdattn
+n, P = 1 << 26, 0x10000
+lens = np.ones(n, np.int32)
+a = pdattn.Args()
+for f in ("q", "k_cache", "v_cache", "out", "block_table", "context_lens", "workspace"):
+    setattr(a, f, P)
+a.context_lens_host = lens.ctypes.data
+a.num_seqs, a.num_q_heads, a.num_kv_heads, a.head_dim, a.block_size = n, 4, 2, 64, 16
+a.max_blocks_per_seq, a.num_blocks, a.scale = 4, 12, 0.1
+a.kv_block_stride, a.kv_head_stride, a.kv_token_stride = 2048, 1024, 64
+a.workspace_bytes = 1 << 62
+s = pdattn.ScoreArgs(0.0, None, 5, None, None, None)
+with open("/proc/self/statm") as f:
+    used = int(f.read().split()[0]) * resource.getpagesize()
+resource.setrlimit(resource.RLIMIT_AS, (used + (64 << 20), resource.RLIM_INFINITY))
+print("status", lib.pdattn_decode_scored(ctypes.byref(a), ctypes.byref(s), None))
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code, pd_build.LIB, root], capture_output=True, text=True, timeout=300,
+                         env=dict(os.environ, CUDA_VISIBLE_DEVICES=""))
+    assert "status %d" % pdattn.UNSUPPORTED in out.stdout, out.stdout + out.stderr
