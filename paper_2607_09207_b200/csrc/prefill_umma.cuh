@@ -4,8 +4,8 @@
 //
 // Work.  The query rows of one KV head are packed: row r of a 128-row tile is head r % G of token r / G, so a tile holds
 // floor(128 / G) whole tokens and K/V tiles are read once for all G heads.  An item is (sequence, pair of tiles, KV head); a
-// persistent CTA walks the 128-key tiles that any row of its pair sees and takes the next item from a counter, late
-// (long) ones first.  Sequence s owns the pair slots from cu[s] / (2 tokens-per-tile) + s on: enough of them without a prefix
+// persistent CTA walks the 128-key tiles that any row of its pair sees and takes the next item from a counter, sequences from the
+// last to the first and in each the late (long) pairs first.  Sequence s owns the pair slots from cu[s] / (2 tokens-per-tile) + s on: enough of them without a prefix
 // sum, so the launch needs no host copy of the lengths (slots without tokens are stepped over).
 //
 //   S_t[128, 128 keys]  = Q_t . K^T         both from shared memory               t = 0, 1: the two tiles of the pair
@@ -32,13 +32,14 @@
 // tensor work again).  The reference of the online softmax follows the running maximum only when that grew by more than 2^8,
 // so O is rarely rescaled.
 //
-// Bound: the chain of a tile, about 4000 cycles a pair and key tile against the 2048 that its 32 MMAs take -- scores to weights
-// 2500 (128 exponentials a thread, two warps to a quadrant), weights to the next scores 1300 (barrier, half of P.V, Q.K^T,
-// barrier).  Tried and not faster: two threads a row (16 softmax warps), the scores in registers throughout (the code then
-// outgrows the instruction caches), a share of the exponentials on the FMA pipe, one MMA warp per tile (the tiles fall into step
-// and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 474-510 us, 0.94-1.01 PFLOP/s (the spread is
-// the clock under the power cap); with a cap 682 (1055 where every score lies past it), with a distance bias 625.  Also tried for those two: the bias as packed
-// multiply-adds (no gain), worked out again in the second pass in place of the write-back (+13 %), tanh in unpacked operations (+10 %).
+// Bound: the chain of a tile, about 4000 cycles a pair and key tile (clock stamps of an instrumented build) against the 2048 that
+// its 32 MMAs take -- scores to weights 2500 (128 exponentials a thread, two warps to a quadrant), weights to the next scores
+// 1300 (barrier, half of P.V, Q.K^T, barrier).  Tried and not faster: two threads a row (16 softmax warps), the scores in registers
+// throughout (the code then outgrows the instruction caches), a share of the exponentials on the FMA pipe, one MMA warp per tile
+// (the tiles fall into step and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 445-510 us, 0.94-1.08
+// PFLOP/s (the spread is the clock under the power cap); with a cap 676-700 (1055 where every score lies past it), with a distance
+// bias 630.  Also tried for those two: the bias as packed multiply-adds (no gain), worked out again in the second pass in place
+// of the write-back (+13 %), tanh in unpacked operations (+10 %).
 //
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA thread drains, tensor memory
 // is freed and the CTA returns.
