@@ -43,7 +43,7 @@ pdattn_status launch_prefill_kernel(const CUtensorMap& mq, const CUtensorMap& mk
 
 // Items of a call (pair slots x KV heads), and the parts each may be cut into along the keys: as many as fill PF_UNITS CTAs; up
 // to 2/3 of PF_UNITS items in three parts, two rounds of a third each in place of a whole one (28/4 heads, whole and in three: 16 x
-// 8 tokens over 16,000 keys 232 and 168 us, over 4000 66 and 56, over 1000 24 and 23; 850 tokens without a history 27 and 31).
+// 8 tokens over 16,000 keys 232 and 168 us, over 4000 66 and 56, over 1000 24 and 23; 850 tokens without a history 25 and 28).
 constexpr int PF_UNITS = 148;
 int64_t prefill_items(int num_seqs, int num_tokens, int Hq, int Hkv) {
   return (static_cast<int64_t>(num_tokens) / (2 * (128 / (Hq / Hkv))) + num_seqs) * Hkv;

@@ -37,8 +37,8 @@
 // 1300 (barrier, half of P.V, Q.K^T, barrier).  Tried and not faster: two threads a row (16 softmax warps), the scores in registers
 // throughout (the code then outgrows the instruction caches), a share of the exponentials on the FMA pipe, one MMA warp per tile
 // (the tiles fall into step and their phases no longer overlap).  8191 causal tokens, 28/4 heads of 128: 445-510 us, 0.94-1.08
-// PFLOP/s (the spread is the clock under the power cap); with a cap 676-700 (1055 where every score lies past it), with a distance
-// bias 630.  Also tried for those two: the bias as packed multiply-adds (no gain), worked out again in the second pass in place
+// PFLOP/s (the spread is the clock under the power cap); with a cap 665-690 (1055 where every score lies past it), with a distance
+// bias 615-640.  Also tried for those two: the bias as packed multiply-adds (no gain), worked out again in the second pass in place
 // of the write-back (+13 %), tanh in unpacked operations (+10 %).
 //
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA thread drains, tensor memory
@@ -77,6 +77,7 @@ constexpr int PF_MIN_TILES = 4;  // key tiles of a part, at least
 constexpr int PF_ITEMS = 3;      // items in flight between the warps
 constexpr int PF_AHEAD = 2;      // a CTA draws its next item when the loads of the present one come to its last two key tiles
 constexpr int PF_GUARDS = 2;     // warps that guard V
+constexpr int PF_TAIL = 4;       // key tiles at the end of an item among which each of its two row tiles ends
 constexpr int PF_NTHREADS = 512;
 constexpr int PF_LAUNCH_REGS = 128, PF_SOFTMAX_REGS = 184, PF_OTHER_REGS = 72;   // a thread
 static_assert(256 * PF_SOFTMAX_REGS + 256 * PF_OTHER_REGS <= PF_NTHREADS * PF_LAUNCH_REGS, "register split");
@@ -439,9 +440,12 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       uint64_t* full = isV ? ctrl->v_full : ctrl->k_full;
       bool any_bad = false, ok = true;
       int c = 0, slot = 0, nq[2] = {0, 0};
+      int start = 0, start1 = 0, read = -1;               // first tiles of this item and the one before; items known to be released
       const PrefillItem* ip;
       for (int k = 0; ok && get_item(k, ip); ++k) {
         const PrefillItem& it = *ip;
+        start1 = start;
+        start = c;
         const int32_t* row = P.block_table + static_cast<int64_t>(it.s) * P.MB;
         const int npages = static_cast<int>((static_cast<int64_t>(it.keys) + (1 << P.bs_log2) - 1) >> P.bs_log2);
         auto page_id = [&](int kt) {
@@ -481,10 +485,21 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
           if (id < 0 || id >= P.NB) id = P.NB;            // out-of-bounds coordinate: TMA fills zeros, nothing is read
           // the slot's previous tile: K(c - NK) is done with step c - NK, V(c - NV) with step c - NV + 1
           const int need = isV ? c - NV + 1 : c - NK;
-          if (c >= ring && !__all_sync(0xffffffffu, prefill_wait(smem_u32(&ctrl->step[need & 7]), (need >> 3) & 1, abort_flag))) {
-            ok = false;
-            break;
-          }
+          // V(c) brings a new v_bad[c & 7], and the softmax warps read the old one only after they handed that tile's weights over:
+          // the products do not hold it for them.  Within an item a row tile's next weights do.  That leaves the last key tile of
+          // each of the two; they end at most 2 apart (hi grows by at most one a token, and a pair has at most 256 tokens), so
+          // among the item's last PF_TAIL.  Where c - 8 is one of those, the release of its item says that it was read.  (Items
+          // three back are released, or this one could not have been published.)
+          const int last = c - 8;
+          const int owner = last < start && last >= start - PF_TAIL ? k - 1 : last < start1 && last >= start1 - PF_TAIL ? k - 2 : -1;
+          const bool owed = isV && last >= 0 && owner > read;
+          if (owed) read = owner;
+          // (one copy of the wait: a second one here, or the read of v_bad before the weights go, moves code and costs 1-5 %)
+#pragma unroll 1
+          for (int i = owed ? 0 : c >= ring ? 1 : 2; i < 2 && ok; ++i)
+            ok = __all_sync(0xffffffffu, prefill_wait(smem_u32(i ? &ctrl->step[need & 7] : &ctrl->item_free[owner % PF_ITEMS]),
+                                                      (i ? need >> 3 : owner / PF_ITEMS) & 1, abort_flag));
+          if (!ok) break;
           const uint32_t bar = smem_u32(&full[c & 7]);
           if (lane == 0) {
             if (!isV) ctrl->page_bad[c & 7] = badmask;
@@ -602,30 +617,14 @@ prefill_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ 
       // ================= guards of V: each takes its share of every 64 keys
       const int w = warp - (16 - PF_GUARDS);
       constexpr int WORDS = 4 / PF_GUARDS;                // 32 keys each
-      // A softmax warp reads v_bad of a tile after it has handed the tile's weights over, so the products do not hold the entry for
-      // it.  Within an item its next weights do, and the two tiles end at most 3 key tiles apart (hi grows by at most one a token);
-      // so what may still be unread when tile c comes is the entry of c - 8 where that belongs to an item before this one: its
-      // release says that it was read.  (Items three back are released, or this one could not have been published.  A read
-      // before the weights go would do too, and costs 4 % of 8191 causal tokens.)
       const PrefillItem* ip;
-      int c = 0, slot = 0, start = 0, start1 = 0;         // first tiles of this item and of the one before it
-      int read = -1;                                      // items up to this one are known to be released
+      int c = 0, slot = 0;
       bool ok = true;
       for (int k = 0; ok && get_item(k, ip); ++k) {
         const PrefillItem& it = *ip;
         const int k1 = tiles_to(it);
-        start1 = start;
-        start = c;
         for (int kt = tiles_from(it); kt < k1; ++kt) {
           if (!active(it, 0, kt) && !active(it, 1, kt)) continue;
-          const int owner = c - 8 >= start1 ? k - 1 : k - 2;
-          if (c >= 8 && c - 8 < start && owner > read) {
-            if (!__all_sync(0xffffffffu, prefill_wait(smem_u32(&ctrl->item_free[owner % PF_ITEMS]), (owner / PF_ITEMS) & 1, abort_flag))) {
-              ok = false;
-              break;
-            }
-            read = owner;
-          }
           if (!__all_sync(0xffffffffu, prefill_wait(smem_u32(&ctrl->v_full[c & 7]), (c >> 3) & 1, abort_flag))) {
             ok = false;
             break;
