@@ -198,7 +198,7 @@ def prepare(c, seed):
         return torch.randn(*shape, device="cuda", dtype=BF16, generator=g)
 
     N = int(n.sum())
-    st.lens_host, st.n_max = L.astype(np.int32), int(n.max())
+    st.lens_host, st.n_max, st.N = L.astype(np.int32), int(n.max()), N
     st.cu = _i32(np.concatenate([[0], np.cumsum(n)]))
     if c["op"] != "accept":
         st.table, st.lens = _i32(table), _i32(L)
@@ -448,7 +448,7 @@ def _own(st):
     if c["op"] == "summarize":
         summary = pdattn.PageSummary(st.codes, st.exps)
         pdattn.summarize_append(st.k_cache, summary, st.table, st.lens, cu_tokens=None if st.one else st.cu,
-                                k_scale=st.k_scale if c["fp8"] else None)
+                                num_tokens=st.N, k_scale=st.k_scale if c["fp8"] else None)
         return [st.codes, st.exps]
     if c["op"] == "select":
         pdattn.select_pages(st.q, pdattn.PageSummary(st.codes, st.exps), st.table, st.lens, st.selected, c["bs"], st.ws,
