@@ -272,6 +272,12 @@ pdattn_status pdattn_rope_append(const pdattn_rope_args* args, pdattn_stream_t s
 pdattn_status pdattn_rope_append_fp8(const pdattn_rope_args* args, const float* k_scale, const float* v_scale,
                                      pdattn_stream_t stream);
 
+/* The two calls above with the positions of the rotation given, one per token (DEVICE int32 [num_tokens], any value): a drafted
+ * token of a tree sits at its depth, several tokens at one, while its slot in the cache is its own. */
+pdattn_status pdattn_rope_append_at(const pdattn_rope_args* args, const int32_t* positions, pdattn_stream_t stream);
+pdattn_status pdattn_rope_append_at_fp8(const pdattn_rope_args* args, const int32_t* positions, const float* k_scale,
+                                        const float* v_scale, pdattn_stream_t stream);
+
 /*
  * Modified scores and masks, for pdattn_prefill and pdattn_decode_scored.  Query token at position pos, query head h,
  * key t:
@@ -326,6 +332,118 @@ pdattn_status pdattn_decode_scored_fp8(const pdattn_args* args, const pdattn_sco
                                        const float* v_scale, pdattn_stream_t stream);
 
 /*
+ * Attention for a tree of drafted tokens (speculative decoding inside the rollout of Section 2.1; the paper has no
+ * counterpart).  Sequence s has n_s = cu_tokens[s + 1] - cu_tokens[s] drafted tokens, at most max_tree_tokens <= 64; their K and V are
+ * the last n_s of its context_lens[s] tokens, in the order of the tokens.  Token j of the tree sees every key before the tree and
+ * the tree's token i where bit i of tree_mask[cu_tokens[s] + j] is set (its ancestors and, as a rule, itself; bits at or past
+ * n_s are ignored):
+ *   out[j, h, :] = softmax_t( scale * q[j, h, :] . K[t, h / G, :] ) . V[t, h / G, :]
+ * q, out DEVICE bf16 [num_tokens, num_q_heads, head_dim], dense; cu_tokens DEVICE int32 [num_seqs + 1], ascending from 0;
+ * tree_mask DEVICE uint64 [num_tokens].  Takes no host copies (args->context_lens_host is not read).  Weights of the softmax are
+ * rounded to bf16 (fp16 over the fp8 cache, q there too) for the second product; fp32 otherwise.
+ *   - A token that sees no key gets zeros, as does one before position 0 (n_s > context_lens[s]).
+ *   - What a token does not see never reaches its output, infinities and NaN included (other branches of the tree, slots past
+ *     the end).  What it sees does, as in pdattn_score_args.
+ *   - Bad page ids and contexts longer than their table row: as in pdattn_decode_ex without a host copy of the lengths.
+ *   - A sequence with more than max_tree_tokens tokens is left out, its rows of out as they were, and pdattn_check reports
+ *     PDATTN_UNSUPPORTED.  Rows of out at or past cu_tokens[num_seqs] are left as they were.
+ *   - Requirements: num_seqs <= 65536; args->workspace holds pdattn_tree_workspace_size() bytes; pdattn_workspace_init before its
+ *     first use, and calls that share it must not overlap.  The order of every sum is fixed by lengths and sizes: results are
+ *     bit-identical from run to run and under any renumbering of the pages.
+ */
+pdattn_status pdattn_tree_workspace_size(int num_q_heads, int num_kv_heads, int head_dim, int block_size, int max_tree_tokens,
+                                         size_t* device_bytes);
+pdattn_status pdattn_decode_tree(const pdattn_args* args, const int32_t* cu_tokens, int num_tokens, const uint64_t* tree_mask,
+                                 int max_tree_tokens, pdattn_stream_t stream);
+pdattn_status pdattn_decode_tree_fp8(const pdattn_args* args, const int32_t* cu_tokens, int num_tokens, const uint64_t* tree_mask,
+                                     int max_tree_tokens, const float* k_scale, const float* v_scale, pdattn_stream_t stream);
+
+/*
+ * The accepted path of a tree: K and V of token accepted[s * max_accepted + i] of sequence s's tree are moved to the slot of its
+ * token i, i < accepted_counts[s] (both DEVICE int32; max_accepted <= 64), in the caches of one layer.  Nothing is advanced here: the
+ * lengths still count the whole tree, and when every layer has been served the sequence is shortened to
+ * context_lens[s] - n_s + accepted_counts[s] tokens (pdattn_pages_trim).
+ *   - The path ascends strictly and names tokens of the tree; otherwise (or with a count below 0 or past n_s) the sequence is left
+ *     as it is: PDATTN_BAD_SEQUENCE from pdattn_check.  The same with PDATTN_BAD_PAGE_INDEX where a page that is read or written is
+ *     no page.  Pages that are written must be owned by one sequence only.
+ *   - element_bytes and strides as in pdattn_pages_copy; workspace (may be NULL) as in pdattn_rope_args.
+ */
+pdattn_status pdattn_tree_accept(void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* context_lens,
+                                 const int32_t* cu_tokens, const int32_t* accepted, const int32_t* accepted_counts,
+                                 int max_accepted, int num_seqs, int num_kv_heads, int head_dim, int block_size,
+                                 int max_blocks_per_seq, int num_blocks, int element_bytes, int64_t kv_block_stride,
+                                 int64_t kv_head_stride, int64_t kv_token_stride, void* workspace, pdattn_stream_t stream);
+
+/*
+ * Sparse attention over chosen pages, for long responses (Section 2.3: they dominate the rollout; Appendix A.1.2's beta_hist term
+ * is what it cuts; the paper has no counterpart).  Per step and layer: append, pdattn_summarize_append, pdattn_select_pages,
+ * pdattn_decode_selected.
+ *
+ * Page summary: for every whole page and KV head the channelwise minimum and maximum of its keys, as int8 codes with one power
+ * of two: e is the smallest exponent in -40 .. 40 with max |k| <= 127 * 2^e (40 where there is none; codes then saturate at +-127),
+ *   codes[page][head][0][i] = floor(min_t k[t][i] / 2^e),   codes[page][head][1][i] = ceil(max_t k[t][i] / 2^e),
+ *   exponents[page][head] = e;   a page with a key that is not finite: codes 0, exponent 127.
+ * (fp8 cache: k = k_scale * code, one fp32 product.)  A summary belongs to its page: rows that share the page share it, and a page
+ * that is copied or moved (pdattn_pages_fork copies partial pages only; pdattn_pages_compact moves whole ones) is summarised
+ * again at its new place, with pdattn_summarize_pages over copy_dst.
+ */
+typedef struct {
+  const void* k_cache;              /* DEVICE bf16 with the strides below, or the K pool of pdattn_decode_fp8   */
+  const float* k_scale;             /* DEVICE fp32 [num_kv_heads]; fp8 cache only                     */
+  int8_t* codes;                    /* DEVICE int8 [num_blocks, num_kv_heads, 2, head_dim], 16-byte aligned      */
+  int8_t* exponents;                /* DEVICE int8 [num_blocks, num_kv_heads]                         */
+  int num_kv_heads, head_dim, block_size, num_blocks;
+  int element_bytes;                /* 2: bf16; 1: e4m3 codes (strides ignored)                       */
+  int64_t kv_block_stride, kv_head_stride, kv_token_stride;
+  void* workspace;                  /* DEVICE, may be NULL: its error word, as in pdattn_rope_args     */
+} pdattn_summary_args;
+/* The pages that the last n_s of context_lens[s] tokens filled: page b of the sequence with
+ * context_lens[s] - n_s < (b + 1) * block_size <= context_lens[s].  cu_tokens as in pdattn_rope_append (NULL: one token each). */
+pdattn_status pdattn_summarize_append(const pdattn_summary_args* args, const int32_t* block_table, const int32_t* context_lens,
+                                      const int32_t* cu_tokens, int num_tokens, int num_seqs, int max_blocks_per_seq,
+                                      pdattn_stream_t stream);
+/* The pages of a list (DEVICE int32 [num_pages]; entries below 0 are passed over), all their slots. */
+pdattn_status pdattn_summarize_pages(const pdattn_summary_args* args, const int32_t* pages, int num_pages, pdattn_stream_t stream);
+
+/*
+ * The pages that the current token of every sequence is to see, per KV head: selected[s][head][0 .. num_selected), numbers within the
+ * sequence (page b holds tokens b * block_size ..), ascending, -1 past the last.  With n = ceil(context_lens[s] / block_size) pages, all
+ * of them where n <= num_selected; else the first num_first, the last num_recent >= 1 (the newest page has no summary as a
+ * rule), and of the others those with the largest
+ *   score(b) = max_h 2^(e_h + e_b) sum_i max(c_h[i] lo_b[i], c_h[i] hi_b[i])       h: the query heads of the KV head
+ * with equal scores in ascending order of b.  lo, hi, e_b: the page's summary (exponent 127: the score is infinite); e_h is the smallest
+ * exponent in -40 .. 40 with max |q_h| <= 127 * 2^e_h and c_h = q_h / 2^e_h rounded to nearest even, within +-127.  A head with an
+ * element that is not finite takes no part.  Scores are exact, so the choice depends on nothing but the inputs.
+ *   - A used table entry that is no page: lowest score, error word set.  Tokens past the table row are left out, error word set.
+ */
+typedef struct {
+  const void* q;                    /* DEVICE bf16 [num_seqs, num_q_heads, head_dim], dense           */
+  const int8_t* codes;              /* as in pdattn_summary_args                                      */
+  const int8_t* exponents;
+  const int32_t* block_table;       /* as in pdattn_args                                              */
+  const int32_t* context_lens;
+  int32_t* selected;                /* DEVICE int32 [num_seqs, num_kv_heads, num_selected]            */
+  int num_seqs, num_q_heads, num_kv_heads, head_dim, block_size, max_blocks_per_seq, num_blocks;
+  int num_selected, num_first, num_recent;   /* num_first + num_recent <= num_selected                */
+  void* workspace;                  /* DEVICE, pdattn_select_workspace_size() bytes, 256-byte aligned; pdattn_workspace_init first */
+  size_t workspace_bytes;
+} pdattn_select_args;
+pdattn_status pdattn_select_workspace_size(int num_seqs, int num_kv_heads, int max_blocks_per_seq, size_t* device_bytes);
+pdattn_status pdattn_select_pages(const pdattn_select_args* args, pdattn_stream_t stream);
+
+/*
+ * The decode step of pdattn_decode_ex / pdattn_decode_fp8 in which each KV head of a sequence sees the tokens of its chosen pages only:
+ * selected DEVICE int32 [num_seqs, num_kv_heads, num_selected], page numbers within the sequence, as pdattn_select_pages leaves them.
+ *   - The first min(num_selected, ceil(context_lens[s] / block_size)) entries are read, in any order; an entry below 0 stands for no
+ *     page.  A page that is named twice counts twice.  One that the sequence does not have is left out and the error word set.
+ *   - No visible token: zeros.  Pages that are not chosen, and slots past the end, may hold anything.
+ *   - Workspace, lengths with or without a host copy, bad page ids: as for pdattn_decode_ex.
+ */
+pdattn_status pdattn_decode_selected(const pdattn_args* args, const int32_t* selected, int num_selected, pdattn_stream_t stream);
+pdattn_status pdattn_decode_selected_fp8(const pdattn_args* args, const int32_t* selected, int num_selected, const float* k_scale,
+                                         const float* v_scale, pdattn_stream_t stream);
+
+/*
  * Page bookkeeping on the device, for rollout groups that share their prompt's pages (Section 2.1): which pages of a pool
  * are free and how often each is referenced.  The books are caller-owned device arrays; their state is a function of the
  * references alone: free_list holds the pages without references in descending id (the lowest on top, at index
@@ -371,6 +489,14 @@ pdattn_status pdattn_pages_fork(const pdattn_page_pool* pool, int32_t* block_tab
  */
 pdattn_status pdattn_pages_free(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
                                 const int32_t* seqs, int num_freed, int num_seqs, int max_blocks_per_seq, int block_size,
+                                void* workspace, size_t workspace_bytes, pdattn_stream_t stream);
+/*
+ * Row s is shortened to new_lens[s] tokens (DEVICE int32 [num_seqs]), 0 <= new_lens[s] <= context_lens[s]: the pages behind them give their
+ * reference back and their entries become -1.  Otherwise the row stays as it is: PDATTN_BAD_SEQUENCE.  Entries that are no page, or
+ * one without references: as in pdattn_pages_free.
+ */
+pdattn_status pdattn_pages_trim(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
+                                const int32_t* new_lens, int num_seqs, int max_blocks_per_seq, int block_size,
                                 void* workspace, size_t workspace_bytes, pdattn_stream_t stream);
 /*
  * Makes the referenced pages dense: with n of them, those at or past n move, in ascending order, into the unreferenced
@@ -530,7 +656,8 @@ pdattn_status pdattn_set_prefix_engine(int engine);
  * would call it once per step or less).  Synchronises `stream`, reads and clears the workspace's sticky
  * error word (hence a non-const pointer).  Returns PDATTN_OK, PDATTN_BAD_PAGE_INDEX, PDATTN_DEVICE_TIMEOUT, or
  * PDATTN_UNSUPPORTED when the device-side planner refused a batch of more than 2^30 tiles (with
- * context_lens_host the call itself returns PDATTN_INVALID_ARG for such a batch); that call computed nothing.
+ * context_lens_host the call itself returns PDATTN_INVALID_ARG for such a batch), which then computed nothing, or when
+ * pdattn_decode_tree met a tree of more than max_tree_tokens tokens.
  * workspace: DEVICE.
  */
 pdattn_status pdattn_check(void* workspace, pdattn_stream_t stream);

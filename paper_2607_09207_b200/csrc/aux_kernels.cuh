@@ -312,9 +312,11 @@ __device__ __forceinline__ int block_scan_1024(int v, int* warp_sums, int lane, 
 __global__ void __launch_bounds__(1024)
 plan_kernel(const int32_t* __restrict__ context_lens, const int32_t* __restrict__ start_tiles, int S, int Hkv,
             int n_static, int n_dyn_max, int32_t* __restrict__ prefix, SpanStart* __restrict__ spans, WsHeader* hdr,
-            int with_merge_words, const int32_t* __restrict__ key_begin, int window) {
+            int with_merge_words, const int32_t* __restrict__ key_begin, int window, int selected_tokens) {
   // leading tiles that the plan leaves out: given, or those before the first key that the token sees
   auto skipped = [&](int s, int L) {
+    // chosen pages only: all tiles but as many as their tokens fill
+    if (selected_tokens > 0) return static_cast<int>(seq_tiles(L, seq_tiles(selected_tokens, 0)));
     return start_tiles ? start_tiles[s] : first_key(L, key_begin ? key_begin[s] : 0, window) / TILE;
   };
   __shared__ int warp_sums[32];

@@ -80,6 +80,9 @@ struct DecodeParams {
   int window;                 // 0: none
   float cap2;                 // cap * log2(e); 0: none
   float cap_r;                // 1 / (cap * log2(e)): base-2 scores to multiples of the cap
+  // chosen pages (decode_kernel with SEL): see pdattn_decode_selected
+  const int32_t* selected;    // [S][Hkv][n_selected] pages of the sequence, in its own numbering
+  int n_selected;
   int inkernel_max;         // > 0: a cut unit whose followers all lie within this many spans after its first one is
                             // merged by the CTA that writes its last partial; 0: every cut unit is left to combine_kernel
   SpanStart spans[MAX_PARAM_SPANS + 1];
@@ -291,7 +294,7 @@ struct Ctrl {                 // lives in the CTRL_BYTES area
   uint64_t empty[MAX_STAGES];   // ... and has been consumed
   uint64_t full_v[MAX_STAGES];  // split halves only: the V half, filled and released on its own
   uint64_t empty_v[MAX_STAGES];
-  uint32_t meta[MAX_STAGES];  // per stage: bit j set = page j of the tile had a bad id
+  uint32_t meta[MAX_STAGES];  // per stage: bit j set = page j of the tile had a bad id (SEL: and see sel_meta)
   uint32_t abort;
   int32_t sq_pub;             // number of run-time span ids published so far
   int32_t sq_id[SPAN_QUEUE];  // k-th id (k >= 1) at [(k-1) % SPAN_QUEUE]; -1 = no more spans
@@ -320,12 +323,14 @@ struct Piece {
   int lo;   // MOD only: first key that the token sees
 };
 // MOD: `start` is key_begin (first key per sequence, may be null) and the skipped tiles follow from it and the window.
-template <bool MOD>
+// SEL: BS > 0, and a unit's tokens are those of its chosen pages, counted as whole pages.
+template <bool MOD, int SEL_BS = 0>
 struct WalkerT {
   const int32_t* ctx;
   const int32_t* start;         // start tiles per sequence, may be null (= 0)
   int Hkv, nunits, unit, tb, rem;
   int window = 0;
+  int n_selected = 0;
   int pf_unit = -1, pf_L = 0, pf_t0 = 0;   // the following unit's length and start, loaded one piece early
   __device__ __forceinline__ bool next(Piece& p) {
     while (rem > 0 && unit < nunits) {
@@ -340,7 +345,8 @@ struct WalkerT {
       }
       const int lo = MOD ? first_key(L, st, window) : 0;
       const int t0 = MOD ? lo / TILE : st;
-      const int nt_all = L > 0 ? (L + TILE - 1) / TILE : 0;
+      const int tokens = SEL_BS > 0 ? selected_pages(L, SEL_BS, n_selected) * SEL_BS : L;
+      const int nt_all = tokens > 0 ? (tokens + TILE - 1) / TILE : 0;
       const int nt = nt_all > t0 ? nt_all - t0 : 0;
       if (tb >= nt) {
         ++unit;
@@ -350,7 +356,7 @@ struct WalkerT {
       p.unit = unit;
       p.s = s;
       p.g = unit - s * Hkv;
-      p.L = L;
+      p.L = tokens;
       p.nt = nt;
       p.t0 = t0;
       p.lo = lo;
@@ -382,6 +388,16 @@ __device__ __forceinline__ float tanh_any(float t) {
   const float small = t * fmaf(fmaf(fmaf(fmaf(kTanh[0], u, kTanh[1]), u, kTanh[2]), u, kTanh[3]), u, 1.f);
   return fabsf(t) <= kTanhNear ? small : tanh_far(t);
 }
+
+// SEL: word of a tile of chosen pages.  Bits 0-3: pages to leave out; bits 4-7: pages that hold the sequence's partial last page
+// (its number may stand anywhere in the list, and twice); bits 8-13: tokens of that one.
+__device__ __forceinline__ uint32_t sel_meta(uint32_t dead, uint32_t partial, int tokens) {
+  return dead | (partial << 4) | (static_cast<uint32_t>(tokens) << 8);
+}
+__device__ __forceinline__ bool sel_partial(uint32_t meta) { return (meta & 0xf0u) != 0; }
+// tokens of page j of the tile
+template <int BS>
+__device__ __forceinline__ int sel_tokens(uint32_t meta, int j) { return (meta >> (4 + j)) & 1u ? static_cast<int>(meta >> 8) : BS; }
 
 // Modified scores of one tile on one warp (compute_tile and compute_tile_f8 with MOD).
 template <int NT>

@@ -264,7 +264,7 @@ __device__ __forceinline__ void stage_queries_loop(const DecodeParams& P, Ctrl* 
 // which class of which of those pieces may touch it next.  Warps that hold no tile of a piece skip it
 // (they do not even read its query rows), so up to NCW short pieces are in work at once.
 // ------------------------------------------------------------------------------------------
-template <int D, int NT, int BS, int EB, bool WIN, bool MOD>
+template <int D, int NT, int BS, int EB, bool WIN, bool MOD, bool SEL>
 __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanParams& pp, Ctrl* ctrl, uint32_t ring,
                                               uint32_t qbuf, uint8_t* handoff, int warp, int lane) {
   using C = Cfg<D, NT, BS, EB>;
@@ -393,7 +393,7 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
         const uint32_t badmask = ctrl->meta[slot];
         const int n_left = pc.L - (pc.t0 + t) * TILE;
         if constexpr (MOD) md.head = pc.lo - (pc.t0 + t) * TILE;
-        const bool whole = n_left - (P.T - 1) >= TILE && !(MOD && md.head > 0);   // every query token sees the whole tile
+        const bool whole = n_left - (P.T - 1) >= TILE && !(MOD && md.head > 0) && !(SEL && sel_partial(badmask));   // every query token sees the whole tile
         if constexpr (EB == 2) {
           // split stage halves: the K half goes back to the producers as soon as the scores are computed, and
           // the V half is waited for only when the probabilities are ready
@@ -405,10 +405,10 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
             if (!mbar_wait(smem_u32(&ctrl->full_v[slot]), (its / NST) & 1)) fail();
           };
           if (whole) {
-            compute_tile<D, NT, BS, false, MOD>(sK, sV, qf, acc, m, l, P.scale_log2, MOD ? n_left : TILE, badmask, lane, lag, md,
+            compute_tile<D, NT, BS, false, MOD, SEL>(sK, sV, qf, acc, m, l, P.scale_log2, MOD ? n_left : TILE, badmask, lane, lag, md,
                                                 after_k, before_v);
           } else {
-            compute_tile<D, NT, BS, true, MOD>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, md, after_k,
+            compute_tile<D, NT, BS, true, MOD, SEL>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, md, after_k,
                                                before_v);
             fence_proxy_async();   // our zero-fill stores must be ordered before the next TMA write
           }
@@ -418,9 +418,9 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
           continue;
         } else {
           if (whole) {
-            compute_tile_f8<D, NT, BS, false, MOD>(sK, sV, qf, acc, m, l, sl2, MOD ? n_left : TILE, badmask, lane, lag, md);
+            compute_tile_f8<D, NT, BS, false, MOD, SEL>(sK, sV, qf, acc, m, l, sl2, MOD ? n_left : TILE, badmask, lane, lag, md);
           } else {
-            compute_tile_f8<D, NT, BS, true, MOD>(sK, sV, qf, acc, m, l, sl2, n_left, badmask, lane, lag, md);
+            compute_tile_f8<D, NT, BS, true, MOD, SEL>(sK, sV, qf, acc, m, l, sl2, n_left, badmask, lane, lag, md);
           }
         }
         __syncwarp();
@@ -654,8 +654,8 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
         }
       }
     } else {
-      WalkerT<MOD> walk{P.context_lens, MOD ? P.key_begin : P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile, sp_end - sp.flat,
-                        P.window};
+      WalkerT<MOD, SEL ? BS : 0> walk{P.context_lens, MOD ? P.key_begin : P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile,
+                                      sp_end - sp.flat, P.window, P.n_selected};
       Piece pc;
       while (walk.next(pc)) {
         const int n_piece = pc.te - pc.tb;
@@ -702,13 +702,16 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
 // WIN: the instantiation for batches of mostly one-tile pieces (chained merge, 8-row tiles, no in-kernel merge):
 // every warp walks the spans 32 units at a time (WindowWalker) and the tenth warp stages the query rows.
 // MOD: modified scores and a first key per sequence (pdattn_decode_scored; chained merge, one query token).
-template <int D, int NT, int BS, bool PROBE = false, bool CHAIN = false, int EB = 2, bool WIN = false, bool MOD = false>
+// SEL: every unit has a list of its sequence's pages and sees those only (pdattn_decode_selected; chained merge, one query token).
+template <int D, int NT, int BS, bool PROBE = false, bool CHAIN = false, int EB = 2, bool WIN = false, bool MOD = false,
+          bool SEL = false>
 __global__ void __launch_bounds__(Cfg<D, NT, BS, EB>::NTHREADS, 1)
 decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
               const __grid_constant__ DecodeParams P) {
   using C = Cfg<D, NT, BS, EB>;
   static_assert(EB == 2 || CHAIN, "the fp8 cache path uses the chained merge");
   static_assert(!MOD || (CHAIN && !PROBE && !WIN), "modified scores use the chained merge");
+  static_assert(!SEL || (CHAIN && !PROBE && !WIN && !MOD), "chosen pages use the chained merge");
   constexpr int NST = C::NSTAGES;
   constexpr int NCW = C::NCW;
   constexpr int NCT = C::NCT;
@@ -804,19 +807,34 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         // A context length beyond what the table row can describe: the entries past the row's end are not
         // read (they belong to the next row, or lie past the allocation); their tokens count as a bad page.
         const int nread = min(npages, P.MB);
-        auto page_id = [&](int idx) {
+        // SEL: the list names pages of the sequence; an entry below zero is left out silently (kSkipped)
+        constexpr int kSkipped = -2;
+        const int32_t* list = SEL ? P.selected + static_cast<int64_t>(pc.unit) * P.n_selected : nullptr;
+        const int ctx = SEL ? __ldg(P.context_lens + pc.s) : 0;
+        const int whole_pages = ctx / BS, all_pages = whole_pages + (ctx % BS != 0);
+        bool part_cur = false, part_nxt = false;       // SEL: this lane's page is the partial one
+        auto page_id = [&](int idx, bool& part) {
           int id = idx < npages ? -1 : 0;
-          if (idx < nread) id = __ldg(row + idx);
+          if constexpr (SEL) {
+            const int b = idx < npages ? __ldg(list + idx) : 0;
+            part = idx < npages && b == whole_pages && all_pages > whole_pages;
+            if (idx < npages && b < 0) id = kSkipped;
+            if (idx < npages && b >= 0 && b < all_pages && b < P.MB) id = __ldg(row + b);
+            if (id == kSkipped && b >= 0) id = -1;     // (a table entry of that value is a bad page)
+          } else {
+            if (idx < nread) id = __ldg(row + idx);
+          }
           return id;
         };
-        int ids_cur = page_id(pbase + lane);
-        int ids_nxt = page_id(pbase + IDS_PER_BATCH + lane);
+        int ids_cur = page_id(pbase + lane, part_cur);
+        int ids_nxt = page_id(pbase + IDS_PER_BATCH + lane, part_nxt);
         for (int t = pc.tb; t < pc.te; ++t, ++it) {
           const int rel = t - pc.tb;
           const int kb = rel % TILES_PER_BATCH;
           if (kb == 0 && rel != 0) {
             ids_cur = ids_nxt;
-            ids_nxt = page_id(pbase + rel * C::PAGES + IDS_PER_BATCH + lane);
+            part_cur = part_nxt;
+            ids_nxt = page_id(pbase + rel * C::PAGES + IDS_PER_BATCH + lane, part_nxt);
           }
           maybe_draw(it);
           if (C::NPW > 1 && it % C::NPW != pw) continue;
@@ -843,7 +861,12 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           const int j = lane % C::PAGES;
           int id = __shfl_sync(0xffffffffu, ids_cur, kb * C::PAGES + j);
           const bool bad = (lane < C::PAGES) && (j < np) && (id < 0 || id >= P.NB);
-          const uint32_t badmask = __ballot_sync(0xffffffffu, bad);
+          uint32_t badmask = __ballot_sync(0xffffffffu, bad);
+          const bool report = SEL ? __any_sync(0xffffffffu, bad && id != kSkipped) : badmask != 0;
+          if constexpr (SEL) {
+            const bool part = __shfl_sync(0xffffffffu, static_cast<int>(part_cur), kb * C::PAGES + j) != 0;
+            badmask = sel_meta(badmask, __ballot_sync(0xffffffffu, lane < C::PAGES && j < np && part), ctx % BS);
+          }
           if (id < 0 || id >= P.NB) id = P.NB;   // out-of-bounds coordinate: TMA fills zeros, nothing is read
           if constexpr (SPLIT) {
             // K half and V half of the stage under their own barriers: the consumers hand the K half back
@@ -895,7 +918,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
             }
           }
           }
-          any_bad |= (badmask != 0);
+          any_bad |= report;
           if (NST % C::NPW != 0) {
             __syncwarp();
             if (lane == 0) st_release_shared(&ctrl->prod_last[pw], it);
@@ -932,8 +955,8 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
           it = it_end;
         }
       } else {
-        WalkerT<MOD> walk{P.context_lens, MOD ? P.key_begin : P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile, sp_end - sp.flat,
-                          P.window};
+        WalkerT<MOD, SEL ? BS : 0> walk{P.context_lens, MOD ? P.key_begin : P.start_tiles, P.Hkv, nunits, sp.unit, sp.tile,
+                                        sp_end - sp.flat, P.window, P.n_selected};
         Piece pc;
         while (!aborted && walk.next(pc)) {
           if (!PROBE && pw == 0) {
@@ -1003,7 +1026,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
   const int qcol = (lane & 3) * 2;
 
   if constexpr (CHAIN) {
-    consume_chain<D, NT, BS, EB, WIN, MOD>(P, pp, ctrl, ring, qbuf,
+    consume_chain<D, NT, BS, EB, WIN, MOD, SEL>(P, pp, ctrl, ring, qbuf,
                              smem + NST * C::STAGE_BYTES + C::QSLOTS * C::Q_BYTES + C::ML_BYTES + C::CTRL_BYTES, warp,
                              lane);
     return;
@@ -1101,9 +1124,9 @@ decode_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         if (PROBE) {
           // ceiling probe: no math
         } else if (n_left - (P.T - 1) >= TILE) {   // every query token sees the whole tile
-          compute_tile<D, NT, BS, false, false>(sK, sV, qf, acc, m, l, P.scale_log2, TILE, badmask, lane, lag, TileMod<NT>{}, [] {}, [] {});
+          compute_tile<D, NT, BS, false, false, false>(sK, sV, qf, acc, m, l, P.scale_log2, TILE, badmask, lane, lag, TileMod<NT>{}, [] {}, [] {});
         } else {
-          compute_tile<D, NT, BS, true, false>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, TileMod<NT>{}, [] {}, [] {});
+          compute_tile<D, NT, BS, true, false, false>(sK, sV, qf, acc, m, l, P.scale_log2, n_left, badmask, lane, lag, TileMod<NT>{}, [] {}, [] {});
           fence_proxy_async();   // our zero-fill stores must be ordered before the next TMA write
         }
         __syncwarp();

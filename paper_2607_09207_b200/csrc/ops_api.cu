@@ -13,8 +13,8 @@ using namespace pdattn;
 bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 
 // ---- rotary positions with the append ------------------------------------------------------------
-pdattn_status rope_common(const pdattn_rope_args* a, bool fp8, const float* k_scale, const float* v_scale,
-                          pdattn_stream_t stream) {
+pdattn_status rope_common(const pdattn_rope_args* a, const int32_t* positions, bool fp8, const float* k_scale,
+                          const float* v_scale, pdattn_stream_t stream) {
   if (!a) return PDATTN_INVALID_ARG;
   if (a->num_tokens < 0 || a->num_seqs < 0 || a->num_q_heads < 0 || a->num_kv_heads <= 0) return PDATTN_INVALID_ARG;
   if (a->head_dim != 64 && a->head_dim != 128) return PDATTN_UNSUPPORTED;
@@ -59,6 +59,7 @@ pdattn_status rope_common(const pdattn_rope_args* a, bool fp8, const float* k_sc
   P.block_table = a->block_table;
   P.context_lens = a->context_lens;
   P.cu_tokens = a->cu_tokens;
+  P.positions = positions;
   P.inv_freq = a->inv_freq;
   P.k_scale = k_scale;
   P.v_scale = v_scale;
@@ -133,11 +134,20 @@ pdattn_status pages_check(const pdattn_page_pool* pool, const void* table, const
 extern "C" {
 
 pdattn_status pdattn_rope_append(const pdattn_rope_args* args, pdattn_stream_t stream) {
-  return rope_common(args, false, nullptr, nullptr, stream);
+  return rope_common(args, nullptr, false, nullptr, nullptr, stream);
 }
 pdattn_status pdattn_rope_append_fp8(const pdattn_rope_args* args, const float* k_scale, const float* v_scale,
                                      pdattn_stream_t stream) {
-  return rope_common(args, true, k_scale, v_scale, stream);
+  return rope_common(args, nullptr, true, k_scale, v_scale, stream);
+}
+pdattn_status pdattn_rope_append_at(const pdattn_rope_args* args, const int32_t* positions, pdattn_stream_t stream) {
+  if (!positions) return PDATTN_INVALID_ARG;
+  return rope_common(args, positions, false, nullptr, nullptr, stream);
+}
+pdattn_status pdattn_rope_append_at_fp8(const pdattn_rope_args* args, const int32_t* positions, const float* k_scale,
+                                        const float* v_scale, pdattn_stream_t stream) {
+  if (!positions) return PDATTN_INVALID_ARG;
+  return rope_common(args, positions, true, k_scale, v_scale, stream);
 }
 
 pdattn_status pdattn_pages_workspace_size(int num_blocks, int num_seqs, size_t* device_bytes) {
@@ -207,6 +217,26 @@ pdattn_status pdattn_pages_free(const pdattn_page_pool* pool, int32_t* block_tab
   cudaError_t e = launch_dependent(pages_free_kernel, num_freed, 128, 0, st, true, p, block_table, context_lens, seqs, num_seqs,
                                    max_blocks_per_seq, block_size, x.err);
   if (e != cudaSuccess) return cuda_fail("pages_free_kernel launch", e);
+  e = launch_dependent(pages_books_kernel<false>, kPagesCluster, kPagesThreads, 0, st, true, p, static_cast<int32_t*>(nullptr),
+                       static_cast<int32_t*>(nullptr), 0, x);
+  if (e != cudaSuccess) return cuda_fail("pages_books_kernel launch", e);
+  return PDATTN_OK;
+}
+
+pdattn_status pdattn_pages_trim(const pdattn_page_pool* pool, int32_t* block_table, int32_t* context_lens,
+                                const int32_t* new_lens, int num_seqs, int max_blocks_per_seq, int block_size,
+                                void* workspace, size_t workspace_bytes, pdattn_stream_t stream) {
+  PagePool p;
+  PagesScratch x;
+  const pdattn_status s = pages_check(pool, block_table, context_lens, num_seqs, max_blocks_per_seq, block_size, workspace,
+                                      workspace_bytes, &p, &x);
+  if (s != PDATTN_OK) return s;
+  if (num_seqs == 0) return PDATTN_OK;
+  if (!new_lens) return PDATTN_INVALID_ARG;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e = launch_dependent(pages_trim_kernel, num_seqs, 128, 0, st, true, p, block_table, context_lens, new_lens,
+                                   max_blocks_per_seq, block_size, x.err);
+  if (e != cudaSuccess) return cuda_fail("pages_trim_kernel launch", e);
   e = launch_dependent(pages_books_kernel<false>, kPagesCluster, kPagesThreads, 0, st, true, p, static_cast<int32_t*>(nullptr),
                        static_cast<int32_t*>(nullptr), 0, x);
   if (e != cudaSuccess) return cuda_fail("pages_books_kernel launch", e);

@@ -308,6 +308,36 @@ pages_free_kernel(PagePool pool, int32_t* __restrict__ table, int32_t* __restric
 }
 
 // ------------------------------------------------------------------------------------------
+// Trim, first part: block s shortens row s to new_lens[s] tokens and takes back the references of the pages behind them.
+// ------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(128)
+pages_trim_kernel(PagePool pool, int32_t* __restrict__ table, int32_t* __restrict__ lens,
+                  const int32_t* __restrict__ new_lens, int MB, int bs, int32_t* err) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int s = blockIdx.x, L = lens[s], n = new_lens[s];
+  if (n < 0 || n > L) {
+    if (threadIdx.x == 0) atomicOr(err, ERR_BAD_SEQUENCE);
+    return;
+  }
+  const int64_t had = (static_cast<int64_t>(L) + bs - 1) / bs, keep = (static_cast<int64_t>(n) + bs - 1) / bs;
+  if (had > MB && threadIdx.x == 0) atomicOr(err, ERR_BAD_SEQUENCE);
+  const int b1 = static_cast<int>(had < MB ? had : MB);
+  int32_t* row = table + static_cast<int64_t>(s) * MB;
+  for (int64_t b = keep + threadIdx.x; b < b1; b += blockDim.x) {
+    const int id = row[b];
+    bool good = id >= 0 && id < pool.NB;
+    if (good && atomicSub(pool.ref + id, 1) <= 0) {   // a page without references: the books do not match the table
+      atomicAdd(pool.ref + id, 1);
+      good = false;
+    }
+    if (!good) atomicOr(err, ERR_BAD_PAGE);
+    row[b] = -1;
+  }
+  __syncthreads();                                    // (every thread has read the length)
+  if (threadIdx.x == 0) lens[s] = n;
+}
+
+// ------------------------------------------------------------------------------------------
 // One pass over the reference counts by a cluster of blocks: the free list of the present counts (COMPACT = false),
 // or the moves that make the live pages dense and the books after them (COMPACT = true).  Block r of the cluster owns
 // a contiguous range of pages; the ranges' live counts are exchanged through distributed shared memory.

@@ -150,6 +150,12 @@ PDATTN_HD inline int first_key(int context_len, int key_begin, int window) {
   return lo;
 }
 
+// Entries of a row of pdattn_decode_selected's list that are read: a sequence has no more pages to choose from.
+PDATTN_HD inline int selected_pages(int context_len, int block_size, int num_selected) {
+  const int pages = context_len > 0 ? (context_len - 1) / block_size + 1 : 0;
+  return pages < num_selected ? pages : num_selected;
+}
+
 // Parts of an item of pdattn_prefill that were written, from the word its CTAs left in the workspace.  When a call's bounded waits
 // run out, units may never be drawn and the word is whatever the memory held: it must not lead past the parts' room.
 PDATTN_HD inline int join_parts(int word, int splits) { return word < 0 ? 0 : word < splits ? word : splits; }

@@ -36,7 +36,7 @@ int g_host_zero_copy = -1;                // pdattn_set_host_zero_copy: -1 defau
 int g_prefix_engine = -1;                 // pdattn_set_prefix_engine: -1 default (tcgen05), 0 warp MMAs, 1 tcgen05
 int g_short_path = -1;                    // pdattn_set_short_piece_path: -1 by batch shape, 0 never, 1 whenever it applies
 constexpr int kAutoShortTilesX2 = 3;      // mode -1: the short-piece kernel below 1.5 tiles per unit on average
-thread_local std::vector<int32_t> g_start_tiles_host;   // scratch of the grouped and the scored path (no call parameter lives here)
+thread_local std::vector<int32_t> g_start_tiles_host;   // scratch of the grouped, the scored and the chosen-pages path (no call parameter lives here)
 
 // What one decode call is, beyond the plain arguments: every entry point fills one of these and hands it to
 // decode_common.
@@ -50,6 +50,8 @@ struct CallDesc {
   const int32_t* prefix_tiles = nullptr;        //   device copy
   const int32_t* prefix_tiles_host = nullptr;   //   host copy
   const pdattn_score_args* score = nullptr;     // pdattn_decode_scored: modified scores and masks
+  const int32_t* selected = nullptr;            // pdattn_decode_selected: chosen pages per sequence and KV head
+  int n_selected = 0;
   bool static_scratch = false;                  // pdattn_decode_static_scratch: scratch is the built-in array
   int32_t* status_out = nullptr;                //   device word that receives the error word after the call
 };
@@ -59,6 +61,7 @@ struct LaunchCtx {
   int block_size;
   bool chain, probe, fp8;
   bool scored;              // modified scores and masks
+  bool selected;            // chosen pages
   bool win;                 // the short-piece instantiation of the chained-merge kernel (8-row tiles, bf16 cache)
   DevInfo* di;
   cudaStream_t stream;
@@ -121,6 +124,9 @@ pdattn_status launch_bs(const CUtensorMap& mk, const CUtensorMap& mv, const Deco
   if (g_prof_start) cudaEventRecord(g_prof_start, stream);
   if (lc.scored) {
     const pdattn_status ss = launch_scored_decode(mk, mv, P, D, BS, NT == 2, lc.fp8, grid, stream, dependent);
+    if (ss != PDATTN_OK) return ss;
+  } else if (lc.selected) {
+    const pdattn_status ss = launch_selected_decode(mk, mv, P, D, BS, NT == 2, lc.fp8, grid, stream, dependent);
     if (ss != PDATTN_OK) return ss;
   } else if (lc.fp8) {
     using C8 = Cfg<D, NT, BS, 1>;
@@ -651,6 +657,32 @@ pdattn_status pdattn_decode_scored_fp8(const pdattn_args* args, const pdattn_sco
   return decode_common(&a, cd, stream);
 }
 
+pdattn_status pdattn_decode_selected(const pdattn_args* args, const int32_t* selected, int num_selected,
+                                     pdattn_stream_t stream) {
+  if (!args || !selected) return PDATTN_INVALID_ARG;
+  CallDesc cd;
+  cd.selected = selected;
+  cd.n_selected = num_selected;
+  return decode_common(args, cd, stream);
+}
+
+pdattn_status pdattn_decode_selected_fp8(const pdattn_args* args, const int32_t* selected, int num_selected,
+                                         const float* k_scale, const float* v_scale, pdattn_stream_t stream) {
+  if (!args || !selected || !k_scale || !v_scale) return PDATTN_INVALID_ARG;
+  pdattn_args a = *args;
+  // dense pools of one-byte codes; the stride fields are not used by this variant
+  a.kv_token_stride = a.head_dim;
+  a.kv_head_stride = static_cast<int64_t>(a.block_size) * a.head_dim;
+  a.kv_block_stride = static_cast<int64_t>(a.num_kv_heads) * a.block_size * a.head_dim;
+  CallDesc cd;
+  cd.selected = selected;
+  cd.n_selected = num_selected;
+  cd.fp8 = true;
+  cd.k_scale = k_scale;
+  cd.v_scale = v_scale;
+  return decode_common(&a, cd, stream);
+}
+
 pdattn_status pdattn_check(void* workspace, pdattn_stream_t stream_) {
   if (!workspace) return PDATTN_INVALID_ARG;
   cudaStream_t stream = reinterpret_cast<cudaStream_t>(stream_);
@@ -746,6 +778,8 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     if (!valid_cap(score->logit_cap) || score->window < 0) return PDATTN_INVALID_ARG;
     if (a->context_lens_host && score->key_begin && !score->key_begin_host) return PDATTN_INVALID_ARG;
   }
+  if (cd.selected && (cd.n_selected < 1 || static_cast<int64_t>(cd.n_selected) * a->block_size > INT32_MAX - kTileTokens))
+    return PDATTN_INVALID_ARG;
   // a context longer than its block_table row can describe is refused here when the host knows the lengths;
   // without a host copy the kernel treats the tokens past the row as a bad page
   if (a->context_lens_host) {
@@ -773,6 +807,13 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
     for (int sq = 0; sq < a->num_seqs; ++sq)
       g_start_tiles_host[sq] =
           first_key(a->context_lens_host[sq], score->key_begin ? score->key_begin_host[sq] : 0, score->window) / kTileTokens;
+    start_tiles_host = g_start_tiles_host.data();
+  }
+  if (cd.selected && a->context_lens_host) {
+    // the plan covers as many tiles as the chosen pages fill
+    if (!start_tiles_room(a->num_seqs)) return PDATTN_UNSUPPORTED;
+    const int64_t most = seq_tiles(static_cast<int64_t>(cd.n_selected) * a->block_size, 0);
+    for (int sq = 0; sq < a->num_seqs; ++sq) g_start_tiles_host[sq] = static_cast<int32_t>(seq_tiles(a->context_lens_host[sq], most));
     start_tiles_host = g_start_tiles_host.data();
   }
 
@@ -857,6 +898,8 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
       P.cap_r = 1.f / P.cap2;
     }
   }
+  P.selected = cd.selected;
+  P.n_selected = cd.n_selected;
   P.tickets = reinterpret_cast<int32_t*>(ws + WS_TICKETS_OFFSET);
   // the final merge of cut units: inside the decode kernel with the chained merge (modes -1 and 1) and 8-row
   // tiles, in combine_kernel alone with the barrier merge (0), with 16-row tiles or when asked for (2)
@@ -889,7 +932,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
       P.inkernel_max = 0;
     // Batches of mostly one-tile pieces (below 1.5 tiles per unit on average) take the short-piece instantiation:
     // every warp walks the spans 32 units at a time and the tenth warp stages the query rows instead of merging.
-    if (chain && !fp8 && !cd.probe && !score && G * T <= 8 &&
+    if (chain && !fp8 && !cd.probe && !score && !cd.selected && G * T <= 8 &&
         (g_short_path == 1 ||
          (g_short_path == -1 && 2 * static_cast<int64_t>(P.plan.total) <
                                     static_cast<int64_t>(kAutoShortTilesX2) * a->num_seqs * a->num_kv_heads))) {
@@ -912,7 +955,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
                                      static_cast<const int32_t*>(nullptr), a->num_seqs, a->num_kv_heads, n_ctas, n_dyn_max,
                                      reinterpret_cast<int32_t*>(ws + wl.prefix),
                                      reinterpret_cast<SpanStart*>(ws + wl.spans), P.hdr, P.inkernel_max > 0 ? 1 : 0,
-                                     P.key_begin, P.window);
+                                     P.key_begin, P.window, cd.selected ? cd.n_selected * a->block_size : 0);
     if (e != cudaSuccess) return cuda_fail("plan_kernel launch", e);
     g_last_launches += 1;
     combine_grid = n_ctas + n_dyn_max;
@@ -936,7 +979,7 @@ pdattn_status decode_common(const pdattn_args* a, const CallDesc& cd, pdattn_str
                a->kv_head_stride, a->kv_token_stride, fp8 ? kMapV8 : rank, &mv);
   if (s != PDATTN_OK) return s;
   P.box5d = rank == 5;
-  const LaunchCtx lc{a->block_size, chain, cd.probe, fp8, score != nullptr, win, di, stream};
+  const LaunchCtx lc{a->block_size, chain, cd.probe, fp8, score != nullptr, cd.selected != nullptr, win, di, stream};
 
   if (grouped) {
     // shared prompt tiles first: one pass per (group, kv head) for the query rows of all samples

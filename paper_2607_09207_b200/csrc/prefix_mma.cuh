@@ -184,9 +184,9 @@ prefix_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
       if (has_rows) {
         const uint32_t sK = ring + slot * C::STAGE_BYTES;
         if constexpr (EB == 2)
-          compute_tile<D, 1, BS, false, false>(sK, sK + C::KV_BYTES, qf, acc, m, l, sl2, TILE, ctrl->meta[slot], lane, no_lag, TileMod<1>{}, [] {}, [] {});
+          compute_tile<D, 1, BS, false, false, false>(sK, sK + C::KV_BYTES, qf, acc, m, l, sl2, TILE, ctrl->meta[slot], lane, no_lag, TileMod<1>{}, [] {}, [] {});
         else
-          compute_tile_f8<D, 1, BS, false, false>(sK, sK + C::KV_BYTES, qf, acc, m, l, sl2, TILE, ctrl->meta[slot], lane, no_lag, TileMod<1>{});
+          compute_tile_f8<D, 1, BS, false, false, false>(sK, sK + C::KV_BYTES, qf, acc, m, l, sl2, TILE, ctrl->meta[slot], lane, no_lag, TileMod<1>{});
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctrl->empty[slot]));

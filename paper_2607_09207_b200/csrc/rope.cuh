@@ -29,6 +29,7 @@ struct RopeParams {
   __nv_bfloat16* q_out;
   void *k_cache, *v_cache;
   const int32_t *block_table, *context_lens, *cu_tokens;   // cu_tokens null: token t belongs to sequence t
+  const int32_t* positions;            // of the rotation, per token; null: the token's place in its sequence
   const float *inv_freq, *k_scale, *v_scale;
   int64_t q_ts, k_ts, v_ts;            // token strides of q, k_new, v_new (elements)
   int64_t sb, sh, st;                  // cache strides (elements)
@@ -59,7 +60,8 @@ __global__ void __launch_bounds__(kRopeThreads, 3)
 rope_append_kernel(const __grid_constant__ RopeParams P) {
   constexpr int TPR = D / 16;          // threads per row: two 16-byte chunks each
   __shared__ float2 cs[kRopeMaxTokens][D / 2];
-  __shared__ int4 info[kRopeMaxTokens];   // (position or -1: no such token, page or -1: not written, slot, q: 1 rotate, 0 zeros)
+  __shared__ int4 info[kRopeMaxTokens];   // (0, or -1: no such token; page or -1: not written; slot; q: 1 rotate, 0 zeros)
+  __shared__ int turn_at[kRopeMaxTokens]; // position of the rotation
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int t0 = blockIdx.x * P.tokens_per_block;
   const int nt = min(P.tokens_per_block, P.N - t0);
@@ -69,12 +71,13 @@ rope_append_kernel(const __grid_constant__ RopeParams P) {
     const int s = P.cu_tokens ? find_sequence(P.cu_tokens, P.S, t, lane) : t;
     if (lane == 0) {
       int4 v = make_int4(-1, -1, 0, 0);
+      int at = 0;
       if (s >= 0) {
         const int after = P.cu_tokens ? __ldg(P.cu_tokens + s + 1) - t : 1;   // new tokens from this one on
         const int pos = __ldg(P.context_lens + s) - after;
         v.x = 0;
         if (pos >= 0) {
-          v.x = pos;
+          at = P.positions ? __ldg(P.positions + t) : pos;
           v.w = 1;
           v.z = pos % P.bs;
           const int b = pos / P.bs;
@@ -84,13 +87,14 @@ rope_append_kernel(const __grid_constant__ RopeParams P) {
         }
       }
       info[warp] = v;
+      turn_at[warp] = at;
     }
   }
   __syncthreads();
   const int half = P.R / 2;
   for (int i = tid; i < nt * half; i += kRopeThreads) {
     const int k = i / half, j = i - k * half;
-    double turn = static_cast<double>(info[k].x) * static_cast<double>(__ldg(P.inv_freq + j)) * 0.15915494309189535;
+    double turn = static_cast<double>(turn_at[k]) * static_cast<double>(__ldg(P.inv_freq + j)) * 0.15915494309189535;
     turn -= rint(turn);
     float sn, cn;
     sincospif(static_cast<float>(2.0 * turn), &sn, &cn);

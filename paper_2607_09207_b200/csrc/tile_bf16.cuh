@@ -11,7 +11,8 @@ namespace pdattn {
 // after_k() is called right after the last read of the K tile, before_v() right before the first access to the V
 // tile (with split stage halves the caller releases K in the one and waits for V in the other).
 // MOD: modified scores and a first token (TileMod); its masked instantiation (TAIL) also masks the tokens before that one.
-template <int D, int NT, int BS, bool TAIL, bool MOD, class AfterK, class BeforeV>
+// SEL: `badmask` is a sel_meta word; the masked instantiation also masks the slots past the end of a partial page.
+template <int D, int NT, int BS, bool TAIL, bool MOD, bool SEL, class AfterK, class BeforeV>
 __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uint32_t (&qf)[NT][D / 16][2],
                                              float (&acc)[NT][D / 16][4], float (&m)[NT][2], float (&l)[NT][2],
                                              float sl2, int n_left, uint32_t badmask, int lane,
@@ -63,6 +64,7 @@ __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uin
   for (int j = 0; j < GROUPS; ++j) {
     bool dead_page = false;
     if (badmask) dead_page = (badmask >> ((j * 16) / BS)) & 1u;
+    const int in_page = SEL && TAIL ? sel_tokens<BS>(badmask, (j * 16) / BS) : BS;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -76,6 +78,7 @@ __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uin
           const int tok = j * 16 + trow + ((r & 2) ? 8 : 0);
           if (tok >= n_left - lag[nt][r & 1]) v = NEG_INF;
           if (MOD && tok < md.head) v = NEG_INF;
+          if (SEL && tok % BS >= in_page) v = NEG_INF;
         }
         if (dead_page) v = NEG_INF;
         sc[j][nt][r] = v;
@@ -160,6 +163,17 @@ __device__ __forceinline__ void compute_tile(uint32_t sK, uint32_t sV, const uin
         const int page = tok / BS, row = tok % BS;
         const uint32_t a = sV + page * C::PAGE_BYTES + (ch >> 3) * C::HALF_BYTES + row * 128 + ((ch & 7) << 4);
         asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+      }
+    }
+    if constexpr (SEL) {     // and the slots behind a partial page
+#pragma unroll 1
+      for (int page = 0; page < C::PAGES; ++page) {
+        const int from = sel_tokens<BS>(badmask, page);
+        for (int idx = lane; idx < (BS - from) * (D / 8); idx += 32) {
+          const int row = from + idx / (D / 8), ch = idx % (D / 8);
+          const uint32_t a = sV + page * C::PAGE_BYTES + (ch >> 3) * C::HALF_BYTES + row * 128 + ((ch & 7) << 4);
+          asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+        }
       }
     }
     __syncwarp();

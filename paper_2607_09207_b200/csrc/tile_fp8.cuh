@@ -22,7 +22,7 @@ namespace pdattn {
 // the score MMA holds token pi(rho) of its 16-token group -- a matter of the row addresses handed to
 // ldmatrix for K.
 // ------------------------------------------------------------------------------------------
-template <int D, int NT, int BS, bool TAIL, bool MOD>
+template <int D, int NT, int BS, bool TAIL, bool MOD, bool SEL>
 __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const uint32_t (&qf)[NT][D / 16][2],
                                                 float (&acc)[NT][D / 16][4], float (&m)[NT][2], float (&l)[NT][2],
                                                 float sl2, int n_left, uint32_t badmask, int lane,
@@ -75,6 +75,7 @@ __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const 
   for (int j = 0; j < GROUPS; ++j) {
     bool dead_page = false;
     if (badmask) dead_page = (badmask >> ((j * 16) / BS)) & 1u;
+    const int in_page = SEL && TAIL ? sel_tokens<BS>(badmask, (j * 16) / BS) : BS;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -86,6 +87,7 @@ __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const 
           const int tok = j * 16 + tok0 + ((r & 2) ? 2 : 0);
           if (tok >= n_left - lag[nt][r & 1]) v = NEG_INF;
           if (MOD && tok < md.head) v = NEG_INF;
+          if (SEL && tok % BS >= in_page) v = NEG_INF;
         }
         if (dead_page) v = NEG_INF;
         sc[j][nt][r] = v;
@@ -151,6 +153,10 @@ __device__ __forceinline__ void compute_tile_f8(uint32_t sK, uint32_t sV, const 
       if (TAIL) {
         const int keep = n_valid - (j * 16 + (lane & 3) * 4);   // of this lane's four tokens
         keep_mask = keep >= 4 ? 0xffffffffu : (keep <= 0 ? 0u : ((1u << (8 * keep)) - 1u));
+        if constexpr (SEL) {                                    // and the slots behind a partial page
+          const int left = sel_tokens<BS>(badmask, (j * 16) / BS) - ((j * 16) % BS + (lane & 3) * 4);
+          keep_mask &= left >= 4 ? 0xffffffffu : (left <= 0 ? 0u : ((1u << (8 * left)) - 1u));
+        }
         if constexpr (MOD) {                                    // and those before the first token
           const int drop = md.head - (j * 16 + (lane & 3) * 4);
           keep_mask &= drop <= 0 ? 0xffffffffu : (drop >= 4 ? 0u : ~((1u << (8 * drop)) - 1u));

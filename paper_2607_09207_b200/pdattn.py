@@ -42,6 +42,9 @@ EXPORTS = [
     "pdattn_decode_scored", "pdattn_decode_scored_fp8",
     "pdattn_pages_workspace_size", "pdattn_pages_init", "pdattn_pages_reserve", "pdattn_pages_fork", "pdattn_pages_free",
     "pdattn_pages_compact", "pdattn_pages_copy",
+    "pdattn_rope_append_at", "pdattn_rope_append_at_fp8", "pdattn_tree_workspace_size", "pdattn_decode_tree", "pdattn_decode_tree_fp8",
+    "pdattn_tree_accept", "pdattn_pages_trim", "pdattn_summarize_append", "pdattn_summarize_pages", "pdattn_select_workspace_size",
+    "pdattn_select_pages", "pdattn_decode_selected", "pdattn_decode_selected_fp8",
 ]
 
 
@@ -87,6 +90,23 @@ class RopeArgs(ctypes.Structure):
 class ScoreArgs(ctypes.Structure):
     _fields_ = [("logit_cap", ctypes.c_float), ("bias_slopes", ctypes.c_void_p), ("window", ctypes.c_int),
                 ("key_begin", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p), ("key_begin_host", ctypes.c_void_p)]
+
+
+class SummaryArgs(ctypes.Structure):
+    _fields_ = [("k_cache", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("codes", ctypes.c_void_p),
+                ("exponents", ctypes.c_void_p), ("num_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("block_size", ctypes.c_int), ("num_blocks", ctypes.c_int), ("element_bytes", ctypes.c_int),
+                ("kv_block_stride", ctypes.c_int64), ("kv_head_stride", ctypes.c_int64), ("kv_token_stride", ctypes.c_int64),
+                ("workspace", ctypes.c_void_p)]
+
+
+class SelectArgs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("codes", ctypes.c_void_p), ("exponents", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("context_lens", ctypes.c_void_p), ("selected", ctypes.c_void_p),
+                ("num_seqs", ctypes.c_int), ("num_q_heads", ctypes.c_int), ("num_kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("block_size", ctypes.c_int), ("max_blocks_per_seq", ctypes.c_int),
+                ("num_blocks", ctypes.c_int), ("num_selected", ctypes.c_int), ("num_first", ctypes.c_int),
+                ("num_recent", ctypes.c_int), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class PoolArgs(ctypes.Structure):
@@ -152,6 +172,19 @@ def lib():
         L.pdattn_pages_free.argtypes = [pool, vp, vp, vp, i32, i32, i32, i32, vp, sz, vp]
         L.pdattn_pages_compact.argtypes = [pool, vp, vp, i32, i32, i32, vp, vp, i32, vp, sz, vp]
         L.pdattn_pages_copy.argtypes = [vp] * 4 + [i32] * 6 + [i64] * 3 + [vp, vp]
+        L.pdattn_rope_append_at.argtypes = [ctypes.POINTER(RopeArgs), vp, vp]
+        L.pdattn_rope_append_at_fp8.argtypes = [ctypes.POINTER(RopeArgs), vp, vp, vp, vp]
+        L.pdattn_tree_workspace_size.argtypes = [i32] * 5 + [ctypes.POINTER(sz)]
+        L.pdattn_decode_tree.argtypes = [ctypes.POINTER(Args), vp, i32, vp, i32, vp]
+        L.pdattn_decode_tree_fp8.argtypes = [ctypes.POINTER(Args), vp, i32, vp, i32, vp, vp, vp]
+        L.pdattn_tree_accept.argtypes = [vp] * 7 + [i32] * 8 + [i64] * 3 + [vp, vp]
+        L.pdattn_pages_trim.argtypes = [pool, vp, vp, vp, i32, i32, i32, vp, sz, vp]
+        L.pdattn_summarize_append.argtypes = [ctypes.POINTER(SummaryArgs), vp, vp, vp, i32, i32, i32, vp]
+        L.pdattn_summarize_pages.argtypes = [ctypes.POINTER(SummaryArgs), vp, i32, vp]
+        L.pdattn_select_workspace_size.argtypes = [i32] * 3 + [ctypes.POINTER(sz)]
+        L.pdattn_select_pages.argtypes = [ctypes.POINTER(SelectArgs), vp]
+        L.pdattn_decode_selected.argtypes = [ctypes.POINTER(Args), vp, i32, vp]
+        L.pdattn_decode_selected_fp8.argtypes = [ctypes.POINTER(Args), vp, i32, vp, vp, vp]
         L.pdattn_profile_events.argtypes = [vp, vp]
         L.pdattn_gather_probe.argtypes = [ctypes.POINTER(Args), vp]
         L.pdattn_stream_read_probe.argtypes = [vp, sz, vp, vp]
@@ -525,17 +558,28 @@ def _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, kv_strides, bloc
                     1 if interleaved else 0, N, S, Hq, Hkv, d, bs, MB, NB, *kv_strides, _ptr(workspace))
 
 
+def _positions(where, positions, num_tokens):
+    _expect_dense(where, torch.int32, positions)
+    if positions.numel() != num_tokens:
+        raise ValueError(f"{where}: {positions.numel()} positions for {num_tokens} tokens")
+    return positions.data_ptr()
+
+
 def rope_append(q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_lens, inv_freq, *, cu_tokens=None,
                 rotary_dim=None, interleaved: bool = False, magnitude: float = 1.0, workspace=None, stream=None,
-                check: bool = True) -> int:
+                check: bool = True, positions=None) -> int:
     """pdattn_rope_append: rotate q ([N, Hq, d], rows of any token stride; None: only k and v) into q_out and k_new into
     the paged cache beside v_new ([N, Hkv, d]).  context_lens counts the new tokens; cu_tokens [S + 1] (None: one new
-    token per sequence)."""
+    token per sequence).  positions (int32 [N], pdattn_rope_append_at): those of the rotation, for tokens of a tree."""
     where = "pdattn_rope_append"
     _expect_caches(where, k_cache, v_cache)
     a = _rope_args(where, q, k_new, v_new, q_out, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, inv_freq,
                    cu_tokens, rotary_dim, interleaved, magnitude, workspace)
-    st = lib().pdattn_rope_append(ctypes.byref(a), _stream_ptr(stream))
+    if positions is None:
+        st = lib().pdattn_rope_append(ctypes.byref(a), _stream_ptr(stream))
+    else:
+        where = "pdattn_rope_append_at"
+        st = lib().pdattn_rope_append_at(ctypes.byref(a), _positions(where, positions, a.num_tokens), _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
     return st
@@ -543,13 +587,18 @@ def rope_append(q, k_new, v_new, q_out, k_cache, v_cache, block_table, context_l
 
 def rope_append_fp8(q, k_new, v_new, q_out, k8, v8, k_scale, v_scale, block_table, context_lens, inv_freq, *,
                     cu_tokens=None, rotary_dim=None, interleaved: bool = False, magnitude: float = 1.0, workspace=None,
-                    stream=None, check: bool = True) -> int:
+                    stream=None, check: bool = True, positions=None) -> int:
     """pdattn_rope_append_fp8: rope_append into the e4m3 code pools of decode_fp8."""
     where = "pdattn_rope_append_fp8"
     _expect_codes(where, k8, v8, k_scale, v_scale)
     a = _rope_args(where, q, k_new, v_new, q_out, k8, v8, (0, 0, 0), block_table, context_lens, inv_freq, cu_tokens, rotary_dim,
                    interleaved, magnitude, workspace)
-    st = lib().pdattn_rope_append_fp8(ctypes.byref(a), k_scale.data_ptr(), v_scale.data_ptr(), _stream_ptr(stream))
+    if positions is None:
+        st = lib().pdattn_rope_append_fp8(ctypes.byref(a), k_scale.data_ptr(), v_scale.data_ptr(), _stream_ptr(stream))
+    else:
+        where = "pdattn_rope_append_at_fp8"
+        st = lib().pdattn_rope_append_at_fp8(ctypes.byref(a), _positions(where, positions, a.num_tokens), k_scale.data_ptr(),
+                                             v_scale.data_ptr(), _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
     return st
@@ -674,6 +723,228 @@ def _scored(where, call, q, a: Args, score: Score, scales, stream, check) -> int
     return st
 
 
+def tree_workspace_size(num_q_heads, num_kv_heads, head_dim, block_size=16, max_tree_tokens=64) -> int:
+    n = ctypes.c_size_t(0)
+    st = lib().pdattn_tree_workspace_size(num_q_heads, num_kv_heads, head_dim, block_size, max_tree_tokens, ctypes.byref(n))
+    if st != OK:
+        raise PdattnError(st, "pdattn_tree_workspace_size")
+    return n.value
+
+
+def _alloc(n, device, stream):
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    st = lib().pdattn_workspace_init(ws.data_ptr(), n, _stream_ptr(stream))
+    if st != OK:
+        raise PdattnError(st, "pdattn_workspace_init")
+    return ws
+
+
+def alloc_tree_workspace(num_q_heads, num_kv_heads, head_dim, block_size=16, max_tree_tokens=64, device="cuda", stream=None):
+    return _alloc(tree_workspace_size(num_q_heads, num_kv_heads, head_dim, block_size, max_tree_tokens), device, stream)
+
+
+def _tree(where, call, q, a: Args, cu_tokens, tree_mask, max_tree_tokens, scales, stream, check) -> int:
+    _expect_dense(where, torch.int32, cu_tokens)
+    if tree_mask.dtype not in (torch.int64, torch.uint64):
+        raise TypeError(f"{where}: tree_mask holds 64 bits per token, got {tree_mask.dtype}")
+    _expect_dense(where, tree_mask.dtype, tree_mask)
+    if cu_tokens.numel() != a.num_seqs + 1:
+        raise ValueError(f"{where}: cu_tokens has {cu_tokens.numel()} entries for {a.num_seqs} sequences")
+    if tree_mask.numel() != q.shape[0]:
+        raise ValueError(f"{where}: tree_mask has {tree_mask.numel()} entries for {q.shape[0]} tokens")
+    st = call(ctypes.byref(a), cu_tokens.data_ptr(), q.shape[0], tree_mask.data_ptr(), max_tree_tokens, *scales, _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def decode_tree(q, k_cache, v_cache, block_table, context_lens, cu_tokens, tree_mask, scale, out, workspace, *,
+                max_tree_tokens: int = 64, stream=None, check: bool = True) -> int:
+    """pdattn_decode_tree: q and out [N, Hq, d]; the drafted tokens cu_tokens[s] .. cu_tokens[s + 1] are the last ones of sequence s's
+    context_lens[s], and token j of them sees token i of the tree where bit i of its tree_mask (int64 or uint64 [N]) is set."""
+    where = "pdattn_decode_tree"
+    _expect_caches(where, k_cache, v_cache)
+    a = _step_args(where, q, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, scale, out, workspace)
+    return _tree(where, lib().pdattn_decode_tree, q, a, cu_tokens, tree_mask, max_tree_tokens, (), stream, check)
+
+
+def decode_tree_fp8(q, k8, v8, k_scale, v_scale, block_table, context_lens, cu_tokens, tree_mask, scale, out, workspace, *,
+                    max_tree_tokens: int = 64, stream=None, check: bool = True) -> int:
+    """pdattn_decode_tree_fp8: decode_tree over the e4m3 code pools of decode_fp8."""
+    where = "pdattn_decode_tree_fp8"
+    _expect_codes(where, k8, v8, k_scale, v_scale)
+    a = _step_args(where, q, k8, v8, (0, 0, 0), block_table, context_lens, scale, out, workspace)
+    return _tree(where, lib().pdattn_decode_tree_fp8, q, a, cu_tokens, tree_mask, max_tree_tokens,
+                 (k_scale.data_ptr(), v_scale.data_ptr()), stream, check)
+
+
+def _expect_pools(where, k_cache, v_cache):
+    """bf16 caches, or the code pools of decode_fp8."""
+    if k_cache.dtype == torch.uint8:
+        _expect_dense(where, torch.uint8, k_cache, v_cache)
+        NB, Hkv, bs, d = k_cache.shape
+        if tuple(v_cache.shape) != (NB, Hkv, d, bs):
+            raise ValueError(f"{where}: code pools {tuple(k_cache.shape)} and {tuple(v_cache.shape)} do not belong together")
+    else:
+        _expect_caches(where, k_cache, v_cache)
+
+
+def tree_accept(k_cache, v_cache, block_table, context_lens, cu_tokens, accepted, accepted_counts, workspace=None, stream=None,
+                check: bool = True) -> int:
+    """pdattn_tree_accept: K and V of the tree's tokens accepted[s, :accepted_counts[s]] (int32 [S, M], [S]) move to the front of the tree's
+    slots, in bf16 caches or the uint8 code pools of decode_fp8; the lengths stay."""
+    where = "pdattn_tree_accept"
+    _expect_dense(where, torch.int32, block_table, context_lens, cu_tokens, accepted, accepted_counts)
+    _expect_pools(where, k_cache, v_cache)
+    if workspace is not None:
+        _expect_workspace(where, workspace)
+    S, MB = block_table.shape
+    if context_lens.numel() != S or cu_tokens.numel() != S + 1 or accepted.dim() != 2 or accepted.shape[0] != S or accepted_counts.numel() != S:
+        raise ValueError(f"{where}: shapes do not belong together")
+    NB, Hkv, bs, d = k_cache.shape
+    st = lib().pdattn_tree_accept(k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
+                                  cu_tokens.data_ptr(), accepted.data_ptr(), accepted_counts.data_ptr(), accepted.shape[1], S, Hkv, d,
+                                  bs, MB, NB, k_cache.element_size(), *k_cache.stride()[:3], _ptr(workspace), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+class PageSummary:
+    """Summaries of a pool's pages (pdattn_summary_args): codes int8 [pages, Hkv, 2, d] (minima, maxima), exponents int8 [pages, Hkv]."""
+
+    def __init__(self, codes, exponents):
+        _expect_dense("PageSummary", torch.int8, codes, exponents)
+        if codes.dim() != 4 or codes.shape[2] != 2 or tuple(exponents.shape) != tuple(codes.shape[:2]):
+            raise ValueError(f"PageSummary: codes {tuple(codes.shape)} and exponents {tuple(exponents.shape)} do not belong together")
+        self.codes, self.exponents = codes, exponents
+        self.device = codes.get_device()
+
+    @classmethod
+    def create(cls, num_blocks: int, num_kv_heads: int, head_dim: int, device="cuda") -> "PageSummary":
+        return cls(torch.zeros(num_blocks, num_kv_heads, 2, head_dim, dtype=torch.int8, device=device),
+                   torch.zeros(num_blocks, num_kv_heads, dtype=torch.int8, device=device))
+
+
+def _summary_args(where, k_cache, summary: PageSummary, k_scale, workspace) -> SummaryArgs:
+    NB, Hkv, bs, d = k_cache.shape
+    if k_cache.dtype == torch.uint8:
+        _expect_dense(where, torch.uint8, k_cache)
+        if k_scale is None or k_scale.numel() != Hkv:
+            raise ValueError(f"{where}: a pool of codes comes with one k_scale per KV head")
+        _expect_dense(where, torch.float32, k_scale)
+    else:
+        _expect(where, torch.bfloat16, k_cache)
+        if k_cache.stride(3) != 1:
+            raise ValueError(f"{where}: head_dim has to be contiguous")
+        if k_scale is not None:
+            raise ValueError(f"{where}: k_scale belongs to a pool of codes")
+    if workspace is not None:
+        _expect_workspace(where, workspace)
+    _expect_device(where, summary.device)
+    if tuple(summary.codes.shape) != (NB, Hkv, 2, d):
+        raise ValueError(f"{where}: a cache {tuple(k_cache.shape)} with summaries {tuple(summary.codes.shape)}")
+    return SummaryArgs(k_cache.data_ptr(), _ptr(k_scale), summary.codes.data_ptr(), summary.exponents.data_ptr(), Hkv, d, bs, NB,
+                       k_cache.element_size(), *k_cache.stride()[:3], _ptr(workspace))
+
+
+def summarize_append(k_cache, summary: PageSummary, block_table, context_lens, cu_tokens=None, num_tokens: Optional[int] = None, k_scale=None,
+                     workspace=None, stream=None, check: bool = True) -> int:
+    """pdattn_summarize_append: summaries of the pages that the last cu_tokens[s + 1] - cu_tokens[s] tokens of every sequence filled (None:
+    one token each).  num_tokens, needed with cu_tokens: cu_tokens[S], or more."""
+    where = "pdattn_summarize_append"
+    _expect_dense(where, torch.int32, block_table, context_lens, cu_tokens)
+    a = _summary_args(where, k_cache, summary, k_scale, workspace)
+    S, MB = block_table.shape
+    if context_lens.numel() != S or (cu_tokens is not None and cu_tokens.numel() != S + 1):
+        raise ValueError(f"{where}: shapes do not belong together")
+    if cu_tokens is None:
+        num_tokens = S
+    elif num_tokens is None:
+        raise ValueError(f"{where}: num_tokens is needed with cu_tokens")
+    st = lib().pdattn_summarize_append(ctypes.byref(a), block_table.data_ptr(), context_lens.data_ptr(), _ptr(cu_tokens), num_tokens, S, MB,
+                                       _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def summarize_pages(k_cache, summary: PageSummary, pages, k_scale=None, workspace=None, stream=None, check: bool = True) -> int:
+    """pdattn_summarize_pages: summaries of the pages of a list (int32; entries below 0 are passed over)."""
+    where = "pdattn_summarize_pages"
+    _expect_dense(where, torch.int32, pages)
+    a = _summary_args(where, k_cache, summary, k_scale, workspace)
+    st = lib().pdattn_summarize_pages(ctypes.byref(a), pages.data_ptr(), pages.numel(), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def select_workspace_size(num_seqs, num_kv_heads, max_blocks_per_seq) -> int:
+    n = ctypes.c_size_t(0)
+    st = lib().pdattn_select_workspace_size(num_seqs, num_kv_heads, max_blocks_per_seq, ctypes.byref(n))
+    if st != OK:
+        raise PdattnError(st, "pdattn_select_workspace_size")
+    return n.value
+
+
+def alloc_select_workspace(num_seqs, num_kv_heads, max_blocks_per_seq, device="cuda", stream=None):
+    return _alloc(select_workspace_size(num_seqs, num_kv_heads, max_blocks_per_seq), device, stream)
+
+
+def select_pages(q, summary: PageSummary, block_table, context_lens, selected, block_size: int, workspace, *, num_first: int = 1,
+                 num_recent: int = 1, stream=None, check: bool = True) -> int:
+    """pdattn_select_pages: selected (int32 [S, Hkv, K]) receives, per sequence and KV head, the pages the token q [S, Hq, d] is to see: the
+    first num_first, the last num_recent and the best of the others by their summaries, ascending, -1 past the last."""
+    where = "pdattn_select_pages"
+    _expect_dense(where, torch.bfloat16, q)
+    _expect_dense(where, torch.int32, block_table, context_lens, selected)
+    _expect_workspace(where, workspace)
+    _expect_device(where, summary.device)
+    S, Hq, d = q.shape
+    NB, Hkv = summary.exponents.shape
+    MB = block_table.shape[1]
+    if (block_table.shape[0] != S or context_lens.numel() != S or selected.dim() != 3 or tuple(selected.shape[:2]) != (S, Hkv)
+            or summary.codes.shape[3] != d):
+        raise ValueError(f"{where}: shapes do not belong together")
+    a = SelectArgs(q.data_ptr(), summary.codes.data_ptr(), summary.exponents.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
+                   selected.data_ptr(), S, Hq, Hkv, d, block_size, MB, NB, selected.shape[2], num_first, num_recent, workspace.data_ptr(),
+                   workspace.numel())
+    st = lib().pdattn_select_pages(ctypes.byref(a), _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def _selected(where, call, q, a: Args, selected, scales, stream, check) -> int:
+    _expect_dense(where, torch.int32, selected)
+    if q.shape[0] != a.num_seqs or selected.dim() != 3 or tuple(selected.shape[:2]) != (a.num_seqs, a.num_kv_heads):
+        raise ValueError(f"{where}: q {tuple(q.shape)} and selected {tuple(selected.shape)} for {a.num_seqs} sequences of {a.num_kv_heads} KV heads")
+    st = call(ctypes.byref(a), selected.data_ptr(), selected.shape[2], *scales, _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def decode_selected(q, k_cache, v_cache, block_table, context_lens, selected, scale, out, workspace,
+                    context_lens_host: Optional[np.ndarray] = None, stream=None, check: bool = True) -> int:
+    """pdattn_decode_selected: decode_ex over the chosen pages of every sequence and KV head (selected int32 [S, Hkv, K])."""
+    where = "pdattn_decode_selected"
+    _expect_caches(where, k_cache, v_cache)
+    a = _step_args(where, q, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, scale, out, workspace,
+                   context_lens_host)
+    return _selected(where, lib().pdattn_decode_selected, q, a, selected, (), stream, check)
+
+
+def decode_selected_fp8(q, k8, v8, k_scale, v_scale, block_table, context_lens, selected, scale, out, workspace,
+                        context_lens_host: Optional[np.ndarray] = None, stream=None, check: bool = True) -> int:
+    """pdattn_decode_selected_fp8: decode_selected over the e4m3 code pools of decode_fp8."""
+    where = "pdattn_decode_selected_fp8"
+    _expect_codes(where, k8, v8, k_scale, v_scale)
+    a = _step_args(where, q, k8, v8, (0, 0, 0), block_table, context_lens, scale, out, workspace, context_lens_host)
+    return _selected(where, lib().pdattn_decode_selected_fp8, q, a, selected, (k_scale.data_ptr(), v_scale.data_ptr()), stream, check)
+
+
 class PagePool:
     """The books of a page pool (pdattn_page_pool): int32 device tensors ref_counts [num_blocks], free_list [num_blocks],
     free_count [1]."""
@@ -765,6 +1036,21 @@ def pages_free(pool: PagePool, block_table, context_lens, seqs, block_size: int,
     st = lib().pdattn_pages_free(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(), seqs.data_ptr(),
                                  seqs.numel(), S, MB, block_size, workspace.data_ptr(), workspace.numel(),
                                  _stream_ptr(stream))
+    if check and st != OK:
+        raise PdattnError(st, where)
+    return st
+
+
+def pages_trim(pool: PagePool, block_table, context_lens, new_lens, block_size: int, workspace, stream=None,
+               check: bool = True) -> int:
+    """pdattn_pages_trim: row s is shortened to new_lens[s] tokens; the pages behind them go back."""
+    where = "pdattn_pages_trim"
+    _pages_check(where, pool, workspace, block_table, context_lens, new_lens)
+    S, MB = block_table.shape
+    if new_lens.numel() != S:
+        raise ValueError(f"{where}: new_lens has one entry per row")
+    st = lib().pdattn_pages_trim(ctypes.byref(pool.args), block_table.data_ptr(), context_lens.data_ptr(), new_lens.data_ptr(), S, MB,
+                                 block_size, workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
     if check and st != OK:
         raise PdattnError(st, where)
     return st
