@@ -156,6 +156,34 @@ PDATTN_HD inline int selected_pages(int context_len, int block_size, int num_sel
   return pages < num_selected ? pages : num_selected;
 }
 
+// ---- pdattn_decode_tree: the stream of its key tiles
+// A unit is (sequence, KV head, pair of row tiles) and costs its key tiles plus kTreeStart for starting it; a sequence's units have the
+// same number of key tiles.  CTA i of n takes the stretch [total * i / n, total * (i + 1) / n) of the cost stream.  tree_cut says where
+// position r of a sequence's stretch falls: the unit and the key tile it begins at.  A cut nearer than kTreeMinCut tiles to a unit's
+// end moves there (a unit shorter than twice that stays whole), and no more CTAs are used than give each a unit or that many tiles.
+constexpr int kTreeKeys = 128;     // keys of a tile
+constexpr int kTreeStart = 2;
+constexpr int kTreeMinCut = 4;
+PDATTN_HD inline void tree_cut(int64_t r, int64_t tiles, int* unit, int* tile) {
+  const int64_t per = tiles + kTreeStart;
+  int64_t u = r / per;
+  const int64_t pos = r - u * per;
+  int64_t t = pos > kTreeStart ? pos - kTreeStart : 0;
+  if (t < kTreeMinCut) {
+    t = 0;
+  } else if (tiles - t < kTreeMinCut) {
+    t = 0;
+    ++u;
+  }
+  *unit = static_cast<int>(u);
+  *tile = static_cast<int>(t);
+}
+
+PDATTN_HD inline int tree_shares(int64_t total_cost, int64_t total_units, int ctas) {
+  const int64_t n = total_cost / kTreeMinCut > total_units ? total_cost / kTreeMinCut : total_units;
+  return n < 1 ? 1 : n < ctas ? static_cast<int>(n) : ctas;
+}
+
 // Parts of an item of pdattn_prefill that were written, from the word its CTAs left in the workspace.  When a call's bounded waits
 // run out, units may never be drawn and the word is whatever the memory held: it must not lead past the parts' room.
 PDATTN_HD inline int join_parts(int word, int splits) { return word < 0 ? 0 : word < splits ? word : splits; }
