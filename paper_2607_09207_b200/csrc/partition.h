@@ -161,9 +161,9 @@ PDATTN_HD inline int selected_pages(int context_len, int block_size, int num_sel
 // same number of key tiles.  CTA i of n takes the stretch [total * i / n, total * (i + 1) / n) of the cost stream.  tree_cut says where
 // position r of a sequence's stretch falls: the unit and the key tile it begins at.  A cut nearer than kTreeMinCut tiles to a unit's
 // end moves there (a unit shorter than twice that stays whole), and no more CTAs are used than give each a unit or that many tiles.
-constexpr int kTreeKeys = 128;     // keys of a tile
-constexpr int kTreeStart = 2;
-constexpr int kTreeMinCut = 4;
+constexpr int kTreeKeys = 64;      // keys of a tile
+constexpr int kTreeStart = 4;
+constexpr int kTreeMinCut = 8;
 PDATTN_HD inline void tree_cut(int64_t r, int64_t tiles, int* unit, int* tile) {
   const int64_t per = tiles + kTreeStart;
   int64_t u = r / per;

@@ -5,8 +5,11 @@
 // Rows.  The query rows of one KV head are packed: row r of a 128-row tile is head r % G of token r / G, so a tile holds
 // floor(128 / G) whole tokens and every K/V tile is read once for all of them.
 //
-//   S_t[128, 128 keys] = Q_t . K^T     both from shared memory            t = 0, 1
-//   O_t[128, d]       += P_t . V       P from tensor memory (over S_t's columns), V from shared memory
+//   S_t[128, 64 keys] = Q_t . K^T     both from shared memory            t = 0, 1
+//   O_t[128, d]      += P_t . V       P from tensor memory (over S_t's columns), V from shared memory
+//
+// A group's scores have two buffers of 64 columns: those of its next key tile are there when it has handed over the weights of the
+// present one, so no product waits in the chain of a group, and 64 scores stay in a thread's registers: read once, no second pass.
 //
 // Two softmax groups of four warps (a thread owns a row: no shuffles) keep the memory system busy, in one of two ways:
 //   PAIR   trees of more than 128 rows: t are two row tiles, every key tile serves both;
@@ -19,10 +22,13 @@
 // the lengths.  A CTA works out its share from the lengths by itself (every warp sums its part of the batch, then one warp walks).  A unit
 // that a share's end cuts leaves (m, l, O) per piece, at most two a CTA; tree_join_kernel puts them together in order.
 //
-// Roles: warps 0-7 softmax, 8 issues the MMAs, 9 walks the units and loads Q, 10 loads K, 11 V (TMA), 12-15: over the bf16 cache two
-// of them guard V (see prefill_umma.cuh: non-finite elements of V at keys that some row does not see are set to 0 and added
-// again for the rows that see them); over the fp8 cache they widen the codes of K and V to fp16 (exact), which is the guard as well.
-// fp8: V's pages are transposed, so its tile is K-major in the second product.
+// Roles: warps 0-7 softmax, 8 walks the units and loads Q and K, 9 loads V (TMA), 10 and 11 issue the MMAs of a group each, 12-15: over the
+// bf16 cache two of them guard V (see prefill_umma.cuh: non-finite elements of V at keys that some row does not see are set to 0 and added
+// again for the rows that see them); over the fp8 cache they widen V's codes to fp16 (exact), which is the guard as well, and split Q.
+//
+// fp8.  The codes of K are an operand as they come: Q is split into two e4m3 terms per element, with a power of two per row, and
+// both run against the same K tile (twice the multiplications at twice the rate).  V's pages are transposed, so its tile is K-major
+// in the second product.
 //
 // Numbers: scores, maxima, sums and O in fp32.  The weights are rounded to bf16 for the second product (at most 2^-8 of each,
 // independent; the fp8 form to fp16, 2^-11): the size of the final rounding.  The reference of the online softmax follows the
@@ -31,6 +37,8 @@
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA warp drains, tensor memory is
 // freed and the CTA returns.
 #pragma once
+
+#include <cuda_fp16.h>
 
 #include <climits>
 #include <type_traits>
@@ -66,21 +74,27 @@ struct TreeParams {
 template <int D, bool PAIR, int EB>
 struct TreeCfg {
   static constexpr int HALVES = D / 64;
-  static constexpr int HALF_BYTES = 128 * 128;              // 128 rows of one 64-column block
-  static constexpr int TILE_BYTES = HALVES * HALF_BYTES;    // a Q, K or V tile of 16-bit elements
-  static constexpr int RAW_BYTES = 128 * D;                 // a K or V tile of codes
+  static constexpr int Q_HALF = 128 * 128;                  // 128 rows of one 64-column block
+  static constexpr int Q_BYTES = HALVES * Q_HALF;           // a row tile of Q
+  static constexpr int HALF_BYTES = kTreeKeys * 128;        // 64 keys of one 64-column block
+  static constexpr int TILE_BYTES = HALVES * HALF_BYTES;    // a K or V tile of 16-bit elements
+  static constexpr int RAW_BYTES = kTreeKeys * D;           // a K or V tile of codes
   static constexpr int QT = PAIR ? 2 : 1;
-  static constexpr int LAG = PAIR ? 1 : 2;                  // the product of key tile c is issued with the scores of c + LAG
-  // rings of K tiles, of V tiles, of code tiles (each of K and of V)
-  static constexpr int NK = EB == 1 ? 2 : D == 128 ? 3 : 6;
-  static constexpr int NV = EB == 1 ? 2 : D == 128 ? (PAIR ? 2 : 3) : (PAIR ? 4 : 6);
-  static constexpr int NR = EB == 2 ? 0 : D == 128 ? (PAIR ? 1 : 2) : 4;   // (at most 4: see page_bad)
-  static constexpr int RING_BYTES = (QT + NK + NV) * TILE_BYTES + 2 * NR * RAW_BYTES;
-  static constexpr int CTRL_BYTES = 2048;
+  static constexpr int NQ = PAIR ? 1 : 2;                   // buffers of an item's Q
+  static constexpr int LAG = PAIR ? 2 : 4;                  // the product of key tile c is issued with the scores of c + LAG
+  // bytes of a K tile (codes as they come, or bf16) and of the two e4m3 tiles that Q becomes over codes (head_dim 128: in Q's place)
+  static constexpr int K_BYTES = EB == 1 ? RAW_BYTES : TILE_BYTES;
+  static constexpr int QP_BYTES = EB == 1 && D == 64 ? 2 * 128 * D : 0;
+  // rings of K tiles, of V tiles, of V's code tiles
+  static constexpr int NK = EB == 2 && D == 128 ? 5 : 6;
+  static constexpr int NV = EB == 1 ? 4 : D == 128 ? 5 : 6;
+  static constexpr int NR = EB == 1 ? 4 : 0;
+  static constexpr int RING_BYTES = NQ * QT * (Q_BYTES + QP_BYTES) + NK * K_BYTES + NV * TILE_BYTES + NR * RAW_BYTES;
+  static constexpr int CTRL_BYTES = EB == 1 ? 3072 : 2048;
   static constexpr int DYN_BYTES = 1024 + RING_BYTES + CTRL_BYTES;
   static constexpr int COL_S = 0, COL_O = 256, TMEM_COLS = 512;
   static_assert(DYN_BYTES <= 232448, "shared memory");
-  static_assert(NV >= LAG && NK >= 2 && (EB == 2 || NR >= 1), "rings");
+  static_assert(NV >= LAG && NK >= 2 && NK <= 6 && (EB == 2 || NR >= 1), "rings");
 };
 
 struct TreeItem {
@@ -94,25 +108,26 @@ struct TreeItem {
 };
 
 struct TreeCtrl {
-  // per key tile c of the CTA (mod 8): K, V have landed; V has passed the guard (fp8: K, V are widened); step c is done, i.e. the scores
+  // per key tile c of the CTA (mod 8): K, V have landed; V has passed the guard (fp8: is widened); step c is done, i.e. the scores
   // of key tile c and the product of c - LAG
-  uint64_t k_full[8], v_full[8], k_ok[8], v_ok[8], step[8];
-  uint64_t q_full, q_ok, q_free;
-  uint64_t s_full[2], p_part[2][2];              // per group: scores are there; the weights of the first, the second 64 keys are stored
-  uint64_t o_full[2];                            // the item's last product into O is done
+  uint64_t k_full[8], v_full[8], v_ok[8], step[8];
+  uint64_t q_full[2], q_ok[2], q_free[2];        // per buffer of Q: it has landed; fp8: is split; its scores are done
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];   // per group and buffer: scores are there; weights are stored; their product is done
   uint64_t item_full[TR_ITEMS], item_free[TR_ITEMS];
-  uint64_t drained, meet, meet_widen;            // all softmax warps are here; all widening warps are
+  uint64_t drained[2], meet, meet_widen;         // all softmax warps are here; all widening warps are
   TreeItem item[TR_ITEMS];
-  // Per key tile (mod 8): bit j set = its page j had a bad id; keys whose V held something non-finite.  Both are read before the last
-  // weights of key tile c are handed over, and written anew for c + 8 only when the product of c is done (K(c + 8) is loaded after
-  // step c + 8 - NK >= c + 2, or codes after those of c + 8 - NR were widened, which waits for step c + 8 - NR - NK >= c + 2).
-  uint32_t page_bad[8];
-  uint32_t v_bad[8][4];
+  // Per key tile: bit j set = its page j had a bad id; keys whose V held something non-finite.  Both are read before the weights of
+  // key tile c are handed over.  They are written anew with K(c + 16), loaded after step c + 16 - NK >= c + 10, which is issued behind
+  // the product of c + 6 or a later one, and with V(c + 8), which waits for step c + 8 - NV + LAG >= c + LAG, the one behind the product of c.
+  uint32_t page_bad[16];
+  uint32_t v_bad[8][2];
   uint32_t odd[TR_ITEMS];                        // split: some row sees such a key
   uint32_t abort, tmem_base;
   float2 ml[64 * 2];                             // split: (m, l) of group 1's rows, then the factors of both groups
 };
 static_assert(sizeof(TreeCtrl) <= 2048, "control block");
+// Behind it over codes: per buffer and row of Q, the factor that belongs to its e4m3 terms.
+constexpr int TR_QSCALE_AT = 2048;
 
 // Bounded wait that also gives up when the CTA's abort flag is up; the clock comes into it after 64 polls.
 __device__ __forceinline__ bool tree_wait(uint32_t bar, uint32_t parity, const uint32_t* abort_flag) {
@@ -127,6 +142,20 @@ __device__ __forceinline__ bool tree_wait(uint32_t bar, uint32_t parity, const u
       if (*reinterpret_cast<const volatile uint32_t*>(abort_flag) || now - t0 > kWaitLimitNs) return false;
     }
   }
+}
+// A look that does not suspend the thread.
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ int tree_uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }   // known to be the same in every lane
 __device__ __forceinline__ uint64_t tree_pack2(float a, float b) {
@@ -145,7 +174,46 @@ __device__ __forceinline__ uint64_t tree_add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// Instruction descriptor as umma_idesc's, for fp16 operands.
+__device__ __forceinline__ uint64_t tree_mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// 2^x of two values on the FMA pipe, x <= 127: x = n + f with n the nearest whole number, and 2^f by the polynomial of degree 4 with the
+// smallest largest relative error on [-1/2, 1/2] (2^-18.5).  0 from x = -126.5 down, NaN for NaN.
+__device__ __forceinline__ void tree_exp2_pair(float& a, float& b) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-127.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-127.f));
+  const uint64_t x = tree_pack2(a, b);
+  constexpr float kMagic = 12582912.f;               // 1.5 * 2^23: the sum's last bits are n
+  const uint64_t t = tree_add2(x, tree_pack2(kMagic, kMagic));
+  const uint64_t n = tree_add2(t, tree_pack2(-kMagic, -kMagic));
+  const uint64_t f = tree_fma2(n, tree_pack2(-1.f, -1.f), x);
+  uint64_t p = tree_fma2(tree_pack2(0.009570089168846607f, 0.009570089168846607f), f, tree_pack2(0.05591785907745361f, 0.05591785907745361f));
+  p = tree_fma2(p, f, tree_pack2(0.2402474582195282f, 0.2402474582195282f));
+  p = tree_fma2(p, f, tree_pack2(0.6931217908859253f, 0.6931217908859253f));
+  p = tree_fma2(p, f, tree_pack2(0.9999992847442627f, 0.9999992847442627f));
+  float ta, tb;
+  tree_unpack2(t, ta, tb);
+  p = tree_mul2(p, tree_pack2(__uint_as_float((__float_as_uint(ta) << 23) + 0x3f800000u),
+                              __uint_as_float((__float_as_uint(tb) << 23) + 0x3f800000u)));
+  tree_unpack2(p, a, b);
+}
+// D[tmem] (+)= A[smem] . B[smem], e4m3 operands
+__device__ __forceinline__ void umma_ss_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p; }" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum)
+      : "memory");
+}
+// Matrix descriptor of K-major rows of D bytes: 128-byte swizzle for 128, 64-byte swizzle for 64.
+template <int D>
+__device__ __forceinline__ uint64_t umma_desc_rows(uint32_t saddr) {
+  static_assert(D == 128 || D == 64, "row size");
+  return static_cast<uint64_t>((saddr >> 4) & 0x3fffu) | (1ull << 16) | (static_cast<uint64_t>((8 * D) >> 4) << 32) | (1ull << 46) |
+         ((D == 128 ? 2ull : 4ull) << 61);
+}
+// Instruction descriptor as umma_idesc's, for fp16 operands (kind::f16) or e4m3 ones (kind::f8f6f4): both are format 0.
 __host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
@@ -215,40 +283,42 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
   uint8_t* smem = smem_raw + pad;
-  const uint32_t sQ = raw + pad, sK = sQ + QT * C::TILE_BYTES, sV = sK + NK * C::TILE_BYTES;
-  const uint32_t rK = sV + NV * C::TILE_BYTES, rV = rK + NR * C::RAW_BYTES;
+  const uint32_t sQ = raw + pad, sQP = sQ + (D == 64 ? C::NQ * QT * C::Q_BYTES : 0);   // (codes) Q's terms
+  const uint32_t sK = sQ + C::NQ * QT * (C::Q_BYTES + C::QP_BYTES), sV = sK + NK * C::K_BYTES, rV = sV + NV * C::TILE_BYTES;
   TreeCtrl* ctrl = reinterpret_cast<TreeCtrl*>(smem + C::RING_BYTES);
+  float* q_scale = reinterpret_cast<float*>(smem + C::RING_BYTES + TR_QSCALE_AT);   // [NQ * QT][128]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float NEG_INF = __int_as_float(0xff800000);
 
   if (threadIdx.x == 0) {
-    mbar_init(smem_u32(&ctrl->drained), 1);
+    mbar_init(smem_u32(&ctrl->drained[0]), 1);
+    mbar_init(smem_u32(&ctrl->drained[1]), 1);
     mbar_init(smem_u32(&ctrl->meet), 8);
     mbar_init(smem_u32(&ctrl->meet_widen), 4);
     for (int i = 0; i < 8; ++i) {
       mbar_init(smem_u32(&ctrl->k_full[i]), 1);
       mbar_init(smem_u32(&ctrl->v_full[i]), 1);
-      mbar_init(smem_u32(&ctrl->k_ok[i]), 4);
       mbar_init(smem_u32(&ctrl->v_ok[i]), F8 ? 4 : 2);
-      mbar_init(smem_u32(&ctrl->step[i]), 1);
+      mbar_init(smem_u32(&ctrl->step[i]), PAIR ? 2 : 1);
     }
-    mbar_init(smem_u32(&ctrl->q_full), 1);
-    mbar_init(smem_u32(&ctrl->q_ok), 4);
-    mbar_init(smem_u32(&ctrl->q_free), 1);
     for (int t = 0; t < 2; ++t) {
-      mbar_init(smem_u32(&ctrl->s_full[t]), 1);
-      mbar_init(smem_u32(&ctrl->p_part[t][0]), 4);
-      mbar_init(smem_u32(&ctrl->p_part[t][1]), 4);
-      mbar_init(smem_u32(&ctrl->o_full[t]), 1);
+      mbar_init(smem_u32(&ctrl->q_full[t]), 1);
+      mbar_init(smem_u32(&ctrl->q_ok[t]), 4);
+      mbar_init(smem_u32(&ctrl->q_free[t]), 2);
+      for (int b = 0; b < 2; ++b) {
+        mbar_init(smem_u32(&ctrl->s_full[t][b]), 1);
+        mbar_init(smem_u32(&ctrl->p_full[t][b]), 4);
+        mbar_init(smem_u32(&ctrl->pv_done[t][b]), 1);
+      }
     }
     for (int i = 0; i < TR_ITEMS; ++i) {
       mbar_init(smem_u32(&ctrl->item_full[i]), 1);
-      mbar_init(smem_u32(&ctrl->item_free[i]), 8 + 1 + 2 + (F8 ? 4 : 2));   // softmax, MMA, loads, guards
+      mbar_init(smem_u32(&ctrl->item_free[i]), 8 + 2 + 1 + (F8 ? 4 : 2));   // softmax, MMA, V, guards
     }
     ctrl->abort = 0;
     fence_mbar_init();
   }
-  if (warp == 8) {
+  if (warp == 10) {
     tmem_alloc(smem_u32(&ctrl->tmem_base), C::TMEM_COLS);
     tmem_relinquish();
   }
@@ -277,9 +347,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   const uint32_t tbase = tree_uniform(static_cast<int>(*reinterpret_cast<volatile uint32_t*>(&ctrl->tmem_base)));
   const uint32_t* abort_flag = &ctrl->abort;
 
-  // ---- this CTA's share: from (s0, u0, t0) to (s1, u1, t1); warp 9 walks it
+  // ---- this CTA's share: from (s0, u0, t0) to (s1, u1, t1); warp 8 walks it
   int s0 = 0, u0 = 0, t0 = 0, s1 = 0, u1 = 0, t1 = 0;
-  if (warp == 9) {
+  if (warp == 8) {
     int64_t total = 0, all_units = 0;
     for (int c = lane; c < chunks; c += 32) {
       total += chunk_cost[c];
@@ -362,17 +432,71 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   // The softmax threads hold many scores each; they take the registers that the others leave.
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TR_OTHER_REGS));
-    if (warp == 9) {
-      // ================= items, and Q of the one before: its buffer is free only when the item before that has all its scores
-      int4 rec[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};
-      int base = s0 & ~31;
-      TreeSeq win = tree_seq<PAIR>(P, base + lane);
-      int s = s0, u = u0, t = t0;
-      bool ok = true, more = true, ran_out = false;
-      int pend_k = -1, pend_g = 0, pend_row = 0;           // item whose Q is to be loaded
-      int nq = 0;
-      for (int k = 0; ok && more; ++k) {                   // (the last round publishes that there are no more)
-        {
+    if (warp == 8 || warp == 9) {
+      // ================= loads: warp 8 walks the share, publishes its items and loads Q and K; warp 9 loads V
+      const bool isV = warp == 9;
+      const int ppt = kTreeKeys >> P.bs_log2;              // pages of a key tile
+      const int pj = lane & (ppt - 1), h = lane / ppt;
+      const bool codes = F8 && isV;                        // to be widened: a ring of their own
+      const int ring = codes ? NR : isV ? NV : NK;
+      const CUtensorMap* tm = isV ? &tmV : &tmK;
+      const uint32_t dst0 = F8 ? (isV ? rV : sK) + (pj << P.bs_log2) * D
+                               : (isV ? sV : sK) + h * C::HALF_BYTES + (pj << P.bs_log2) * 128;
+      uint64_t* full = isV ? ctrl->v_full : ctrl->k_full;
+      bool any_bad = false, ok = true;
+      int c = 0, slot = 0;
+      auto load_tiles = [&](const TreeItem& it) {
+        const int32_t* row = P.block_table + static_cast<int64_t>(it.s) * P.MB;
+        const int npages = static_cast<int>((static_cast<int64_t>(it.keys) + (1 << P.bs_log2) - 1) >> P.bs_log2);
+        auto page_id = [&](int kt) {
+          const int i = kt * ppt + pj;
+          return i < npages ? __ldg(row + i) : -2;          // -2: past the end, filled with zeros
+        };
+        const int te = it.te, g = it.g;
+        int id_next = it.tb < te ? page_id(it.tb) : 0;
+        for (int kt = it.tb; kt < te; ++kt) {
+          int id = id_next;
+          if (kt + 1 < te) id_next = page_id(kt + 1);
+          const bool bad = id != -2 && (id < 0 || id >= P.NB);
+          const uint32_t badmask = __ballot_sync(0xffffffffu, bad && h == 0);
+          any_bad |= badmask != 0;
+          if (id < 0 || id >= P.NB) id = P.NB;              // out-of-bounds coordinate: TMA fills zeros, nothing is read
+          // the slot's previous tile: codes are free when they have been widened; K(c - NK) with step c - NK, V(c - NV) with
+          // step c - NV + LAG
+          if (c >= ring) {
+            if (codes) ok = wait(&ctrl->v_ok[(c - NR) & 7], (c - NR) >> 3);
+            else ok = wait(&ctrl->step[(isV ? c - NV + LAG : c - NK) & 7], (isV ? c - NV + LAG : c - NK) >> 3);
+            if (!ok) return;
+          }
+          const uint32_t bar = smem_u32(&full[c & 7]);
+          if (lane == 0) {
+            if (!isV) ctrl->page_bad[c & 15] = badmask;
+            mbar_arrive_expect_tx(bar, static_cast<uint32_t>(F8 ? C::RAW_BYTES : C::TILE_BYTES));
+          }
+          __syncwarp();
+          if constexpr (F8) {
+            if (h == 0) tma_load_4d(dst0 + slot * C::RAW_BYTES, tm, 0, 0, g, id, bar);
+          } else {
+            if (h < C::HALVES) tma_load_4d(dst0 + slot * C::TILE_BYTES, tm, h * 64, 0, g, id, bar);
+          }
+          if (++slot == ring) slot = 0;
+          ++c;
+        }
+      };
+      if (isV) {
+        const TreeItem* ip;
+        for (int k = 0; ok && get_item(k, ip); ++k) {
+          load_tiles(*ip);
+          done_item(k);
+        }
+      } else {
+        int4 rec[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};
+        int base = s0 & ~31;
+        TreeSeq win = tree_seq<PAIR>(P, base + lane);
+        int s = s0, u = u0, t = t0;
+        bool more = true, ran_out = false;
+        int nq = 0;
+        for (int k = 0; ok && more; ++k) {                   // (the last round publishes that there are no more)
           TreeItem it;
           it.s = -1;
           while (s < P.S && (s < s1 || (s == s1 && (u < u1 || (u == u1 && t < t1))))) {
@@ -416,6 +540,24 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             break;
           }
           more = it.s >= 0;
+          if (more && it.te > it.tb) {
+            // Q first: an MMA warp that finds nothing to do in an item is done with its Q at once, and must not be so for the
+            // buffer's next user before this wait has seen the last one
+            const int qb = nq % C::NQ;
+            ok = wait(&ctrl->q_free[qb], (nq / C::NQ) ^ 1);
+            if (!ok) break;
+            if (lane == 0) {
+              const uint32_t bar = smem_u32(&ctrl->q_full[qb]);
+              mbar_arrive_expect_tx(bar, static_cast<uint32_t>(QT * C::HALVES * P.TQ * P.G * 128));
+#pragma unroll
+              for (int i = 0; i < QT; ++i)
+#pragma unroll
+                for (int hh = 0; hh < C::HALVES; ++hh)
+                  tma_load_4d(sQ + (qb * QT + i) * C::Q_BYTES + hh * C::Q_HALF, &tmQ, hh * 64, 0, it.g, it.row0 + it.tok0 + i * P.TQ, bar);
+            }
+            __syncwarp();
+            ++nq;
+          }
           ok = wait(&ctrl->item_free[k % TR_ITEMS], (k / TR_ITEMS) ^ 1);
           if (!ok) break;
           if (lane == 0) {
@@ -424,195 +566,156 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             mbar_arrive(smem_u32(&ctrl->item_full[k % TR_ITEMS]));     // (release: the item is visible to whoever sees the phase)
           }
           __syncwarp();
-          const int now_k = more && it.te > it.tb ? k : -1, now_g = it.g, now_row = it.row0 + it.tok0;
-          // Q of the item before
-          if (pend_k >= 0) {
-            ok = wait(&ctrl->q_free, nq ^ 1);
-            if (ok && lane == 0) {
-              const uint32_t bar = smem_u32(&ctrl->q_full);
-              mbar_arrive_expect_tx(bar, static_cast<uint32_t>(QT * C::HALVES * P.TQ * P.G * 128));
-#pragma unroll
-              for (int i = 0; i < QT; ++i)
-#pragma unroll
-                for (int hh = 0; hh < C::HALVES; ++hh)
-                  tma_load_4d(sQ + i * C::TILE_BYTES + hh * C::HALF_BYTES, &tmQ, hh * 64, 0, pend_g, pend_row + i * P.TQ, bar);
-            }
-            __syncwarp();
-            if (ok) ++nq;
-          }
-          pend_k = now_k;
-          pend_g = now_g;
-          pend_row = now_row;
+          if (more) load_tiles(it);
         }
-      }
-      if (lane == 0) {
-        P.rec[2 * blockIdx.x] = rec[0];
-        P.rec[2 * blockIdx.x + 1] = rec[1];
-        if (ran_out) atomicOr(&P.hdr->err, ERR_BAD_PAGE);
-        if (!ok) fail();
-      }
-      // given up: no copy may still be on its way into this CTA's shared memory when it ends
-      if (*reinterpret_cast<const volatile uint32_t*>(abort_flag) && nq > 0) mbar_wait(smem_u32(&ctrl->q_full), (nq - 1) & 1);
-    } else if (warp == 10 || warp == 11) {
-      // ================= loads: K (warp 10), V (warp 11)
-      const bool isV = warp == 11;
-      const int ppt = kTreeKeys >> P.bs_log2;              // pages of a key tile
-      const int j = lane & (ppt - 1), h = lane / ppt;
-      const int ring = F8 ? NR : isV ? NV : NK;
-      const CUtensorMap* tm = isV ? &tmV : &tmK;
-      const uint32_t dst0 = F8 ? (isV ? rV : rK) + (j << P.bs_log2) * D
-                               : (isV ? sV : sK) + h * C::HALF_BYTES + (j << P.bs_log2) * 128;
-      const int slot_bytes = F8 ? C::RAW_BYTES : C::TILE_BYTES;
-      uint64_t* full = isV ? ctrl->v_full : ctrl->k_full;
-      bool any_bad = false, ok = true;
-      int c = 0, slot = 0;
-      const TreeItem* ip;
-      for (int k = 0; ok && get_item(k, ip); ++k) {
-        const TreeItem& it = *ip;
-        const int32_t* row = P.block_table + static_cast<int64_t>(it.s) * P.MB;
-        const int npages = static_cast<int>((static_cast<int64_t>(it.keys) + (1 << P.bs_log2) - 1) >> P.bs_log2);
-        auto page_id = [&](int kt) {
-          const int i = kt * ppt + j;
-          return i < npages ? __ldg(row + i) : -2;          // -2: past the end, filled with zeros
-        };
-        const int te = it.te, g = it.g;
-        int id_next = it.tb < te ? page_id(it.tb) : 0;
-        for (int kt = it.tb; kt < te; ++kt) {
-          int id = id_next;
-          if (kt + 1 < te) id_next = page_id(kt + 1);
-          const bool bad = id != -2 && (id < 0 || id >= P.NB);
-          const uint32_t badmask = __ballot_sync(0xffffffffu, bad && h == 0);
-          any_bad |= badmask != 0;
-          if (id < 0 || id >= P.NB) id = P.NB;              // out-of-bounds coordinate: TMA fills zeros, nothing is read
-          // the slot's previous tile: codes are free when they have been widened; K(c - NK) with step c - NK, V(c - NV) with
-          // step c - NV + LAG
-          if (c >= ring) {
-            if (F8) ok = wait(isV ? &ctrl->v_ok[(c - ring) & 7] : &ctrl->k_ok[(c - ring) & 7], (c - ring) >> 3);
-            else ok = wait(&ctrl->step[(isV ? c - NV + LAG : c - NK) & 7], (isV ? c - NV + LAG : c - NK) >> 3);
-            if (!ok) break;
-          }
-          const uint32_t bar = smem_u32(&full[c & 7]);
-          if (lane == 0) {
-            if (!isV) ctrl->page_bad[c & 7] = badmask;
-            mbar_arrive_expect_tx(bar, static_cast<uint32_t>(slot_bytes));
-          }
-          __syncwarp();
-          if constexpr (F8) {
-            if (h == 0) tma_load_4d(dst0 + slot * C::RAW_BYTES, tm, 0, 0, g, id, bar);
-          } else {
-            if (h < C::HALVES) tma_load_4d(dst0 + slot * C::TILE_BYTES, tm, h * 64, 0, g, id, bar);
-          }
-          if (++slot == ring) slot = 0;
-          ++c;
+        if (lane == 0) {
+          P.rec[2 * blockIdx.x] = rec[0];
+          P.rec[2 * blockIdx.x + 1] = rec[1];
+          if (ran_out) atomicOr(&P.hdr->err, ERR_BAD_PAGE);
         }
-        done_item(k);
+        // given up: no copy may still be on its way into this CTA's shared memory when it ends
+        if (*reinterpret_cast<const volatile uint32_t*>(abort_flag))
+          for (int i = max(0, nq - C::NQ); i < nq; ++i) mbar_wait(smem_u32(&ctrl->q_full[i % C::NQ]), (i / C::NQ) & 1);
       }
       if (lane == 0) {
         if (any_bad) atomicOr(&P.hdr->err, ERR_BAD_PAGE);
         if (!ok) fail();
       }
-      // given up: see above
       if (*reinterpret_cast<const volatile uint32_t*>(abort_flag))
         for (int i = max(0, c - ring); i < c; ++i) mbar_wait(smem_u32(&full[i & 7]), (i >> 3) & 1);
-    } else if (warp == 8) {
-      // ================= MMA issue: the warp runs the loop as one, one elected lane issues
+    } else if (warp == 10 || warp == 11) {
+      // ================= MMA issue, a warp per group: one thread waits and issues.  It has the scores of at most two key tiles out at a
+      // time, one per buffer, and takes what comes first: the weights of the older one (their product), or the next K tile (its
+      // scores), which may belong to the next item.
+      const int t = warp - 10;
       uint32_t elected;
       asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(elected));
-      const TreeItem* ip;
-      int c = 0, kslot = 0, vslot = 0;   // key tiles of this CTA so far; ring slots of K(c) and of the next V
-      uint32_t nq = 0, np = 0;           // parity of q; bit t: parity of p_part of group t
-      int nv = 0;                        // products so far
-      bool ok = true;
-      constexpr uint32_t ID_S = F8 ? umma_idesc_f16(128, kTreeKeys) : umma_idesc(128, kTreeKeys, 0, 0);   // Q x K tile, both K-major
-      constexpr uint32_t ID_O = F8 ? umma_idesc_f16(128, D) : umma_idesc(128, D, 0, 1);   // P (tensor memory) x V (MN-major; fp8: K-major)
-      const uint64_t q_desc = umma_desc(sQ, 16, 1024), k_desc = umma_desc(sK, 16, 1024);
-      const uint64_t v_desc = F8 ? umma_desc(sV, 16, 1024) : umma_desc(sV, C::HALF_BYTES, 1024);
-      for (int k = 0; ok && get_item(k, ip); ++k) {
-        const int n = tree_uniform(ip->te - ip->tb);
-        const uint32_t active = PAIR ? 1u | (tree_uniform(ip->rows[1]) > 0 ? 2u : 0u) : 3u;
-        done_item(k);
-        if (n <= 0) continue;
-        for (int j = 0; j < n + LAG && ok; ++j) {
-          const uint32_t turn = PAIR ? active : 1u << (j & 1);        // groups that key tiles j and j - LAG belong to
-          if (j >= LAG) ok = wait(&ctrl->v_ok[nv & 7], nv >> 3);
-          if (ok && j < n) ok = wait(F8 ? &ctrl->k_ok[c & 7] : &ctrl->k_full[c & 7], c >> 3);
-          if (ok && j == 0) {
-            ok = wait(F8 ? &ctrl->q_ok : &ctrl->q_full, nq);
-            nq ^= 1;
-          }
-#pragma unroll 1
-          for (int t = 0; t < 2 && ok; ++t) {
-            if (!((turn >> t) & 1)) continue;
-            const uint32_t tS = tbase + C::COL_S + t * 128, tO = tbase + C::COL_O + t * D;
-            if (j >= LAG) {
-              // O_t (+)= P_t . V of key tile j - LAG; the first half runs while the second is still being made
-              uint64_t vd = v_desc + static_cast<uint64_t>(tree_uniform(vslot) * (C::TILE_BYTES >> 4));
-              uint32_t accum = j >= 2 * LAG ? 1u : 0u, a = tS;
-#pragma unroll 1
-              for (int h = 0; h < 2; ++h) {
-                ok = wait(&ctrl->p_part[t][h], np >> t);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  umma_ts_elected(tO, a, vd + (F8 ? i * 2 : i * (2048 >> 4)), ID_O, accum, elected);
-                  accum = 1u;
-                  a += 8;
-                }
-                vd += F8 ? (D * 128) >> 4 : 4 * (2048 >> 4);
-              }
-              if (!ok) break;
-              np ^= 1u << t;
-              if (j >= n) tc_commit_elected(smem_u32(&ctrl->o_full[t]), elected);   // that was this group's last
+      if (elected) {
+        // Q x K tile, both K-major; fp8: two terms of Q, one after the other, against the codes
+        constexpr uint32_t ID_S = F8 ? umma_idesc_f16(128, kTreeKeys) : umma_idesc(128, kTreeKeys, 0, 0);
+        constexpr uint32_t ID_O = F8 ? umma_idesc_f16(128, D) : umma_idesc(128, D, 0, 1);   // P (tensor memory) x V (MN-major; fp8: K-major)
+        constexpr int STRIDE = PAIR ? 1 : 2;       // from one key tile of this group to the next
+        const uint64_t q_desc = F8 ? umma_desc_rows<D>(sQP + (PAIR ? t : 0) * C::Q_BYTES) : umma_desc(sQ + (PAIR ? t : 0) * C::Q_BYTES, 16, 1024);
+        const uint64_t k_desc = F8 ? umma_desc_rows<D>(sK) : umma_desc(sK, 16, 1024);
+        const uint64_t v_desc = F8 ? umma_desc(sV, 16, 1024) : umma_desc(sV, C::HALF_BYTES, 1024);
+        const uint32_t tS0 = tbase + C::COL_S + t * 128, tO = tbase + C::COL_O + t * D;
+        uint32_t np = 0;                           // bit b: parity of p_full of buffer b
+        int out = 0, v0 = 0, v1 = 0;               // key tiles whose product is to come: how many, the older and the younger
+        bool open0 = false, open1 = false;         // ... and whether it begins O anew
+        int c = PAIR ? 0 : t, end = 0;             // this group's next key tile; end of the present item
+        int first = 0, k = 0, nq = 0;              // its first key tile; items so far, those with key tiles
+        bool active = false, more = true, ok = true;
+        unsigned long long since = 0ull;
+        uint32_t idle = 0;
+        while (ok && (more || out > 0)) {
+          bool moved = false;
+          if (out > 0) {
+            // O (+)= P . V of the older key tile.  Nothing else can be done while both buffers are taken.
+            const int b = (PAIR ? v0 : v0 >> 1) & 1;
+            const uint32_t bar_v = smem_u32(&ctrl->v_ok[v0 & 7]), bar_p = smem_u32(&ctrl->p_full[t][b]);
+            bool ready;
+            if (out == 2 || !more) {
+              ok = tree_wait(bar_v, (v0 >> 3) & 1, abort_flag) && tree_wait(bar_p, (np >> b) & 1u, abort_flag);
+              ready = ok;
+            } else {
+              ready = mbar_test_wait(bar_p, (np >> b) & 1u) && mbar_test_wait(bar_v, (v0 >> 3) & 1);
             }
-            if (j < n) {
+            if (ready) {
+              np ^= 1u << b;
               tc_fence_after();
-              uint64_t kd = k_desc + static_cast<uint64_t>(tree_uniform(kslot) * (C::TILE_BYTES >> 4));
-              uint64_t qd = q_desc + static_cast<uint64_t>(PAIR ? t * (C::TILE_BYTES >> 4) : 0);
-              uint32_t accum = 0u;
-#pragma unroll 1
-              for (int hh = 0; hh < C::HALVES; ++hh) {
+              const uint64_t vd = v_desc + static_cast<uint64_t>((v0 % NV) * (C::TILE_BYTES >> 4));
+              uint32_t accum = open0 ? 0u : 1u;
 #pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                  umma_ss_elected(tS, qd + kk * 2, kd + kk * 2, ID_S, accum, elected);
-                  accum = 1u;
-                }
-                qd += C::HALF_BYTES >> 4;
-                kd += C::HALF_BYTES >> 4;
+              for (int i = 0; i < kTreeKeys / 16; ++i) {
+                umma_ts(tO, tS0 + b * 64 + i * 8, vd + (F8 ? i * 2 : i * (2048 >> 4)), ID_O, accum);
+                accum = 1u;
               }
-              tc_commit_elected(smem_u32(&ctrl->s_full[t]), elected);
+              tc_commit(smem_u32(&ctrl->pv_done[t][b]));
+              v0 = v1;
+              open0 = open1;
+              --out;
+              moved = true;
             }
           }
-          if (!ok) break;
-          if (j >= LAG) {
-            ++nv;
-            if (++vslot == NV) vslot = 0;
+          if (more && c >= end) {
+            // the item is through (this group's scores of it are issued), or it had no key tile for this group
+            if (mbar_test_wait(smem_u32(&ctrl->item_full[k % TR_ITEMS]), (k / TR_ITEMS) & 1)) {
+              const TreeItem& it = ctrl->item[k % TR_ITEMS];
+              const int n = it.te - it.tb;
+              more = it.s >= 0;
+              active = !PAIR || it.rows[t] > 0;
+              mbar_arrive(smem_u32(&ctrl->item_free[k % TR_ITEMS]));
+              ++k;
+              moved = true;
+              if (more && n > 0) {
+                first = end;
+                end += n;
+                ++nq;
+                if (c >= end) tc_commit(smem_u32(&ctrl->q_free[(nq - 1) % C::NQ]));
+              }
+            }
+          } else if (more && (out == 0 || v0 > c - LAG)) {
+            const int qb = (nq - 1) % C::NQ, b = (PAIR ? c : c >> 1) & 1;
+            if (mbar_test_wait(smem_u32(&ctrl->k_full[c & 7]), (c >> 3) & 1) &&
+                (!active || mbar_test_wait(smem_u32(F8 ? &ctrl->q_ok[qb] : &ctrl->q_full[qb]), ((nq - 1) / C::NQ) & 1))) {
+              if (active) {
+                tc_fence_after();
+                uint64_t kd = k_desc + static_cast<uint64_t>((c % NK) * (C::K_BYTES >> 4));
+                uint64_t qd = q_desc + static_cast<uint64_t>(qb * QT * (C::Q_BYTES >> 4));
+                uint32_t accum = 0u;
+#pragma unroll
+                for (int hh = 0; hh < (F8 ? 2 : C::HALVES); ++hh) {
+#pragma unroll
+                  for (int kk = 0; kk < (F8 ? D / 32 : 4); ++kk) {
+                    if constexpr (F8) umma_ss_f8(tS0 + b * 64, qd + kk * 2, kd + kk * 2, ID_S, accum);
+                    else umma_ss(tS0 + b * 64, qd + kk * 2, kd + kk * 2, ID_S, accum);
+                    accum = 1u;
+                  }
+                  qd += F8 ? (128 * D) >> 4 : C::Q_HALF >> 4;
+                  if (!F8) kd += C::HALF_BYTES >> 4;
+                }
+                tc_commit(smem_u32(&ctrl->s_full[t][b]));
+                const bool opens = c - first < STRIDE;
+                if (out == 0) {
+                  v0 = c;
+                  open0 = opens;
+                } else {
+                  v1 = c;
+                  open1 = opens;
+                }
+                ++out;
+              }
+              // this group's scores of c and product of c - LAG
+              tc_commit(smem_u32(&ctrl->step[c & 7]));
+              c += STRIDE;
+              if (c >= end) tc_commit(smem_u32(&ctrl->q_free[qb]));    // this group's scores of the item
+              moved = true;
+            }
           }
-          if (j < n) {
-            if (j == n - 1) tc_commit_elected(smem_u32(&ctrl->q_free), elected);
-            // the scores of c and the product of c - LAG (an earlier item's last ones included)
-            tc_commit_elected(smem_u32(&ctrl->step[c & 7]), elected);
-            ++c;
-            if (++kslot == NK) kslot = 0;
+          if (moved) {
+            idle = 0;
+          } else if ((++idle & 63u) == 0u) {
+            const unsigned long long now = globaltimer_ns();
+            if (idle == 64u) since = now;
+            ok = ok && !*reinterpret_cast<const volatile uint32_t*>(abort_flag) && now - since <= kWaitLimitNs;
           }
         }
+        if (!ok) fail();
+        // nothing that was issued may still be running on the tensor cores when the tensor memory goes back
+        tc_commit(smem_u32(&ctrl->drained[t]));
+        mbar_wait(smem_u32(&ctrl->drained[t]), 0);
       }
-      if (lane == 0 && !ok) fail();
-      // nothing that was issued may still be running on the tensor cores when the tensor memory goes back
-      tc_commit_elected(smem_u32(&ctrl->drained), elected);
-      mbar_wait(smem_u32(&ctrl->drained), 0);
       __syncwarp();
     } else if (F8) {
-      // ================= widening, warps 12-15: a thread moves 16 codes at a time.  K of the next key tile comes before V of this one.
+      // ================= warps 12-15: Q split into two e4m3 terms, V widened to fp16, 16 codes at a time
       const int w = warp - 12, id = w * 32 + lane;
       const TreeItem* ip;
-      int c = 0, nq = 0;
-      int rk = 0, rv = 0, ok_ = 0, ov = 0;                 // ring slots: codes of K, of V; K, V
-      int nv = 0, meets = 0;
+      int nq = 0, nv = 0, rv = 0, ov = 0, meets = 0;       // items with key tiles; V tiles; ring slots of V's codes and of V
       bool ok = true;
-      auto widen = [&](uint32_t src, uint32_t d0, uint32_t d1) {     // 16 codes to two 16-byte chunks; returns whether one is NaN
-        uint32_t x[4];
+      auto load16 = [&](uint32_t src, uint32_t (&x)[4]) {    // 16 codes
         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(src) : "memory");
+      };
+      auto widen = [&](const uint32_t (&x)[4], uint32_t d0, uint32_t d1) {     // ... to two 16-byte chunks
         uint32_t y[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = cvt_e4m3x2_f16x2(x[i >> 1] >> (16 * (i & 1)));
@@ -625,98 +728,146 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         if (lane == 0) mbar_arrive(smem_u32(bar));
       };
       auto do_v = [&](int edge_tile, int v) {
-        // V(v): codes [page][d][slot], linear; tile [64-key block][d][64 keys]
+        // V(v): codes [page][d][slot], linear; tile [d][64 keys]
         ok = ok && wait(&ctrl->v_full[v & 7], v >> 3);
         if (ok && v >= NV) ok = wait(&ctrl->step[(v - NV + LAG) & 7], (v - NV + LAG) >> 3);
         if (!ok) return;
         const uint32_t src = rV + rv * C::RAW_BYTES, dst = sV + ov * C::TILE_BYTES;
         if (edge_tile) {
-          // the guard: which keys hold a NaN code
-          // warp w looks at keys 32 w .. + 31, all of d
+          // the guard: which keys hold a NaN code.  Warp w looks at keys 16 w .. + 15, all of d
           uint32_t bad = 0u;
 #pragma unroll 1
-          for (int i = lane; i < 2 * D; i += 32) {         // 16 keys of one d
-            const int key = w * 32 + (i / D) * 16, dd = i % D;
-            const int page = key >> P.bs_log2, in = key & ((1 << P.bs_log2) - 1);
-            uint32_t x[4];
-            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                         : "r"(src + ((page * D + dd) << P.bs_log2) + in) : "memory");
+          for (int dd = lane; dd < D; dd += 32) {
+            const int key = w * 16, page = key >> P.bs_log2, in = key & ((1 << P.bs_log2) - 1);
+            const uint32_t from = src + ((page * D + dd) << P.bs_log2) + in;
+            uint32_t x[4], mine = 0u;
+            asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(from) : "memory");
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               // a byte is NaN when its low seven bits are all set: adding one carries into the eighth
               const uint32_t hit = ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-              if (hit) {
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                  if (hit >> (8 * b + 7) & 1u) bad |= 1u << ((i / D) * 16 + e * 4 + b);
-                x[e] &= ~((hit >> 7) * 0xffu);
-              }
+              for (int i = 0; i < 4; ++i) mine |= (hit >> (8 * i + 7) & 1u) << (e * 4 + i);
+              x[e] &= ~((hit >> 7) * 0xffu);
             }
             // (written back: the widening below reads it, by other warps too)
-            if (bad)
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(src + ((page * D + dd) << P.bs_log2) + in), "r"(x[0]), "r"(x[1]),
-                           "r"(x[2]), "r"(x[3]) : "memory");
+            if (mine)
+              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(from), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
+            bad |= mine;
           }
           bad = __reduce_or_sync(0xffffffffu, bad);
-          if (lane == 0) ctrl->v_bad[v & 7][w] = bad;
+          if (lane == 0) reinterpret_cast<uint16_t*>(ctrl->v_bad[v & 7])[w] = static_cast<uint16_t>(bad);
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&ctrl->meet_widen));
           ok = wait(&ctrl->meet_widen, meets++);           // (bounded, unlike a named barrier)
           if (!ok) return;
         }
-#pragma unroll 4
-        for (int i = id; i < D * 8; i += 128) {            // chunk i of 16 codes, as they lie
-          const int page = (i << 4) / (D << P.bs_log2), in_page = (i << 4) - page * (D << P.bs_log2);
+        constexpr int NC = D * 4 / 128;                    // chunks of 16 codes a thread moves: all loads, then all stores
+        uint32_t x[NC][4];
+#pragma unroll
+        for (int e = 0; e < NC; ++e) load16(src + ((e * 128 + id) << 4), x[e]);
+#pragma unroll
+        for (int e = 0; e < NC; ++e) {
+          const int i = e * 128 + id;                      // chunk i, as they lie
+          const int page = (i << 4) >> (P.bs_log2 + (D == 128 ? 7 : 6)), in_page = (i << 4) - page * (D << P.bs_log2);
           const int dd = in_page >> P.bs_log2, key = (page << P.bs_log2) + (in_page & ((1 << P.bs_log2) - 1));
-          const uint32_t row = dst + (key >> 6) * (D * 128) + dd * 128;
-          const int ch = (key & 63) >> 3;
-          widen(src + (i << 4), row + ((ch ^ (dd & 7)) << 4), row + (((ch + 1) ^ (dd & 7)) << 4));
+          const uint32_t row = dst + dd * 128;
+          const int ch = key >> 3;
+          widen(x[e], row + ((ch ^ (dd & 7)) << 4), row + (((ch + 1) ^ (dd & 7)) << 4));
         }
         publish(&ctrl->v_ok[v & 7]);
         if (++rv == NR) rv = 0;
         if (++ov == NV) ov = 0;
       };
+      // Row `id` of a row tile of Q: q = 2^-e (q1 + q2), q1 = e4m3(2^e q), q2 = e4m3 of the rest, with 2^e the power of two that brings the
+      // row's largest magnitude to (224, 448].  A bf16 has 8 bits, the terms 4 and 4: exact down to 2^-9 of the largest, and off by
+      // at most 2^-10 * 2^-e below.  An element that is not finite becomes NaN.
+      auto read64 = [&](uint32_t src, uint32_t (&x)[32]) {    // 64 elements of the row
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[4 * i]), "=r"(x[4 * i + 1]), "=r"(x[4 * i + 2]), "=r"(x[4 * i + 3])
+                       : "r"(src + ((i ^ (id & 7)) << 4)) : "memory");
+      };
+      auto largest = [&](const uint32_t (&x)[32]) {           // magnitudes as whole numbers; NaN and infinities do not count
+        uint32_t top = 0u;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const uint32_t lo = (x[i] << 16) & 0x7fffffffu, hi = x[i] & 0x7fff0000u;
+          top = max(top, max(lo < 0x7f800000u ? lo : 0u, hi < 0x7f800000u ? hi : 0u));
+        }
+        return top;
+      };
+      auto terms = [&](uint32_t u, float up, uint32_t& t1, uint32_t& t2) {   // of two elements
+        float a = __uint_as_float(u << 16) * up, b = __uint_as_float(u & 0xffff0000u) * up;
+        a = fabsf(a) <= 448.f ? a : __int_as_float(0x7fffffff);
+        b = fabsf(b) <= 448.f ? b : __int_as_float(0x7fffffff);
+        unsigned short q1, q2;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q1) : "f"(b), "f"(a));
+        const uint32_t back = cvt_e4m3x2_f16x2(q1);
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q2) : "f"(b - f.y), "f"(a - f.x));
+        t1 = q1;
+        t2 = q2;
+      };
+      auto put64 = [&](uint32_t row, int i0, const uint32_t (&y)[16]) {      // 64 codes from chunk i0 of a row on
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t at = static_cast<uint32_t>(D == 128 ? (i0 + i) ^ (id & 7) : i ^ ((id >> 1) & 3)) << 4;
+          asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(row + at), "r"(y[4 * i]), "r"(y[4 * i + 1]), "r"(y[4 * i + 2]),
+                       "r"(y[4 * i + 3]) : "memory");
+        }
+      };
+      auto split64 = [&](const uint32_t (&x)[32], float up, uint32_t (&y1)[16], uint32_t (&y2)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          uint32_t a1, a2, b1, b2;
+          terms(x[2 * i], up, a1, a2);
+          terms(x[2 * i + 1], up, b1, b2);
+          y1[i] = a1 | (b1 << 16);
+          y2[i] = a2 | (b2 << 16);
+        }
+      };
+      auto split_row = [&](int tile) {
+        const uint32_t src = sQ + tile * C::Q_BYTES + id * 128;
+        uint32_t x[32], y1[16], y2[16];
+        uint32_t top = 0u;
+#pragma unroll 1
+        for (int h = 0; h < C::HALVES; ++h) {
+          read64(src + h * C::Q_HALF, x);
+          top = max(top, largest(x));
+        }
+        int e = 135 - static_cast<int>(top >> 23) - ((top & 0x7fffffu) > 0x600000u ? 1 : 0);   // 448 = 1.75 * 2^8
+        e = top == 0u ? 0 : min(126, e);
+        const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
+        q_scale[tile * 128 + id] = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        // the terms' rows; with head_dim 128 they lie over the row itself: a half's second terms wait until the other half is read
+        const uint32_t d1 = sQP + tile * C::Q_BYTES + id * D, d2 = d1 + 128 * D;
+        read64(src, x);
+        split64(x, up, y1, y2);
+        put64(d1, 0, y1);
+        if constexpr (D == 128) {
+          read64(src + C::Q_HALF, x);
+          put64(d2, 0, y2);
+          split64(x, up, y1, y2);
+          put64(d1, 4, y1);
+          put64(d2, 4, y2);
+        } else {
+          put64(d2, 0, y2);
+        }
+      };
       for (int k = 0; ok && get_item(k, ip); ++k) {
         const TreeItem& it = *ip;
         const int tb = it.tb, te = it.te, edge = it.edge;
-        for (int kt = tb; kt < te && ok; ++kt) {
-          // K(c): codes [key][d], rows swizzled by the copy; tile [64-element block][key][64]
-          ok = wait(&ctrl->k_full[c & 7], c >> 3);
-          if (ok && c >= NK) ok = wait(&ctrl->step[(c - NK) & 7], (c - NK) >> 3);
+        if (te > tb) {
+          const int qb = nq % C::NQ;
+          ok = wait(&ctrl->q_full[qb], nq / C::NQ);
+          ++nq;
           if (!ok) break;
-          {
-            const uint32_t src = rK + rk * C::RAW_BYTES + id * D, dst = sK + ok_ * C::TILE_BYTES + id * 128;   // key `id`
-#pragma unroll 4
-            for (int i = 0; i < D / 16; ++i) {
-              const int from = D == 128 ? i ^ (id & 7) : i ^ ((id >> 1) & 3);
-              const uint32_t row = dst + (i >> 2) * C::HALF_BYTES;
-              const int ch = (i & 3) * 2;
-              widen(src + (from << 4), row + ((ch ^ (id & 7)) << 4), row + (((ch + 1) ^ (id & 7)) << 4));
-            }
-          }
-          publish(&ctrl->k_ok[c & 7]);
-          if (++rk == NR) rk = 0;
-          if (++ok_ == NK) ok_ = 0;
-          if (kt == tb) {
-            // Q in place, bf16 to fp16
-            ok = wait(&ctrl->q_full, nq);
-            nq ^= 1;
-            if (!ok) break;
 #pragma unroll 1
-            for (int i = id; i < QT * C::TILE_BYTES / 16; i += 128) {
-              uint32_t x[4];
-              asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(sQ + i * 16) : "memory");
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = pack_f16x2(__uint_as_float(x[e] << 16), __uint_as_float(x[e] & 0xffff0000u));
-              asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(sQ + i * 16), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
-            }
-            publish(&ctrl->q_ok);
-          } else {
-            do_v(kt - 1 >= edge, nv++);
-          }
-          ++c;
+          for (int i = 0; i < QT; ++i) split_row(qb * QT + i);
+          publish(&ctrl->q_ok[qb]);
         }
-        if (te > tb && ok) do_v(te - 1 >= edge, nv++);
+        for (int kt = tb; kt < te && ok; ++kt) do_v(kt >= edge, nv++);
         done_item(k);
       }
       if (!ok && lane == 0) fail();
@@ -734,11 +885,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           if (!ok) break;
           if (kt >= edge) {
             const uint32_t base = sV + slot * C::TILE_BYTES;
-#pragma unroll 1
-            for (int e = 0; e < 2; ++e) {
+            {
               // 32 keys: a key's row of a 64-column block is 128 bytes = 8 chunks, four keys per warp-wide load.  A bf16 is not
               // finite when its eight exponent bits are all set: adding one to them then carries into the sign's place.
-              const uint32_t rows = base + (w * 2 + e) * 32 * 128;
+              const uint32_t rows = base + w * 32 * 128;
               uint32_t bad = 0u;
 #pragma unroll 1
               for (int hq = 0; hq < C::HALVES * 8; ++hq) {
@@ -759,7 +909,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 }
               }
               bad = __reduce_or_sync(0xffffffffu, bad);
-              if (lane == 0) ctrl->v_bad[c & 7][w * 2 + e] = bad;
+              if (lane == 0) ctrl->v_bad[c & 7][w] = bad;
             }
             fence_proxy_async();         // the stores above before the tensor cores' reads
             __syncwarp();
@@ -792,7 +942,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       wait_all(&ctrl->meet, meets++);
     };
     const TreeItem* ip;
-    int c0 = 0, nt = 0, no = 0;        // key tiles of the CTA before this item; of this group; items of this group that had keys
+    int c0 = 0, nq = 0;                // key tiles of the CTA before this item; items with key tiles
+    uint32_t ns = 0;                   // bit b: parity of s_full (and of p_full, pv_done) of this group's buffer b
     for (int k = 0; get_item(k, ip); ++k) {
       const TreeItem& it = *ip;
       const int tb = it.tb, te = it.te, edge = it.edge, rows = it.rows[t], keys = it.keys;
@@ -808,122 +959,114 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       float sc = P.scale_log2 * (F8 ? __ldg(P.k_scale + it.g) : 1.f);
       const bool flip = sc < 0.f;
       sc = fabsf(sc);
+      if (F8 && te > tb) {
+        const int qb = nq % C::NQ;
+        wait_all(&ctrl->q_ok[qb], nq / C::NQ);
+        sc *= q_scale[(qb * QT + (PAIR ? t : 0)) * 128 + r];
+        ++nq;
+      }
       if (sc == 0.f) sc = 1.1754944e-38f;               // (all weights alike; 0 * inf would be NaN)
-      float m = NEG_INF, l = 0.f;
+      float m = NEG_INF, mu = 0.f, l = 0.f;             // running maximum (reference), the same or 0 in its place; sum
       bool odd = false;                                 // this row sees a key with a non-finite V
-      for (int kt = PAIR ? tb : tb + t; mine && kt < te; kt += PAIR ? 1 : 2) {
-        const int c = c0 + (kt - tb);
-        wait_all(&ctrl->s_full[t], nt);
-        tc_fence_after();
-        const bool first = kt == (PAIR ? tb : tb + t);
-        ++nt;
+      int last = -1;                                    // this group's last buffer in use
+      const int own = PAIR ? tb : tb + ((c0 ^ t) & 1);  // split: group t has the key tiles whose number in the CTA has its parity
+      for (int kt = own; mine && kt < te; kt += PAIR ? 1 : 2) {
+        const int c = c0 + (kt - tb), b = (PAIR ? c : c >> 1) & 1;
+        const bool first = last < 0;
+        wait_all(&ctrl->s_full[t][b], ns >> b);
         if (!busy) {
-          if (lane < 2) mbar_arrive(smem_u32(&ctrl->p_part[t][lane]));
+          if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_full[t][b]));
+          ns ^= 1u << b;
+          last = b;
           continue;
         }
-        // Two passes over the scores, 32 columns at a time, so that the loops stay small; the next columns are on their way while
-        // these are worked on.  The first pass takes the maximum, and where scores are masked it writes them back; the second makes
-        // the weights, whose columns 16 q .. + 15 lie over scores that have been read.
-        uint32_t x0[32], x1[32];
-        auto first_pass = [&](auto masked_) {
-          constexpr bool MASKED = decltype(masked_)::value;
-          const uint32_t pb = MASKED ? ctrl->page_bad[c & 7] : 0u;
-          float m4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
-          auto columns = [&](uint32_t (&x)[32], int q) {
-            if (MASKED) {
-              const int k0 = kt * kTreeKeys + q * 32;
-              uint32_t vis = sees ? tree_visible(k0, at, keys, mask) : 0u;
-              if (pb) {
-                if (P.bs_log2 == 4) vis &= ~(((pb >> (2 * q)) & 1u ? 0xffffu : 0u) | ((pb >> (2 * q + 1)) & 1u ? 0xffff0000u : 0u));
-                else if ((pb >> (q >> (P.bs_log2 - 5))) & 1u) vis = 0u;
-              }
-              if (flip) {
+        tc_fence_after();
+        uint32_t x[64];
+        tmem_ld32(tS + b * 64, *reinterpret_cast<uint32_t(*)[32]>(&x[0]));
+        tmem_ld32(tS + b * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(&x[32]));
+        tc_wait_ld();
+        const uint32_t pb = ctrl->page_bad[c & 15];
+        if (kt >= edge || flip || pb != 0) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] ^= 0x80000000u;
-              }
+          for (int q = 0; q < 2; ++q) {
+            uint32_t vis = sees ? tree_visible(kt * kTreeKeys + q * 32, at, keys, mask) : 0u;
+            if (P.bs_log2 == 4) vis &= ~(((pb >> (2 * q)) & 1u ? 0xffffu : 0u) | ((pb >> (2 * q + 1)) & 1u ? 0xffff0000u : 0u));
+            else if ((pb >> (q >> (P.bs_log2 - 5))) & 1u) vis = 0u;
+            if (flip) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (!((vis >> i) & 1u)) x[i] = __float_as_uint(NEG_INF);
-              tmem_st32(tS + q * 32, x);
+              for (int i = 0; i < 32; ++i) x[q * 32 + i] ^= 0x80000000u;
             }
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
-          };
-          tmem_ld32(tS, x0);
-#pragma unroll 1
-          for (int q = 0; q < 4; q += 2) {
-            tc_wait_ld();
-            tmem_ld32(tS + q * 32 + 32, x1);
-            columns(x0, q);
-            tc_wait_ld();
-            if (q == 0) tmem_ld32(tS + 64, x0);
-            columns(x1, q + 1);
+            for (int i = 0; i < 32; ++i)
+              if (!((vis >> i) & 1u)) x[q * 32 + i] = __float_as_uint(NEG_INF);
           }
-          if (MASKED) tc_wait_st();
-          return fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
-        };
-        const bool masked = kt >= edge || flip || ctrl->page_bad[c & 7] != 0;
-        float mx = masked ? first_pass(std::true_type{}) : first_pass(std::false_type{});
-        tmem_ld32(tS, x0);                              // (for the second pass)
-        mx = mx == NEG_INF ? NEG_INF : mx * sc;
-        const bool grow = first || mx > m + 8.f;
-        const float m_new = grow ? fmaxf(m, mx) : m;
-        const float mu = m_new == NEG_INF ? 0.f : m_new;
-        const float alpha = grow ? fast_exp2(m - mu) : 1.f;
-        m = m_new;
-        if (__any_sync(0xffffffffu, valid && !first && alpha != 1.f)) {
-          // new reference: scale this row of O.  PAIR: the product before this one was done when the scores came; split: so it
-          // was, the scores of this tile were issued behind it.
-#pragma unroll 1
-          for (int q = 0; q < D / 16; ++q) {
-            uint32_t o[16];
-            tmem_ld16(tO + q * 16, o);
-            tc_wait_ld();
+          if (kt >= edge) {
+            // before the weights go, for they let the guard's word be written anew: does this row see a guarded key?
+            wait_all(&ctrl->v_ok[c & 7], c >> 3);
+            if (sees) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-            tmem_st16(tO + q * 16, o);
+              for (int q = 0; q < 2; ++q)
+                odd |= (*reinterpret_cast<volatile uint32_t*>(&ctrl->v_bad[c & 7][q]) &
+                        tree_visible(kt * kTreeKeys + 32 * q, at, keys, mask)) != 0u;
+            }
+          }
+        }
+        float m4[4] = {NEG_INF, NEG_INF, NEG_INF, NEG_INF};
+#pragma unroll
+        for (int i = 0; i < 64; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+        float mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
+        mx = mx == NEG_INF ? NEG_INF : mx * sc;
+        float alpha = 1.f;
+        // the reference moves with the first tile, and when the maximum grew by more than 2^8
+        if (__any_sync(0xffffffffu, valid && (first || mx > m + 8.f))) {
+          const bool grow = first || mx > m + 8.f;
+          const float m_new = grow ? fmaxf(m, mx) : m;
+          mu = m_new == NEG_INF ? 0.f : m_new;
+          alpha = grow ? fast_exp2(m - mu) : 1.f;
+          m = m_new;
+          if (!first) {
+            // scale this row of O, once the product before this one is done
+            wait_all(&ctrl->pv_done[t][last], (ns >> last) ^ 1u);
+            tc_fence_after();
+#pragma unroll 1
+            for (int q = 0; q < D / 16; ++q) {
+              uint32_t o[16];
+              tmem_ld16(tO + q * 16, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+              tmem_st16(tO + q * 16, o);
+            }
           }
         }
         uint64_t sum0 = 0ull, sum1 = 0ull;
         const uint64_t sc2 = tree_pack2(sc, sc), mu2 = tree_pack2(-mu, -mu);
-        auto weights = [&](const uint32_t (&x)[32], int q) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float p0, p1;
-            tree_unpack2(tree_fma2(tree_pack2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sc2, mu2), p0, p1);
-            p0 = fast_exp2(p0);
-            p1 = fast_exp2(p1);
+            tree_unpack2(tree_fma2(tree_pack2(__uint_as_float(x[q * 32 + 2 * i]), __uint_as_float(x[q * 32 + 2 * i + 1])), sc2, mu2), p0, p1);
+            if ((i & 3) == 3) {                         // a quarter on the FMA pipe: the exponential unit is what both groups wait for
+              tree_exp2_pair(p0, p1);
+            } else {
+              p0 = fast_exp2(p0);
+              p1 = fast_exp2(p1);
+            }
             const uint64_t pp = tree_pack2(p0, p1);
             if (i & 1) sum1 = tree_add2(sum1, pp);
             else sum0 = tree_add2(sum0, pp);
             pk[i] = F8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);
           }
-          tmem_st16(tS + q * 16, pk);
-        };
-#pragma unroll 1
-        for (int q = 0; q < 4; q += 2) {
-          tc_wait_ld();
-          tmem_ld32(tS + q * 32 + 32, x1);
-          weights(x0, q);
-          tc_wait_ld();
-          if (q == 0) tmem_ld32(tS + 64, x0);
-          weights(x1, q + 1);
-          if (q == 2 && kt >= edge) {
-            // before the last weights go, for they let the guard's word be written anew: does this row see a guarded key?
-            wait_all(&ctrl->v_ok[c & 7], c >> 3);
-            if (sees) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                odd |= (*reinterpret_cast<volatile uint32_t*>(&ctrl->v_bad[c & 7][e]) &
-                        tree_visible(kt * kTreeKeys + 32 * e, at, keys, mask)) != 0u;
-            }
-          }
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_part[t][q >> 1]));
+          tmem_st16(tS + b * 64 + q * 16, pk);          // (over scores that have been read)
         }
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_full[t][b]));
+        ns ^= 1u << b;
+        last = b;
         {
           float a0, a1, b0, b1;
           tree_unpack2(sum0, a0, a1);
@@ -931,13 +1074,11 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           l = l * alpha + ((a0 + a1) + (b0 + b1));
         }
       }
-      c0 += te - tb;
       // ---- the item's rows
-      const bool any = mine && (PAIR ? te > tb : te > tb + t);   // this group had key tiles
+      const bool any = last >= 0;                       // this group had key tiles
       const float vs = F8 ? __ldg(P.v_scale + it.g) : 1.f;
       if (any) {
-        wait_all(&ctrl->o_full[t], no);
-        ++no;
+        wait_all(&ctrl->pv_done[t][last], (ns >> last) ^ 1u);   // the last product is done, and with it those before it
         tc_fence_after();
       }
       float f[2] = {0.f, 0.f};                          // factors of O_0 and O_1 in this row's output
@@ -948,8 +1089,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         have[1] = any && t == 1;
         f[t] = whole ? (l > 0.f ? 1.f / l : (l != l ? l : 0.f)) : 1.f;
       } else {
-        have[0] = te > tb;
-        have[1] = te > tb + 1;
+        const int even = tb + (c0 & 1), odds = tb + ((c0 & 1) ^ 1);
+        have[0] = te > even;
+        have[1] = te > odds;
         if (odd) atomicOr(&ctrl->odd[k % TR_ITEMS], 1u);
         if (t == 1) ctrl->ml[r] = make_float2(m, l);
         meet();
@@ -1050,13 +1192,14 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       }
       // split: neither group may hand weights of the next item over while the other still reads O
       if (!PAIR) meet();
+      c0 += te - tb;
       done_item(k);
     }
   }
 
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) tmem_dealloc(tbase, C::TMEM_COLS);
+  if (warp == 10) tmem_dealloc(tbase, C::TMEM_COLS);
 }
 
 // The pieces of the units that shares' ends cut, put together in order: block (share in which the unit begins, row tile, 8 columns),

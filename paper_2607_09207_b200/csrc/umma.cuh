@@ -30,7 +30,14 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
       "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accum)
       : "memory");
 }
-// D[tmem] (+)= A[smem] . B[smem], and the product above, issued by the lane whose `elected` is not 0 (elect.sync) while the warp
+// D[tmem] (+)= A[smem] . B[smem]
+__device__ __forceinline__ void umma_ss(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
+  asm volatile(
+      "{ .reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum)
+      : "memory");
+}
+// The two products above, issued by the lane whose `elected` is not 0 (elect.sync) while the warp
 // runs as one: the compiler then keeps descriptors and addresses in uniform registers, which a single-lane branch costs a move
 // per operand and MMA.
 __device__ __forceinline__ void umma_ss_elected(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum,
