@@ -10,8 +10,8 @@ namespace {
 
 using namespace pdattn;
 
-constexpr size_t kTreeRec = WS_CLEARED_BYTES;                                                   // [TR_CTAS][2] int4
-constexpr size_t kTreePartials = (kTreeRec + TR_CTAS * 2 * sizeof(int4) + 255) / 256 * 256;
+constexpr size_t kTreeRec = WS_CLEARED_BYTES;                                                   // [TR_CTAS][2][2] int4
+constexpr size_t kTreePartials = (kTreeRec + TR_CTAS * 4 * sizeof(int4) + 255) / 256 * 256;
 size_t part_bytes(int head_dim) { return static_cast<size_t>(2) * (head_dim + 2) * 128 * 4; }   // of one piece: two row tiles
 
 template <int D, bool PAIR, int EB>
@@ -38,7 +38,7 @@ pdattn_status launch_tree(const CUtensorMap& mq, const CUtensorMap& mk, const CU
   if (e != cudaSuccess) return cuda_fail("tree_kernel launch", e);
   // no unit that a row of the table can describe is long enough to be cut: nothing to join
   if ((static_cast<int64_t>(P.MB) << P.bs_log2) <= (2 * kTreeMinCut - 1) * kTreeKeys) return PDATTN_OK;
-  e = launch_dependent(tree_join_kernel<D, PAIR>, dim3(grid, PAIR ? 2 : 1, D / 8), 128, 0, stream, true, P, grid);
+  e = launch_dependent(tree_join_kernel<D, PAIR>, dim3(grid, PAIR ? 2 : 1, D / TR_JOIN_COLS), 128, 0, stream, true, P, grid);
   if (e != cudaSuccess) return cuda_fail("tree_join_kernel launch", e);
   return PDATTN_OK;
 }

@@ -63,7 +63,8 @@ struct TreeParams {
   int64_t sb, sh, st;
   const float *k_scale, *v_scale;
   WsHeader* hdr;
-  int4* rec;                     // [gridDim][2] pieces of cut units: (sequence or -1, KV head, row pair, 1: it ends the unit)
+  int4* rec;                     // [gridDim][2][2] pieces of cut units: (sequence or -1, KV head, row pair, 1: it ends the unit),
+                                 // (cu_tokens of the sequence, tokens of the tree, 0, 0)
   float* partials;               // [gridDim][2][2 tiles][O columns, m, l][128 rows]
   int N, S, Hq, Hkv, G, MB, NB, bs_log2;
   int TQ;                        // tokens of a row tile: 128 / G
@@ -490,7 +491,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           done_item(k);
         }
       } else {
-        int4 rec[2] = {make_int4(-1, 0, 0, 0), make_int4(-1, 0, 0, 0)};
+        int4 rec[4] = {make_int4(-1, 0, 0, 0), make_int4(0, 0, 0, 0), make_int4(-1, 0, 0, 0), make_int4(0, 0, 0, 0)};
         int base = s0 & ~31;
         TreeSeq win = tree_seq<PAIR>(P, base + lane);
         int s = s0, u = u0, t = t0;
@@ -527,7 +528,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             if (it.te - it.tb < tiles) {
               const int which = it.tb > 0 ? 0 : 1;
               it.part = 2 * blockIdx.x + which;
-              rec[which] = make_int4(s, it.g, pair, it.te == tiles ? 1 : 0);
+              rec[2 * which] = make_int4(s, it.g, pair, it.te == tiles ? 1 : 0);
+              rec[2 * which + 1] = make_int4(it.row0, n, 0, 0);
             }
             it.rows[0] = min(P.TQ, n - it.tok0);
             it.rows[1] = PAIR ? min(P.TQ, max(0, n - it.tok0 - P.TQ)) : it.rows[0];
@@ -569,8 +571,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           if (more) load_tiles(it);
         }
         if (lane == 0) {
-          P.rec[2 * blockIdx.x] = rec[0];
-          P.rec[2 * blockIdx.x + 1] = rec[1];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) P.rec[4 * blockIdx.x + i] = rec[i];
           if (ran_out) atomicOr(&P.hdr->err, ERR_BAD_PAGE);
         }
         // given up: no copy may still be on its way into this CTA's shared memory when it ends
@@ -936,10 +938,19 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       if (!wait(bar, parity) && lane == 0) fail();
     };
     int meets = 0;
-    auto meet = [&]() {                // all eight warps (bounded, unlike a named barrier)
+    // all eight warps (bounded, unlike a named barrier)
+    auto meet_arrive = [&]() {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ctrl->meet));
+    };
+    bool owed = false;                 // arrived, but not waited
+    auto meet_wait = [&]() {
       wait_all(&ctrl->meet, meets++);
+      owed = false;
+    };
+    auto meet = [&]() {
+      meet_arrive();
+      meet_wait();
     };
     const TreeItem* ip;
     int c0 = 0, nq = 0;                // key tiles of the CTA before this item; items with key tiles
@@ -975,6 +986,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         const bool first = last < 0;
         wait_all(&ctrl->s_full[t][b], ns >> b);
         if (!busy) {
+          if (!F8 && owed) meet_wait();
           if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_full[t][b]));
           ns ^= 1u << b;
           last = b;
@@ -1048,7 +1060,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           for (int i = 0; i < 16; ++i) {
             float p0, p1;
             tree_unpack2(tree_fma2(tree_pack2(__uint_as_float(x[q * 32 + 2 * i]), __uint_as_float(x[q * 32 + 2 * i + 1])), sc2, mu2), p0, p1);
-            if ((i & 3) == 3) {                         // a quarter on the FMA pipe: the exponential unit is what both groups wait for
+            // PAIR: a quarter on the FMA pipe (8 x 64 tokens 388 -> 379 us under the power cap; split, 256 x 8: 281 -> 287)
+            if (PAIR && (i & 3) == 3) {
               tree_exp2_pair(p0, p1);
             } else {
               p0 = fast_exp2(p0);
@@ -1064,6 +1077,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
+        if (!F8 && owed) meet_wait();                   // (these weights may make O anew: the other group has read the last item's)
         if (lane == 0) mbar_arrive(smem_u32(&ctrl->p_full[t][b]));
         ns ^= 1u << b;
         last = b;
@@ -1092,46 +1106,45 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         const int even = tb + (c0 & 1), odds = tb + ((c0 & 1) ^ 1);
         have[0] = te > even;
         have[1] = te > odds;
+        if (owed) meet_wait();
         if (odd) atomicOr(&ctrl->odd[k % TR_ITEMS], 1u);
         if (t == 1) ctrl->ml[r] = make_float2(m, l);
         meet();
         odd = *reinterpret_cast<volatile uint32_t*>(&ctrl->odd[k % TR_ITEMS]) != 0u;
-        if (whole) {
-          if (t == 0) {
-            const float2 other = ctrl->ml[r];
-            const float M = fmaxf(m, other.x);
-            f[0] = m == NEG_INF ? 0.f : fast_exp2(m - M);
-            f[1] = other.x == NEG_INF ? 0.f : fast_exp2(other.x - M);
-            const float sum = l * f[0] + other.y * f[1];
-            const float inv = sum > 0.f ? 1.f / sum : (sum != sum ? sum : 0.f);
+        if (t == 0) {
+          const float2 other = ctrl->ml[r];
+          const float M = fmaxf(m, other.x);
+          f[0] = m == NEG_INF ? 0.f : fast_exp2(m - M);
+          f[1] = other.x == NEG_INF ? 0.f : fast_exp2(other.x - M);
+          m = M;
+          l = l * f[0] + other.y * f[1];
+          if (whole) {
+            const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
             f[0] *= inv;
             f[1] *= inv;
-            ctrl->ml[r] = make_float2(f[0], f[1]);
           }
-          meet();
-          if (t == 1) {
-            const float2 both = ctrl->ml[r];
-            f[0] = both.x;
-            f[1] = both.y;
-          }
-          tc_fence_after();                             // (the other group's O: its product was seen to be done before the barrier)
-        } else {
-          f[t] = 1.f;
-          have[t ^ 1] = false;
+          ctrl->ml[r] = make_float2(f[0], f[1]);
         }
+        meet();
+        if (t == 1) {
+          const float2 both = ctrl->ml[r];
+          f[0] = both.x;
+          f[1] = both.y;
+        }
+        tc_fence_after();                               // (the other group's O: its product was seen to be done before the barrier)
       }
       f[0] *= vs;
       f[1] *= vs;
       if (mine && busy) {
         // a part of a unit leaves its sums as they are
-        float* part = whole ? nullptr : P.partials + (static_cast<int64_t>(it.part) * 2 + t) * ((D + 2) * 128) + r;
-        if (part && valid) {
+        float* part = whole ? nullptr : P.partials + (static_cast<int64_t>(it.part) * 2 + (PAIR ? t : 0)) * ((D + 2) * 128) + r;
+        if (part && valid && (PAIR || t == 0)) {
           part[D * 128] = m;
           part[(D + 1) * 128] = l;
         }
         __nv_bfloat16* out0 = P.out + (static_cast<int64_t>(it.row0 + it.tok0 + (PAIR ? t * P.TQ : 0)) * P.Hq + it.g * P.G) * D;
         const int offset = valid ? (rj * P.Hq + rh) * D : -1;     // of this thread's row
-        const int q0 = PAIR || part ? 0 : t * (D / 64), q1 = PAIR || part ? D / 32 : q0 + D / 64;
+        const int q0 = PAIR ? 0 : t * (D / 64), q1 = PAIR ? D / 32 : q0 + D / 64;   // split: half of the columns each
 #pragma unroll 1
         for (int q = q0; q < q1; ++q) {
           float v[32];
@@ -1147,7 +1160,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = f[tt] != 0.f ? fmaf(__uint_as_float(o[i]), f[tt], v[i]) : v[i];
           }
-          if (odd && sees && (PAIR || !part || t == 0)) {
+          if (odd && sees) {
             float add[32];                              // (a copy: v stays in registers)
 #pragma unroll
             for (int i = 0; i < 32; ++i) add[i] = v[i];
@@ -1190,8 +1203,13 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         tc_fence_before();
       }
-      // split: neither group may hand weights of the next item over while the other still reads O
-      if (!PAIR) meet();
+      // split: neither group may hand weights of the next item over while the other still reads O.  It waits for that when it has some;
+      // over codes at once (the check in the loop over the key tiles cost more there: 317 -> 346 us for 32 x 16 tokens).
+      if (!PAIR) {
+        meet_arrive();
+        if (F8) meet_wait();
+        else owed = true;
+      }
       c0 += te - tb;
       done_item(k);
     }
@@ -1202,83 +1220,84 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   if (warp == 10) tmem_dealloc(tbase, C::TMEM_COLS);
 }
 
-// The pieces of the units that shares' ends cut, put together in order: block (share in which the unit begins, row tile, 8 columns),
+// The pieces of the units that shares' ends cut, put together in order: block (share in which the unit begins, row tile, 16 columns),
 // a thread per row.     M = max m_j;  out = sum O_j 2^(m_j - M) / sum l_j 2^(m_j - M)
-// Bound by the latency of its loads (neighbouring rows are neighbours in memory): four pieces are fetched at a time.
+// Bound by the latency of its loads (neighbouring rows are neighbours in memory): the records of all shares that may follow come at
+// once, then all maxima, then four pieces at a time.
+constexpr int TR_JOIN_COLS = 16;
 template <int D, bool PAIR>
 __global__ void __launch_bounds__(128)
 tree_join_kernel(const __grid_constant__ TreeParams P, int ctas) {
-  __shared__ int list[2 * TR_CTAS], last[4], count[4];
+  __shared__ int list[2 * TR_CTAS], last[8], count[8];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int c = blockIdx.x, t = blockIdx.y, q = blockIdx.z, r = threadIdx.x, warp = r >> 5, lane = r & 31;
-  const int4 head = P.rec[2 * c + 1];
+  static_assert(TR_CTAS <= 257, "two records a thread");
+  const int4 head = P.rec[4 * c + 2], whose = P.rec[4 * c + 3];
+  int4 x[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int cc = c + 1 + e * 128 + r;
+    x[e] = cc < ctas ? P.rec[4 * cc] : make_int4(-1, 0, 0, 0);
+  }
   if (head.x < 0) return;
   // the unit's other pieces: first pieces of the shares that follow, up to the one that ends the unit (shares may be empty)
-  int n = 1;
-  if (r == 0) list[0] = 2 * c + 1;
-  for (int base = c + 1; base < ctas; base += 128) {
-    const int cc = base + r;
-    const int4 x = cc < ctas ? P.rec[2 * cc] : make_int4(-1, 0, 0, 0);
-    const bool own = x.x == head.x && x.y == head.y && x.z == head.z;
-    const uint32_t ends = __ballot_sync(0xffffffffu, own && x.w == 1), owns = __ballot_sync(0xffffffffu, own);
-    const uint32_t upto = ends ? (ends & (0u - ends)) * 2u - 1u : 0xffffffffu;      // lanes up to the one that ends the unit
+  uint32_t mine[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const bool own = x[e].x == head.x && x[e].y == head.y && x[e].z == head.z;
+    const uint32_t ends = __ballot_sync(0xffffffffu, own && x[e].w == 1), owns = __ballot_sync(0xffffffffu, own);
+    mine[e] = owns & (ends ? (ends & (0u - ends)) * 2u - 1u : 0xffffffffu);       // up to the one that ends the unit
     if (lane == 0) {
-      last[warp] = ends != 0u;
-      count[warp] = __popc(owns & upto);
+      last[e * 4 + warp] = ends != 0u;
+      count[e * 4 + warp] = __popc(mine[e]);
     }
-    __syncthreads();
-    int before = n;
-    bool over = false;
-    for (int w = 0; w < warp; ++w) {
-      over |= last[w] != 0;
-      before += count[w];
-    }
-    if (!over && own && (upto >> lane & 1u)) list[before + __popc(owns & upto & ((1u << lane) - 1u))] = 2 * cc;
-    bool ended = false;
-    for (int w = 0; w < 4 && !ended; ++w) {
-      n += count[w];
-      ended = last[w] != 0;
-    }
-    __syncthreads();
-    if (ended) break;
+  }
+  if (r == 0) list[0] = 2 * c + 1;
+  __syncthreads();
+  int n = 1;
+  bool over = false;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    if (!over && (w & 3) == warp && (mine[w >> 2] >> lane & 1u))
+      list[n + __popc(mine[w >> 2] & ((1u << lane) - 1u))] = 2 * (c + 1 + (w >> 2) * 128 + r);
+    if (!over) n += count[w];
+    over |= last[w] != 0;
   }
   __syncthreads();
-  const int row0 = __ldg(P.cu_tokens + head.x), tree = __ldg(P.cu_tokens + head.x + 1) - row0;
   const int rj = r / P.G, rh = r - rj * P.G;
   const int j = (PAIR ? (2 * head.z + t) * P.TQ : 0) + rj;
-  if (rj >= P.TQ || j >= tree) return;
-  // PAIR: a piece has one part per row tile; split: both groups' parts belong to the one row tile
-  const int parts = PAIR ? n : 2 * n;
+  if (rj >= P.TQ || j >= whose.y) return;
   constexpr int64_t TILE_FLOATS = (D + 2) * 128;
-  auto part = [&](int p) {
-    const int slot = PAIR ? list[p] : list[p >> 1];
-    return P.partials + (static_cast<int64_t>(slot) * 2 + (PAIR ? t : p & 1)) * TILE_FLOATS + r;
-  };
+  auto part = [&](int p) { return P.partials + (static_cast<int64_t>(list[p]) * 2 + t) * TILE_FLOATS + r; };
   const float NEG_INF = __int_as_float(0xff800000);
-  float M = NEG_INF, L = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int p = 0; p < parts; ++p) M = fmaxf(M, part(p)[D * 128]);
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const float* x = part(p);
-    const float m = x[D * 128], l = x[(D + 1) * 128];
-    float y[8];
+  float M = NEG_INF, L = 0.f, o[TR_JOIN_COLS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = x[(q * 8 + i) * 128];
+  for (int i = 0; i < TR_JOIN_COLS; ++i) o[i] = 0.f;
+#pragma unroll 8
+  for (int p = 0; p < n; ++p) M = fmaxf(M, part(p)[D * 128]);
+#pragma unroll 4
+  for (int p = 0; p < n; ++p) {
+    const float* from = part(p);
+    const float m = from[D * 128], l = from[(D + 1) * 128];
+    float y[TR_JOIN_COLS];
+#pragma unroll
+    for (int i = 0; i < TR_JOIN_COLS; ++i) y[i] = from[(q * TR_JOIN_COLS + i) * 128];
     if (m == NEG_INF) continue;                          // saw nothing: what it holds may be anything
     const float f = fast_exp2(m - M);
     L += l * f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < TR_JOIN_COLS; ++i) {
       // infinities and NaN of V stand whatever the weight
       const bool odd = (__float_as_uint(y[i]) & 0x7f800000u) == 0x7f800000u;
       o[i] += odd ? y[i] : y[i] * f;
     }
   }
   const float inv = L > 0.f ? 1.f / L : (L != L ? L : 0.f);
-  *reinterpret_cast<uint4*>(P.out + (static_cast<int64_t>(row0 + j) * P.Hq + head.y * P.G + rh) * D + q * 8) =
-      make_uint4(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
-                 pack_bf16x2(o[6] * inv, o[7] * inv));
+  uint4* out = reinterpret_cast<uint4*>(P.out + (static_cast<int64_t>(whose.x + j) * P.Hq + head.y * P.G + rh) * D + q * TR_JOIN_COLS);
+#pragma unroll
+  for (int i = 0; i < TR_JOIN_COLS / 8; ++i)
+    out[i] = make_uint4(pack_bf16x2(o[8 * i] * inv, o[8 * i + 1] * inv), pack_bf16x2(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                        pack_bf16x2(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack_bf16x2(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
 }
 
 }  // namespace pdattn
