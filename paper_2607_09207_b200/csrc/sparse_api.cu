@@ -39,9 +39,14 @@ pdattn_status summarize(SummaryParams& P, int head_dim, bool fp8, int64_t grid, 
   return PDATTN_OK;
 }
 
-// Blocks of a unit in select_kernel: 512 pages each while the workspace's zeroed words number the units, so that few long sequences
-// keep every SM busy; above that there are units enough, and a block takes a whole one.
-constexpr int kSelectChunk = 512;
+// Pages that a block of select_kernel scores: as many, from 256 to 2048, as leave four blocks an SM (48 sequences to 32,768 tokens, 64/8
+// heads: 25 us with 1024, 29 with 512).  More units than the workspace's zeroed words can number are enough by themselves: a block takes a
+// whole one.
+int select_chunk(int64_t units, int pages, int sms) {
+  int chunk = 2048;
+  while (chunk > 256 && units * ((pages + chunk - 1) / chunk) < 4ll * sms) chunk /= 2;
+  return chunk;
+}
 constexpr size_t kSelectKeys = WS_CLEARED_BYTES;
 static_assert(WS_CLEARED_BYTES == 8448 && (WS_CLEARED_BYTES % 256) == 0, "workspace layout");
 
@@ -122,8 +127,12 @@ pdattn_status pdattn_select_pages(const pdattn_select_args* a, pdattn_stream_t s
   P.K = a->num_selected;
   P.first = a->num_first;
   P.recent = a->num_recent;
-  P.chunk = units <= MAX_SPANS ? kSelectChunk : a->max_blocks_per_seq;
   const int most = a->max_blocks_per_seq - a->num_first - a->num_recent;      // pages that a unit may have to score
+  int dev = 0;
+  DevInfo* di = nullptr;
+  const pdattn_status ds = device_info(&dev, &di);
+  if (ds != PDATTN_OK) return ds;
+  P.chunk = units <= MAX_SPANS ? select_chunk(units, most > 1 ? most : 1, di->sm_count) : a->max_blocks_per_seq;
   P.chunks = most > P.chunk ? (most + P.chunk - 1) / P.chunk : 1;
   const int64_t grid = units * P.chunks;
   if (grid > INT32_MAX) return PDATTN_UNSUPPORTED;

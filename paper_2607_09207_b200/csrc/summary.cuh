@@ -207,82 +207,128 @@ __device__ __forceinline__ void mma_s8(int (&c)[4], uint32_t a0, uint32_t a1, ui
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// sum over the block of `v` (32-bit); `sums` has one word per warp and two sets that alternate, so that one barrier is enough
-__device__ __forceinline__ int block_sum(int v, int* sums, int turn) {
+// Exclusive sum over the block of v in the threads' order.
+template <class T>
+__device__ __forceinline__ T block_exclusive(T v, T* warp_sums) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  v = __reduce_add_sync(0xffffffffu, v);
-  int* set = sums + (turn & 1) * (SEL_THREADS / 32);
-  if (lane == 0) set[warp] = v;
-  __syncthreads();
-  int t = 0;
+  T run = v;
 #pragma unroll
-  for (int w = 0; w < SEL_THREADS / 32; ++w) t += set[w];
-  return t;
+  for (int o = 1; o < 32; o <<= 1) {
+    const T y = __shfl_up_sync(0xffffffffu, run, o);
+    if (lane >= o) run += y;
+  }
+  if (lane == 31) warp_sums[warp] = run;
+  __syncthreads();
+  T before = run - v;
+#pragma unroll
+  for (int w = 0; w < SEL_THREADS / 32; ++w) before += w < warp ? warp_sums[w] : T(0);
+  return before;
 }
 
 // The R largest of M keys, ties to the lower index, as ascending page numbers out[0 .. R).  Thread t owns the indices t * each ..
-// + each - 1, in registers up to E of them (E = 0: read again in every round).  The R-th largest key is built bit by bit: 32 counts.
-template <int E>
-__device__ __forceinline__ void take_largest(const uint32_t* keys, int M, int R, int first, int32_t* out, int* sums) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+// + each - 1, in registers up to E of them (E = 0: read again in every round).  Keys that this block has just written lie in its shared
+// memory.  The R-th largest key is found eight bits at a time,
+// from the highest in which the keys differ: a histogram of the keys that agree with it so far, and the bin in which the count from
+// above reaches R.  (Bit by bit, with 32 counts, 2048 keys took 2.5 us longer.)
+struct SelectScratch {
+  int bins[2][256];
+  int warp_counts[SEL_THREADS / 32];
+  unsigned long long warp_sums[SEL_THREADS / 32];
+  uint32_t ends[2], digit;
+  int left;
+};
+static_assert(SEL_THREADS == 256, "a thread per bin");
+// (A function of its own: inlined, its registers slowed the scoring loop, 25.5 -> 31 us for 48 sequences to 32,768 tokens.)
+template <int E, bool SHARED>
+__device__ __noinline__ void take_largest(const uint32_t* keys, int M, int R, int first, int32_t* out, SelectScratch* sh) {
+  const int tid = threadIdx.x, lane = tid & 31;
   const int each = E > 0 ? E : (M + SEL_THREADS - 1) / SEL_THREADS;
   const int i0 = tid * each;
-  uint32_t x[E > 0 ? E : 1];
+  const int mine = max(0, min(each, M - i0));
+  auto read = [&](int j) { return SHARED ? keys[i0 + j] : __ldcg(keys + i0 + j); };
+  uint32_t x[E > 0 ? E : 1] = {};
   if constexpr (E > 0) {
 #pragma unroll
-    for (int j = 0; j < E; ++j) x[j] = i0 + j < M ? __ldcg(keys + i0 + j) : 0u;
+    for (int j = 0; j < E; ++j) x[j] = j < mine ? read(j) : 0u;
   }
-  auto key = [&](int j) { return E > 0 ? x[E > 0 ? j : 0] : __ldcg(keys + i0 + j); };
-  const int mine = E > 0 ? E : max(0, min(each, M - i0));          // (keys past the end are 0, below every score's)
-  uint32_t t = 0u;
-  int turn = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t cand = t | (1u << bit);
-    int n = 0;
+  // f(index in the thread's share, key) for all of them
+  auto each_key = [&](auto f) {
+    if constexpr (E > 0) {
 #pragma unroll
-    for (int j = 0; j < mine; ++j) n += key(j) >= cand ? 1 : 0;
-    if (block_sum(n, sums, turn++) >= R) t = cand;
+      for (int j = 0; j < E; ++j)
+        if (j < mine) f(j, x[j]);
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < mine; ++j) f(j, read(j));
+    }
+  };
+  uint32_t largest = 0u, least = 0xffffffffu;
+  each_key([&](int, uint32_t k) {
+    largest = max(largest, k);
+    least = min(least, k);
+  });
+  if (tid == 0) {
+    sh->ends[0] = 0u;
+    sh->ends[1] = 0xffffffffu;
   }
-  // keys above the threshold, and equal ones in order until there are R: both counts scanned as one 64-bit word
-  int gt = 0, eq = 0;
-#pragma unroll
-  for (int j = 0; j < mine; ++j) {
-    const bool in = i0 + j < M;
-    gt += in && key(j) > t ? 1 : 0;
-    eq += in && key(j) == t ? 1 : 0;
-  }
-  const int above = block_sum(gt, sums, turn++);
-  unsigned long long v = (static_cast<unsigned long long>(gt) << 32) | static_cast<unsigned>(eq), run = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const unsigned long long y = __shfl_up_sync(0xffffffffu, run, o);
-    if (lane >= o) run += y;
-  }
-  __shared__ unsigned long long warp_run[SEL_THREADS / 32];
-  if (lane == 31) warp_run[warp] = run;
+  sh->bins[0][tid] = 0;
   __syncthreads();
-  unsigned long long before = run - v;
-  for (int w = 0; w < warp; ++w) before += warp_run[w];
+  largest = __reduce_max_sync(0xffffffffu, largest);
+  least = __reduce_min_sync(0xffffffffu, least);
+  if (lane == 0) {
+    atomicMax(&sh->ends[0], largest);
+    atomicMin(&sh->ends[1], least);
+  }
+  __syncthreads();
+  const uint32_t differ = sh->ends[0] ^ sh->ends[1];
+  int low = differ ? 32 - __clz(differ) : 0;            // bits below this one are still to be found
+  uint32_t t = low >= 32 ? 0u : sh->ends[1] >> low << low;
+  int want = R;                                         // of the keys that agree with t in the bits from `low` on
+  for (int turn = 0; low > 0; turn ^= 1) {
+    const int shift = max(0, low - 8), bits = low - shift;
+    each_key([&](int, uint32_t k) {
+      if (low >= 32 || (k >> low) == (t >> low)) atomicAdd(&sh->bins[turn][(k >> shift) & ((1u << bits) - 1u)], 1);
+    });
+    __syncthreads();
+    // thread i looks at bin 255 - i: keys in larger bins come before
+    const int n = sh->bins[turn][255 - tid];
+    sh->bins[turn ^ 1][tid] = 0;
+    const int above = block_exclusive(n, sh->warp_counts);
+    if (above < want && above + n >= want) {
+      sh->digit = static_cast<uint32_t>(255 - tid);
+      sh->left = want - above;
+    }
+    __syncthreads();
+    t |= sh->digit << shift;
+    want = sh->left;
+    low = shift;
+  }
+  // keys above t, and `want` of those equal to it in order: both counts scanned as one 64-bit word
+  int gt = 0, eq = 0;
+  each_key([&](int, uint32_t k) {
+    gt += k > t ? 1 : 0;
+    eq += k == t ? 1 : 0;
+  });
+  const unsigned long long before =
+      block_exclusive((static_cast<unsigned long long>(gt) << 32) | static_cast<unsigned>(eq), sh->warp_sums);
   int g = static_cast<int>(before >> 32), q = static_cast<int>(before & 0xffffffffull);
-  const int want = R - above;                                       // equal keys that are taken
-#pragma unroll
-  for (int j = 0; j < mine; ++j) {
-    if (i0 + j >= M) break;
-    const uint32_t k = key(j);
+  each_key([&](int j, uint32_t k) {
     if (k > t || (k == t && q < want)) out[g + min(q, want)] = first + i0 + j;
     if (k > t) ++g;
     if (k == t) ++q;
-  }
+  });
 }
 
+constexpr int SEL_OWN = 2048;     // keys that a block which has a unit to itself keeps in shared memory
 template <int D, int NT>   // NT: groups of 8 query heads
-__global__ void __launch_bounds__(SEL_THREADS)
+__global__ void __launch_bounds__(SEL_THREADS, NT == 1 ? 4 : 2)
 select_kernel(const __grid_constant__ SelectParams P) {
   constexpr int RB = 2 * D, NI = RB / 64;
   __shared__ __align__(16) int8_t qc[8 * NT][RB];
   __shared__ int qe[8 * NT];
-  __shared__ int sums[2 * (SEL_THREADS / 32)];
+  __shared__ SelectScratch scratch;
   __shared__ int is_last;
+  __shared__ uint32_t own_keys[SEL_OWN];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int unit = blockIdx.x / P.chunks, chunk = blockIdx.x - unit * P.chunks;
   const int s = unit / P.Hkv, g = unit - s * P.Hkv;
@@ -305,6 +351,14 @@ select_kernel(const __grid_constant__ SelectParams P) {
   const int i0 = chunk * P.chunk;
   if (i0 >= M) return;
   const int i1 = min(M, i0 + P.chunk);
+  // ids of a warp's 16 pages, a round ahead of their use
+  constexpr int STEP = SEL_THREADS / 32 * 16;          // pages of a round of the block
+  const int32_t* row = P.table + static_cast<int64_t>(s) * P.MB + P.first;
+  auto page_of = [&](int b0) {
+    const int i = b0 + (lane & 15);
+    return i < i1 ? __ldg(row + i) : 0;
+  };
+  int next_id = page_of(i0 + warp * 16);
 
   // ---- the group's query heads as codes: the parts below zero against the minima, the others against the maxima
   for (int h = warp; h < 8 * NT; h += SEL_THREADS / 32) {
@@ -343,11 +397,11 @@ select_kernel(const __grid_constant__ SelectParams P) {
   }
   const float NEG_INF = __int_as_float(0xff800000);
   uint32_t* keys = P.keys + static_cast<int64_t>(unit) * P.MB;
-  const int32_t* row = P.table + static_cast<int64_t>(s) * P.MB + P.first;
+  const bool own = M <= P.chunk && M <= SEL_OWN;       // no other block scores for this unit
   bool bad = false;
-  for (int b0 = i0 + warp * 16; b0 < i1; b0 += SEL_THREADS / 32 * 16) {
-    const int i = b0 + (lane & 15);
-    int id = i < i1 ? __ldg(row + i) : 0;
+  for (int b0 = i0 + warp * 16; b0 < i1; b0 += STEP) {
+    int id = next_id;
+    next_id = page_of(b0 + STEP);
     const bool gone = id < 0 || id >= P.NB;
     bad |= gone;
     if (gone) id = -1;
@@ -383,7 +437,11 @@ select_kernel(const __grid_constant__ SelectParams P) {
       best[half] = fmaxf(best[half], __shfl_xor_sync(0xffffffffu, best[half], 2));
       if (ek[half] == SUM_EXP_ODD) best[half] = __int_as_float(0x7f800000);
       const int at = b0 + r + 8 * half;
-      if (c == 0 && at < i1) __stcg(keys + at, ids[half] < 0 ? 1u : score_key(best[half]));
+      if (c == 0 && at < i1) {
+        const uint32_t key = ids[half] < 0 ? 1u : score_key(best[half]);
+        if (own) own_keys[at] = key;
+        else __stcg(keys + at, key);
+      }
     }
   }
   if (bad) atomicOr(P.err, ERR_BAD_PAGE);
@@ -406,9 +464,10 @@ select_kernel(const __grid_constant__ SelectParams P) {
   }
   for (int i = tid; i < P.first; i += SEL_THREADS) out[i] = i;
   for (int i = tid; i < P.recent; i += SEL_THREADS) out[P.first + R + i] = nb - P.recent + i;
-  if (M <= SEL_THREADS * 8) take_largest<8>(keys, M, R, P.first, out + P.first, sums);
-  else if (M <= SEL_THREADS * 32) take_largest<32>(keys, M, R, P.first, out + P.first, sums);
-  else take_largest<0>(keys, M, R, P.first, out + P.first, sums);
+  static_assert(SEL_OWN == SEL_THREADS * 8, "eight keys a thread");
+  if (own) take_largest<8, true>(own_keys, M, R, P.first, out + P.first, &scratch);
+  else if (M <= SEL_THREADS * 8) take_largest<8, false>(keys, M, R, P.first, out + P.first, &scratch);
+  else take_largest<0, false>(keys, M, R, P.first, out + P.first, &scratch);
 }
 
 }  // namespace pdattn
