@@ -91,7 +91,7 @@ struct TreeCfg {
   static constexpr int NV = EB == 1 ? 4 : D == 128 ? 5 : 6;
   static constexpr int NR = EB == 1 ? 4 : 0;
   static constexpr int RING_BYTES = NQ * QT * (Q_BYTES + QP_BYTES) + NK * K_BYTES + NV * TILE_BYTES + NR * RAW_BYTES;
-  static constexpr int CTRL_BYTES = EB == 1 ? 3072 : 2048;
+  static constexpr int CTRL_BYTES = 2048 + (EB == 1 ? TR_ITEMS * QT * 512 : 0);
   static constexpr int DYN_BYTES = 1024 + RING_BYTES + CTRL_BYTES;
   static constexpr int COL_S = 0, COL_O = 256, TMEM_COLS = 512;
   static_assert(DYN_BYTES <= 232448, "shared memory");
@@ -113,6 +113,9 @@ struct TreeCtrl {
   // of key tile c and the product of c - LAG
   uint64_t k_full[8], v_full[8], v_ok[8], step[8];
   uint64_t q_full[2], q_ok[2], q_free[2];        // per buffer of Q: it has landed; fp8: is split; its scores are done
+  // fp8: the factors of an item's rows are there.  Per item in flight, not per buffer of Q: the scores run ahead of the softmax, so a
+  // buffer may have its next users before the softmax has come to the first.
+  uint64_t scale_ok[TR_ITEMS];
   uint64_t s_full[2][2], p_full[2][2], pv_done[2][2];   // per group and buffer: scores are there; weights are stored; their product is done
   uint64_t item_full[TR_ITEMS], item_free[TR_ITEMS];
   uint64_t drained[2], meet, meet_widen;         // all softmax warps are here; all widening warps are
@@ -127,7 +130,7 @@ struct TreeCtrl {
   float2 ml[64 * 2];                             // split: (m, l) of group 1's rows, then the factors of both groups
 };
 static_assert(sizeof(TreeCtrl) <= 2048, "control block");
-// Behind it over codes: per buffer and row of Q, the factor that belongs to its e4m3 terms.
+// Behind it over codes: per item in flight and row of its Q, the factor that belongs to the e4m3 terms.
 constexpr int TR_QSCALE_AT = 2048;
 
 // Bounded wait that also gives up when the CTA's abort flag is up; the clock comes into it after 64 polls.
@@ -287,7 +290,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
   const uint32_t sQ = raw + pad, sQP = sQ + (D == 64 ? C::NQ * QT * C::Q_BYTES : 0);   // (codes) Q's terms
   const uint32_t sK = sQ + C::NQ * QT * (C::Q_BYTES + C::QP_BYTES), sV = sK + NK * C::K_BYTES, rV = sV + NV * C::TILE_BYTES;
   TreeCtrl* ctrl = reinterpret_cast<TreeCtrl*>(smem + C::RING_BYTES);
-  float* q_scale = reinterpret_cast<float*>(smem + C::RING_BYTES + TR_QSCALE_AT);   // [NQ * QT][128]
+  float* q_scale = reinterpret_cast<float*>(smem + C::RING_BYTES + TR_QSCALE_AT);   // [TR_ITEMS][QT][128]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float NEG_INF = __int_as_float(0xff800000);
 
@@ -313,6 +316,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       }
     }
     for (int i = 0; i < TR_ITEMS; ++i) {
+      mbar_init(smem_u32(&ctrl->scale_ok[i]), 4);
       mbar_init(smem_u32(&ctrl->item_full[i]), 1);
       mbar_init(smem_u32(&ctrl->item_free[i]), 8 + 2 + 1 + (F8 ? 4 : 2));   // softmax, MMA, V, guards
     }
@@ -829,7 +833,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           y2[i] = a2 | (b2 << 16);
         }
       };
-      auto split_row = [&](int tile) {
+      auto split_row = [&](int tile, float* factor) {
         const uint32_t src = sQ + tile * C::Q_BYTES + id * 128;
         uint32_t x[32], y1[16], y2[16];
         uint32_t top = 0u;
@@ -841,7 +845,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         int e = 135 - static_cast<int>(top >> 23) - ((top & 0x7fffffu) > 0x600000u ? 1 : 0);   // 448 = 1.75 * 2^8
         e = top == 0u ? 0 : min(126, e);
         const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23);
-        q_scale[tile * 128 + id] = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+        factor[id] = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
         // the terms' rows; with head_dim 128 they lie over the row itself: a half's second terms wait until the other half is read
         const uint32_t d1 = sQP + tile * C::Q_BYTES + id * D, d2 = d1 + 128 * D;
         read64(src, x);
@@ -866,9 +870,10 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           ++nq;
           if (!ok) break;
 #pragma unroll 1
-          for (int i = 0; i < QT; ++i) split_row(qb * QT + i);
+          for (int i = 0; i < QT; ++i) split_row(qb * QT + i, q_scale + (k % TR_ITEMS * QT + i) * 128);
           publish(&ctrl->q_ok[qb]);
         }
+        if (lane == 0) mbar_arrive(smem_u32(&ctrl->scale_ok[k % TR_ITEMS]));
         for (int kt = tb; kt < te && ok; ++kt) do_v(kt >= edge, nv++);
         done_item(k);
       }
@@ -953,7 +958,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       meet_wait();
     };
     const TreeItem* ip;
-    int c0 = 0, nq = 0;                // key tiles of the CTA before this item; items with key tiles
+    int c0 = 0;                        // key tiles of the CTA before this item
     uint32_t ns = 0;                   // bit b: parity of s_full (and of p_full, pv_done) of this group's buffer b
     for (int k = 0; get_item(k, ip); ++k) {
       const TreeItem& it = *ip;
@@ -971,10 +976,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       const bool flip = sc < 0.f;
       sc = fabsf(sc);
       if (F8 && te > tb) {
-        const int qb = nq % C::NQ;
-        wait_all(&ctrl->q_ok[qb], nq / C::NQ);
-        sc *= q_scale[(qb * QT + (PAIR ? t : 0)) * 128 + r];
-        ++nq;
+        wait_all(&ctrl->scale_ok[k % TR_ITEMS], k / TR_ITEMS);
+        sc *= q_scale[(k % TR_ITEMS * QT + (PAIR ? t : 0)) * 128 + r];
       }
       if (sc == 0.f) sc = 1.1754944e-38f;               // (all weights alike; 0 * inf would be NaN)
       float m = NEG_INF, mu = 0.f, l = 0.f;             // running maximum (reference), the same or 0 in its place; sum

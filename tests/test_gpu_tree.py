@@ -130,8 +130,8 @@ class Case:
 
 
 def close(got, want, size, fp8=False):
-    # the result is rounded once (2^-8 of it); the weights are rounded once (bf16 2^-8 of each, fp16 2^-11; q of ordinary size is
-    # exact in fp16); scores and sums are fp32 with exponentials good to 2^-22 (below 2^-12 of sum p |v| for scores up to a few hundred)
+    # the result is rounded once (2^-8 of it); the weights are rounded once (bf16 2^-8 of each, fp16 2^-11; over codes q is off by
+    # 2^-17.8 of a row's largest, 2^-13 of the weight for sums of |k| up to a few hundred); scores and sums are fp32 with exponentials good to 2^-22 (below 2^-12 of sum p |v| for scores up to a few hundred)
     got = got.double().cpu().numpy()
     assert np.isfinite(got).all()
     err, tol = abs(got - want), 2.0 ** -8 * abs(want) + ((2.0 ** -11 if fp8 else 2.0 ** -8) + 2.0 ** -12) * size + 1e-30
@@ -177,6 +177,20 @@ def test_many_short_sequences(fp8):
     n = r.integers(0, 7, 700)
     c = Case(n, n + r.integers(0, 300, 700), 8, 2, 128, 16, seed=2, fp8=fp8)
     close(c.run(), *c.want(), fp8)
+
+
+@pytest.mark.parametrize("d,Hq", [(64, 24), (128, 56)])
+@pytest.mark.parametrize("top", [16, 64])
+def test_short_sequences_in_numbers(d, Hq, top):
+    """Every CTA has several units of one or two key tiles: queries come and go faster than their weights."""
+    rng = np.random.default_rng(d + top)
+    n = rng.integers(1, top + 1, 200)
+    for fp8 in (True, False):
+        c = Case(n, n + rng.integers(0, 100, 200), Hq, 8, d, 64, seed=top, fp8=fp8)
+        first = c.run(top)
+        close(first, *c.want(), fp8)
+        for _ in range(20):
+            assert torch.equal(c.run(top), first)
 
 
 def test_lengths_of_every_kind():
