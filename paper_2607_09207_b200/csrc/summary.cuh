@@ -120,8 +120,11 @@ __device__ __forceinline__ void summarize_page(const SummaryParams& P, int page,
       wl[i] = wh[i] = 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        wl[i] |= (any_odd ? 0u : code_byte(floorf(a[4 * i + j] * inv))) << (8 * j);
-        wh[i] |= (any_odd ? 0u : code_byte(ceilf(b[4 * i + j] * inv))) << (8 * j);
+        // (a product may vanish in 32 bits beside keys that are far larger; its bound does not)
+        const float x = a[4 * i + j], y = b[4 * i + j];
+        const float down = fminf(floorf(x * inv), x < 0.f ? -1.f : 127.f), up = fmaxf(ceilf(y * inv), y > 0.f ? 1.f : -127.f);
+        wl[i] |= (any_odd ? 0u : code_byte(down)) << (8 * j);
+        wh[i] |= (any_odd ? 0u : code_byte(up)) << (8 * j);
       }
     }
     const int64_t at = static_cast<int64_t>(page) * P.Hkv + h;

@@ -113,6 +113,28 @@ def test_pages_filled_by_new_tokens(bs, d, fp8, one):
             assert (codes[p, h] == want[0]).all() and exps[p, h] == want[1], (p, h)
 
 
+@pytest.mark.parametrize("fp8", [False, True])
+def test_the_least_keys_beside_the_largest(fp8):
+    """A key below zero has a code below zero and one above zero a code above it, however small its share of the page's power of two."""
+    d, bs = 128, 16
+    if fp8:
+        k = torch.zeros(2, 1, bs, d, dtype=torch.uint8, device="cuda")
+        k[0, 0, 0, :4] = torch.tensor([0x7e, 0x81, 0x01, 0x80], dtype=torch.uint8, device="cuda")     # 448, -2^-9, 2^-9, -0
+        scale = torch.tensor([2.0 ** 100], device="cuda")
+        k[1, 0, :, :2] = torch.tensor([0x81, 0x01], dtype=torch.uint8, device="cuda")
+        k[1, 0, :, 2] = 0x7e
+    else:
+        k = torch.zeros(2, 1, bs, d, dtype=BF16, device="cuda")
+        k[0, 0, 0, :5] = torch.tensor([1e14, -1e-38, 1e-38, -0.0, 2.0 ** -133], dtype=torch.float64).to(BF16).cuda()
+        k[1, 0, :, :3] = torch.tensor([2.0 ** 25, -(2.0 ** -133), 2.0 ** -133], dtype=torch.float64).to(BF16).cuda()
+        scale = None
+    s = pdattn.PageSummary.create(2, 1, d)
+    pdattn.summarize_pages(k, s, i32([0, 1]), k_scale=scale)
+    for p in range(2):
+        want = summary_of(keys_of(k, p, 0, scale))
+        assert (s.codes[p, 0].cpu().numpy() == want[0]).all() and int(s.exponents[p, 0]) == want[1]
+
+
 def test_summary_of_a_page_that_is_none():
     k, _ = pool(5, 2, 16, 64)
     s = pdattn.PageSummary.create(5, 2, 64)
