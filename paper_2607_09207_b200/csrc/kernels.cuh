@@ -9,8 +9,11 @@
 // and, in translation units of their own:
 //   rope.cuh, pages.cuh   rope_append_kernel; the page bookkeeping (ops_api.cu)
 //   prefill_umma.cuh      prefill_kernel, prefill_join_kernel: prompt attention on tcgen05 (prefill_api.cu)
+//   tree_umma.cuh         tree_kernel, tree_join_kernel: trees of drafted tokens on tcgen05 (tree_api.cu)
+//   summary.cuh, accept.cuh   summarize_kernel, select_kernel: pages chosen by their keys' bounds; accept_kernel (sparse_api.cu)
 //   scored_api.cu         decode_kernel with modified scores and masks (scored.h)
-// umma.cuh holds the tcgen05 wrappers that both tensor-memory kernels use, host_common.h what the host sides share.
+//   selected_api.cu       decode_kernel over chosen pages (scored.h); both by variant_launch.cuh
+// umma.cuh holds the tcgen05 wrappers that the tensor-memory kernels use, host_common.h what the host sides share.
 #pragma once
 
 #include "common.cuh"
