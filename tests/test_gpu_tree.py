@@ -476,6 +476,33 @@ def test_trim():
     assert pdattn.check(ws) == pdattn.BAD_PAGE_INDEX
 
 
+@pytest.mark.parametrize("S", [300, 2500])
+def test_trim_of_many_rows(S):
+    """Many rows over many pages; every seventh cannot be served."""
+    bs, MB = 32, 40
+    r = np.random.default_rng(S)
+    lens = r.integers(0, MB * bs + 1, S)
+    NB = int((-(-lens // bs)).sum()) + 17
+    table, perm, at = np.full((S, MB), -1, np.int32), r.permutation(NB), 0
+    for s in range(S):
+        k = -(-int(lens[s]) // bs)
+        table[s, :k], at = perm[at:at + k], at + k
+    new = (lens * r.random(S)).astype(np.int64)
+    new[::7] = lens[::7] + 1
+    ref, free, count = books(table, lens, NB, bs)
+    dev = [i32(x) for x in (table, lens, ref, free, [count])]
+    ws = pdattn.alloc_pages_workspace(NB, S)
+    pdattn.pages_trim(pdattn.PagePool(*dev[2:]), dev[0], dev[1], i32(new), bs, ws)
+    assert pdattn.check(ws) == pdattn.BAD_SEQUENCE
+    for s in range(S):
+        if s % 7:
+            lens[s] = new[s]
+            table[s, -(-int(new[s]) // bs):] = -1
+    ref, free, count = books(table, lens, NB, bs)
+    for got, want in zip(dev, (table, lens, ref, free, [count])):
+        assert (got.cpu().numpy() == want).all()
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_rotation_positions_are_the_callers(fp8, interleaved):
