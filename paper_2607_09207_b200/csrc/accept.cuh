@@ -86,8 +86,10 @@ accept_kernel(const __grid_constant__ AcceptParams P) {
     };
     uint8_t v[PV];
 #pragma unroll
-    for (int e = 0; e < PV; ++e)
+    for (int e = 0; e < PV; ++e) {
+      if (e * ROWS >= a) break;                            // (short paths pay for their own tokens only)
       if (i0 + e * ROWS < a) v[e] = *column(src[i0 + e * ROWS]);
+    }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
@@ -95,8 +97,10 @@ accept_kernel(const __grid_constant__ AcceptParams P) {
       if (i < a) *row(P.k, dst[i], piece) = k[e];
     }
 #pragma unroll
-    for (int e = 0; e < PV; ++e)
+    for (int e = 0; e < PV; ++e) {
+      if (e * ROWS >= a) break;
       if (i0 + e * ROWS < a) *column(dst[i0 + e * ROWS]) = v[e];
+    }
   }
 }
 

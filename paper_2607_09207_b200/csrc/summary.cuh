@@ -12,6 +12,10 @@
 // by the 2 d + 1 bytes it reads per page-head.  The products run on int8 MMAs straight from global memory: a lane's 16-byte loads
 // are fragments of two MMAs when the contraction index is permuted alike in both operands, so nothing passes through shared
 // memory.  The block that finishes a (sequence, KV head) last picks its pages: no second launch.
+//
+// Times (replays of a graph): summaries of 12 prompts of 700 to 2100 tokens (8 heads of 128, pages of 16, 38 MB) 9.5 us, of the pages
+// that 256 single tokens fill 3.7 us (the launch and three dependent loads); 128 of up to 2048 pages for 48 sequences x 8 KV heads (100 MB)
+// 25.5 us, the choice of the last units behind their scores; 6 sequences x 4 KV heads of up to 250 pages 7.0 us (latency of one block).
 #pragma once
 
 #include <climits>
