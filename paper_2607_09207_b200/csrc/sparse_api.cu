@@ -40,7 +40,7 @@ pdattn_status summarize(SummaryParams& P, int head_dim, bool fp8, int64_t grid, 
 }
 
 // Pages that a block of select_kernel scores: as many, from 256 to 2048, as leave four blocks an SM (48 sequences to 32,768 tokens, 64/8
-// heads: 25 us with 1024, 29 with 512).  More units than the workspace's zeroed words can number are enough by themselves: a block takes a
+// heads: 25 us with 1024, 29 with 512, 36 with 2048).  More units than the workspace's zeroed words can number are enough by themselves: a block takes a
 // whole one.
 int select_chunk(int64_t units, int pages, int sms) {
   int chunk = 2048;
