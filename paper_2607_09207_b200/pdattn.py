@@ -815,8 +815,9 @@ class PageSummary:
 
     def __init__(self, codes, exponents):
         _expect_dense("PageSummary", torch.int8, codes, exponents)
-        if codes.dim() != 4 or codes.shape[2] != 2 or tuple(exponents.shape) != tuple(codes.shape[:2]):
-            raise ValueError(f"PageSummary: codes {tuple(codes.shape)} and exponents {tuple(exponents.shape)} do not belong together")
+        self.shape = shape = codes.shape
+        if len(shape) != 4 or shape[2] != 2 or exponents.shape != shape[:2]:
+            raise ValueError(f"PageSummary: codes {tuple(shape)} and exponents {tuple(exponents.shape)} do not belong together")
         self.codes, self.exponents = codes, exponents
         self.device = codes.get_device()
 
@@ -828,24 +829,26 @@ class PageSummary:
 
 def _summary_args(where, k_cache, summary: PageSummary, k_scale, workspace) -> SummaryArgs:
     NB, Hkv, bs, d = k_cache.shape
-    if k_cache.dtype == torch.uint8:
+    strides = k_cache.stride()
+    codes = k_cache.dtype is torch.uint8
+    if codes:
         _expect_dense(where, torch.uint8, k_cache)
         if k_scale is None or k_scale.numel() != Hkv:
             raise ValueError(f"{where}: a pool of codes comes with one k_scale per KV head")
         _expect_dense(where, torch.float32, k_scale)
     else:
         _expect(where, torch.bfloat16, k_cache)
-        if k_cache.stride(3) != 1:
+        if strides[3] != 1:
             raise ValueError(f"{where}: head_dim has to be contiguous")
         if k_scale is not None:
             raise ValueError(f"{where}: k_scale belongs to a pool of codes")
     if workspace is not None:
         _expect_workspace(where, workspace)
     _expect_device(where, summary.device)
-    if tuple(summary.codes.shape) != (NB, Hkv, 2, d):
-        raise ValueError(f"{where}: a cache {tuple(k_cache.shape)} with summaries {tuple(summary.codes.shape)}")
+    if summary.shape != (NB, Hkv, 2, d):
+        raise ValueError(f"{where}: a cache {tuple(k_cache.shape)} with summaries {tuple(summary.shape)}")
     return SummaryArgs(k_cache.data_ptr(), _ptr(k_scale), summary.codes.data_ptr(), summary.exponents.data_ptr(), Hkv, d, bs, NB,
-                       k_cache.element_size(), *k_cache.stride()[:3], _ptr(workspace))
+                       1 if codes else 2, strides[0], strides[1], strides[2], _ptr(workspace))
 
 
 def summarize_append(k_cache, summary: PageSummary, block_table, context_lens, cu_tokens=None, num_tokens: Optional[int] = None, k_scale=None,
@@ -902,13 +905,13 @@ def select_pages(q, summary: PageSummary, block_table, context_lens, selected, b
     _expect_workspace(where, workspace)
     _expect_device(where, summary.device)
     S, Hq, d = q.shape
-    NB, Hkv = summary.exponents.shape
-    MB = block_table.shape[1]
-    if (block_table.shape[0] != S or context_lens.numel() != S or selected.dim() != 3 or tuple(selected.shape[:2]) != (S, Hkv)
-            or summary.codes.shape[3] != d):
+    NB, Hkv, _, dim = summary.shape
+    rows, MB = block_table.shape
+    lists = selected.shape
+    if rows != S or context_lens.numel() != S or len(lists) != 3 or lists[0] != S or lists[1] != Hkv or dim != d:
         raise ValueError(f"{where}: shapes do not belong together")
     a = SelectArgs(q.data_ptr(), summary.codes.data_ptr(), summary.exponents.data_ptr(), block_table.data_ptr(), context_lens.data_ptr(),
-                   selected.data_ptr(), S, Hq, Hkv, d, block_size, MB, NB, selected.shape[2], num_first, num_recent, workspace.data_ptr(),
+                   selected.data_ptr(), S, Hq, Hkv, d, block_size, MB, NB, lists[2], num_first, num_recent, workspace.data_ptr(),
                    workspace.numel())
     st = lib().pdattn_select_pages(ctypes.byref(a), _stream_ptr(stream))
     if check and st != OK:
