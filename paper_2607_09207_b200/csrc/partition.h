@@ -162,7 +162,7 @@ PDATTN_HD inline int selected_pages(int context_len, int block_size, int num_sel
 // position r of a sequence's stretch falls: the unit and the key tile it begins at.  A cut nearer than kTreeMinCut tiles to a unit's
 // end moves there (a unit shorter than twice that stays whole), and no more CTAs are used than give each a unit or that many tiles.
 constexpr int kTreeKeys = 64;      // keys of a tile
-constexpr int kTreeStart = 4;
+constexpr int kTreeStart = 8;      // (256 x 8 tokens, 28/4 heads: 4 us a unit, 0.65 a tile; 4 in its place: 253 instead of 249 us, fp8 32 x 16 314 instead of 306)
 constexpr int kTreeMinCut = 8;
 PDATTN_HD inline void tree_cut(int64_t r, int64_t tiles, int* unit, int* tile) {
   const int64_t per = tiles + kTreeStart;

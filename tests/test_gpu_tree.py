@@ -296,6 +296,28 @@ def test_what_a_token_does_not_see_may_be_anything(fp8, n):
     assert not out[:n[0], 4:, 9].isfinite().any() and out[:n[0], :4].isfinite().all() and out[n[0]:].isfinite().all()
 
 
+@pytest.mark.parametrize("d,G", [(128, 7), (64, 4), (128, 2), (64, 16)])
+@pytest.mark.parametrize("n", [4, 9, 64])
+@pytest.mark.parametrize("hist", [200, 9000])
+def test_infinities_that_every_token_sees(d, G, n, hist):
+    """Of the history's V: an infinity alone gives itself, infinities of both signs or a NaN give NaN, the other channels stay."""
+    ns = np.array([n, 1, max(1, n - 1)])
+    c = Case(ns, ns + np.array([hist, 70, hist // 2]), G, 1, d, 32, seed=d + G)
+    want, size = c.want()
+    for s in (0, 2):
+        for key, channel, x in [(5, 0, math.inf), (40, 3, -math.inf), (77, d - 1, math.inf), (3, 9, math.inf), (61, 9, -math.inf), (90, 33, math.nan)]:
+            c.v[int(c.tab[s, key // 32]), 0, key % 32, channel] = x
+        rows = slice(int(c.cu[s]), int(c.cu[s + 1]))
+        for channel, x in [(0, math.inf), (3, -math.inf), (d - 1, math.inf), (9, math.nan), (33, math.nan)]:
+            want[rows, :, channel] = x
+    got = c.run()
+    odd = ~np.isfinite(want)
+    assert (np.isnan(want[odd]) == np.isnan(got.double().cpu().numpy()[odd])).all()
+    assert np.array_equal(np.nan_to_num(want[odd], posinf=1, neginf=-1), np.nan_to_num(got.double().cpu().numpy()[odd], posinf=1, neginf=-1))
+    odd = torch.from_numpy(odd).cuda()
+    close(torch.where(odd, 0, got), np.where(odd.cpu().numpy(), 0, want), size)
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_bad_pages_and_rows_that_are_too_short(fp8):
     n = np.array([6, 40, 7])
