@@ -15,7 +15,8 @@
 //
 // Times (replays of a graph): summaries of 12 prompts of 700 to 2100 tokens (8 heads of 128, pages of 16, 38 MB) 9.5 us, of the pages
 // that 256 single tokens fill 3.7 us (the launch and three dependent loads); 128 of up to 2048 pages for 48 sequences x 8 KV heads (100 MB)
-// 25.5 us, the choice of the last units behind their scores; 6 sequences x 4 KV heads of up to 250 pages 7.0 us (latency of one block).
+// 24.6 us, of which 17 are scores (a warp's 16 pages take 2 us, most of it latency), 1.5 the tickets and 4 the choice of the last units;
+// 6 sequences x 4 KV heads of up to 250 pages 6.4 us (latency of one block).  Equal parts for a unit's blocks: 25.5 instead of 24.6.
 #pragma once
 
 #include <climits>
@@ -234,15 +235,15 @@ __device__ __forceinline__ T block_exclusive(T v, T* warp_sums) {
 
 // The R largest of M keys, ties to the lower index, as ascending page numbers out[0 .. R).  Thread t owns the indices t * each ..
 // + each - 1, in registers up to E of them (E = 0: read again in every round).  Keys that this block has just written lie in its shared
-// memory.  The R-th largest key is found eight bits at a time,
-// from the highest in which the keys differ: a histogram of the keys that agree with it so far, and the bin in which the count from
-// above reaches R.  (Bit by bit, with 32 counts, 2048 keys took 2.5 us longer.)
+// memory.  The R-th largest key is found eight bits at a time, from the highest in which the keys differ: a histogram of the keys that
+// agree with it so far, and the bin in which the count from above reaches R, until all of a bin is wanted.  (Bit by bit, with 32
+// counts, 2048 keys took 2.5 us longer; without the early end 0.6.)
 struct SelectScratch {
   int bins[2][256];
   int warp_counts[SEL_THREADS / 32];
   unsigned long long warp_sums[SEL_THREADS / 32];
   uint32_t ends[2], digit;
-  int left;
+  int left, in_bin;
 };
 static_assert(SEL_THREADS == 256, "a thread per bin");
 // (A function of its own: inlined, its registers slowed the scoring loop, 25.5 -> 31 us for 48 sequences to 32,768 tokens.)
@@ -304,22 +305,26 @@ __device__ __noinline__ void take_largest(const uint32_t* keys, int M, int R, in
     if (above < want && above + n >= want) {
       sh->digit = static_cast<uint32_t>(255 - tid);
       sh->left = want - above;
+      sh->in_bin = n;
     }
     __syncthreads();
     t |= sh->digit << shift;
     want = sh->left;
     low = shift;
+    if (want == sh->in_bin) break;                      // all of the bin: the bits below do not matter
   }
+  t >>= low;                                            // (low < 32)
   // keys above t, and `want` of those equal to it in order: both counts scanned as one 64-bit word
   int gt = 0, eq = 0;
   each_key([&](int, uint32_t k) {
-    gt += k > t ? 1 : 0;
-    eq += k == t ? 1 : 0;
+    gt += (k >> low) > t ? 1 : 0;
+    eq += (k >> low) == t ? 1 : 0;
   });
   const unsigned long long before =
       block_exclusive((static_cast<unsigned long long>(gt) << 32) | static_cast<unsigned>(eq), sh->warp_sums);
   int g = static_cast<int>(before >> 32), q = static_cast<int>(before & 0xffffffffull);
   each_key([&](int j, uint32_t k) {
+    k >>= low;
     if (k > t || (k == t && q < want)) out[g + min(q, want)] = first + i0 + j;
     if (k > t) ++g;
     if (k == t) ++q;
@@ -458,13 +463,11 @@ select_kernel(const __grid_constant__ SelectParams P) {
   __syncthreads();
   if (blocks > 1) {
     if (tid == 0) {
-      __threadfence();
-      const int k = atomicAdd(P.tickets + unit, 1);
+      int k;
+      // (release: this block's keys; acquire: those of the others)
+      asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(k) : "l"(P.tickets + unit) : "memory");
       is_last = k == blocks - 1;
-      if (is_last) {
-        P.tickets[unit] = 0;
-        __threadfence();
-      }
+      if (is_last) P.tickets[unit] = 0;
     }
     __syncthreads();
     if (!is_last) return;

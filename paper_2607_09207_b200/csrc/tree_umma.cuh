@@ -35,12 +35,15 @@
 // running maximum when that grew by more than 2^8, so O is rarely rescaled.
 //
 // Bound and times (replays of a graph; in brackets under the power cap, which long runs of this kernel reach):
-//   256 sequences x up to 8 tokens over up to 4600 keys, 28/4 heads of 128    250 us [290]   bytes, 5.5 TB/s
+//   256 sequences x up to 8 tokens over up to 4600 keys, 28/4 heads of 128    248 us [290]   bytes, 5.6 TB/s; 4 us a unit at the change from one
+//       to the next (the groups meet, results), 0.65 a key tile
 //   8 x 64 over up to 32,000, 64/8 heads    324 us [385]   0.94 PFLOP/s: the chain of a group, scores -> weights -> product; a
 //       key tile takes a pair of row tiles 1950 cycles, 1280 of them MMAs (48 cycles one of scores: 128 x 16 x 64, Q from shared memory)
-//   32 x 16 over up to 32,767, e4m3 codes, 64/8 heads    307-317 us [365]   the same; 1190 cycles a key tile, 640 of them MMAs
+//   32 x 16 over up to 32,767, e4m3 codes, 64/8 heads    304 us [356]   the same; 1190 cycles a key tile, 640 of them MMAs
 // Built and not faster: key tiles of 128 read twice (8 x 64 417 instead of 385 under the cap), two warps a row (324 -> 372, codes
-// 306 -> 355: the chain's latencies stay and its halves have to meet), the maximum of the tile before, turns at the exponential unit.
+// 306 -> 355: the chain's latencies stay and its halves have to meet), the maximum of the tile before, turns at the exponential unit,
+// four loading warps instead of two (256 x 8: the same).  Rows of small trees twice in the row tile, each with half of a tile's keys, so
+// that all softmax warps work (at most 64 rows): 249 -> 246, not worth a form of its own.
 //
 // Every wait is bounded; on expiry the CTA raises ERR_TIMEOUT, the waits fall through, the MMA warp drains, tensor memory is
 // freed and the CTA returns.
