@@ -1296,7 +1296,8 @@ tree_join_kernel(const __grid_constant__ TreeParams P, int ctas) {
     float y[TR_JOIN_COLS];
 #pragma unroll
     for (int i = 0; i < TR_JOIN_COLS; ++i) y[i] = from[(q * TR_JOIN_COLS + i) * 128];
-    if (m == NEG_INF) continue;                          // saw nothing: what it holds may be anything
+    // Saw nothing: what it holds may be anything.  (Scores that are all NaN leave the maximum there too, but not the sum: it stays.)
+    if (m == NEG_INF && l == 0.f) continue;
     const float f = fast_exp2(m - M);
     L += l * f;
 #pragma unroll
