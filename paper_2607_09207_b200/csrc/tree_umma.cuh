@@ -1109,13 +1109,16 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         wait_all(&ctrl->pv_done[t][last], (ns >> last) ^ 1u);   // the last product is done, and with it those before it
         tc_fence_after();
       }
-      float f[2] = {0.f, 0.f};                          // factors of O_0 and O_1 in this row's output
+      // Factors of O_0 and O_1 in this row's output; below 0: the row saw nothing there, and what O holds may be anything.  (A factor of
+      // 0 is a weight that vanishes: what is not finite stays so.)
+      constexpr float kUnseen = -1.f;
+      float f[2] = {kUnseen, kUnseen};
       bool have[2];
       const bool whole = it.part < 0;
       if (PAIR) {
         have[0] = any && t == 0;
         have[1] = any && t == 1;
-        f[t] = whole ? (l > 0.f ? 1.f / l : (l != l ? l : 0.f)) : 1.f;
+        f[t] = l == 0.f ? kUnseen : whole ? 1.f / l : 1.f;
       } else {
         const int even = tb + (c0 & 1), odds = tb + ((c0 & 1) ^ 1);
         have[0] = te > even;
@@ -1128,15 +1131,18 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         if (t == 0) {
           const float2 other = ctrl->ml[r];
           const float M = fmaxf(m, other.x);
+          const bool saw0 = l != 0.f, saw1 = other.y != 0.f;
           f[0] = m == NEG_INF ? 0.f : fast_exp2(m - M);
           f[1] = other.x == NEG_INF ? 0.f : fast_exp2(other.x - M);
           m = M;
           l = l * f[0] + other.y * f[1];
           if (whole) {
-            const float inv = l > 0.f ? 1.f / l : (l != l ? l : 0.f);
+            const float inv = 1.f / l;                  // (used where something was seen)
             f[0] *= inv;
             f[1] *= inv;
           }
+          if (!saw0) f[0] = kUnseen;
+          if (!saw1) f[1] = kUnseen;
           ctrl->ml[r] = make_float2(f[0], f[1]);
         }
         meet();
@@ -1147,6 +1153,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         tc_fence_after();                               // (the other group's O: its product was seen to be done before the barrier)
       }
+      const bool saw[2] = {!(f[0] < 0.f), !(f[1] < 0.f)};
       f[0] *= vs;
       f[1] *= vs;
       if (mine && busy) {
@@ -1170,9 +1177,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             uint32_t o[32];
             tmem_ld32(tbase + C::COL_O + tt * D + lane_addr + q * 32, o);
             tc_wait_ld();
-            // (a factor of 0: the row saw nothing in those tiles, and what O holds may be anything)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = f[tt] != 0.f ? fmaf(__uint_as_float(o[i]), f[tt], v[i]) : v[i];
+            for (int i = 0; i < 32; ++i) v[i] = saw[tt] ? fmaf(__uint_as_float(o[i]), f[tt], v[i]) : v[i];
           }
           if (odd && sees) {
             float add[32];                              // (a copy: v stays in registers)

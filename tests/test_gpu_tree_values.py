@@ -43,3 +43,40 @@ def test_scales_that_are_not_numbers(n, hist):
         out = c.run()
         assert out[:, 4:].isnan().all()
         close(out[:, :4], want[:, :4], size[:, :4], True)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("n,hist", [(4, 700), (4, 9000), (64, 700), (64, 9000)])
+@pytest.mark.parametrize("high", [0, 3, 6])
+def test_values_that_are_not_finite_where_the_weight_vanishes(fp8, n, hist, high):
+    """One key tile 500 above all others: an infinity or NaN of V in any other tile of the history still leaves its element not finite."""
+    d, bs, heads = 64, 16, 4
+    tiles = hist // 64
+    for low in sorted({t for t in (0, 1, 2, 3, 4, 5, 6, 7, tiles - 1) if t != high}):
+        c = Case([n], [n + hist], heads, 1, d, bs, seed=1, fp8=fp8)
+        dead = (c.v.view(torch.float8_e4m3fn) if fp8 else c.v).float().isnan().any(2 if fp8 else 3)[:, 0]     # [page, slot]
+        if fp8:
+            c.ks.fill_(1.0)
+        c.q.zero_()
+        c.q[:, :, 0] = 8.0
+        c.scale = 1.0
+        c.k.zero_()
+        key = np.arange(high * 64, high * 64 + 64)
+        pages, slots = (torch.from_numpy(x).cuda() for x in (c.tab[0, key // bs].astype(np.int64), key % bs))
+        c.k[pages, 0, slots, 0] = 0x6c if fp8 else 64.0                # 64 as a code is 0x68, 96 is 0x6c: 512 and 768 above the others
+        want, size = c.want()
+        bad = [(9, math.nan)] if fp8 else [(9, math.inf), (33, -math.inf), (50, math.nan)]
+        for channel, x in bad:
+            t = low * 64 + channel
+            p, s = int(c.tab[0, t // bs]), t % bs
+            assert not dead[p, s]
+            if fp8:
+                c.v[p, 0, channel, s] = 0x7f
+            else:
+                c.v[p, 0, s, channel] = x
+        out = c.run()
+        at = [ch for ch, _ in bad]
+        assert not out[:, :, at].isfinite().any(), low
+        out[:, :, at] = 0
+        want[:, :, at], size[:, :, at] = 0, 0
+        close(out, want, size, fp8)
