@@ -31,8 +31,13 @@
 // in the second product.
 //
 // Numbers: scores, maxima, sums and O in fp32.  The weights are rounded to bf16 for the second product (at most 2^-8 of each,
-// independent; the fp8 form to fp16, 2^-11): the size of the final rounding.  The reference of the online softmax follows the
-// running maximum when that grew by more than 2^8, so O is rarely rescaled.
+// independent): the size of the final rounding.  The reference of the online softmax follows the running maximum when that grew by
+// more than 2^8, so O is rarely rescaled.  The fp8 form rounds them to fp16 (2^-11 of each), whose range is short: all carry a factor
+// 2^11, which l and O then have alike, and the reference, a whole number at or above the maximum when it moves, lags by 2^4 at most.
+// So weights end at 2^15 and have all bits down to 2^-24 of the row's largest; smaller ones are off by at most 2^-35 of it.  (With plain
+// weights what lies 2^-25 below vanished, and with it what thousands of keys 17 below the largest score add up to.)  All rows of a warp
+// move their references when one must: the factors are powers of two, so that changes no bit of them, and there are fewer moves (each
+// row by itself, with a lag of 2^2: 304 -> 342 us for 32 x 16 tokens).
 //
 // Bound and times (replays of a graph; in brackets under the power cap, which long runs of this kernel reach):
 //   256 sequences x up to 8 tokens over up to 4600 keys, 28/4 heads of 128    248 us [290]   bytes, 5.6 TB/s; 4 us a unit at the change from one
@@ -971,6 +976,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     const TreeItem* ip;
     int c0 = 0;                        // key tiles of the CTA before this item
     uint32_t ns = 0;                   // bit b: parity of s_full (and of p_full, pv_done) of this group's buffer b
+    constexpr float kLag = F8 ? 4.f : 8.f, kFactor = 11.f;   // (base 2)
     for (int k = 0; get_item(k, ip); ++k) {
       const TreeItem& it = *ip;
       const int tb = it.tb, te = it.te, edge = it.edge, rows = it.rows[t], keys = it.keys;
@@ -1041,11 +1047,13 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
 #pragma unroll
         for (int i = 0; i < 64; i += 2) m4[(i >> 1) & 3] = max3(m4[(i >> 1) & 3], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
         float mx = fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]);
-        mx = mx == NEG_INF ? NEG_INF : mx * sc;
+        mx = mx == NEG_INF ? NEG_INF : F8 ? ceilf(__fmul_ru(mx, sc)) : mx * sc;
         float alpha = 1.f;
-        // the reference moves with the first tile, and when the maximum grew by more than 2^8
-        if (__any_sync(0xffffffffu, valid && (first || mx > m + 8.f))) {
-          const bool grow = first || mx > m + 8.f;
+        // The reference moves with the first tile, and when the maximum grew by more than 2^kLag.  (Codes: rounded so that no weight
+        // leaves fp16's range where fp32 cannot tell such scores apart any more.)
+        bool grow = first || mx > (F8 ? __fadd_rd(m, kLag) : m + kLag);
+        if (__any_sync(0xffffffffu, valid && grow)) {
+          if (F8) grow = true;
           const float m_new = grow ? fmaxf(m, mx) : m;
           mu = m_new == NEG_INF ? 0.f : m_new;
           alpha = grow ? fast_exp2(m - mu) : 1.f;
@@ -1066,7 +1074,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           }
         }
         uint64_t sum0 = 0ull, sum1 = 0ull;
-        const uint64_t sc2 = tree_pack2(sc, sc), mu2 = tree_pack2(-mu, -mu);
+        const float off = F8 ? __fadd_rd(kFactor, -mu) : -mu;
+        const uint64_t sc2 = tree_pack2(sc, sc), mu2 = tree_pack2(off, off);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t pk[16];

@@ -80,3 +80,59 @@ def test_values_that_are_not_finite_where_the_weight_vanishes(fp8, n, hist, high
         out[:, :, at] = 0
         want[:, :, at], size[:, :, at] = 0, 0
         close(out, want, size, fp8)
+
+
+def far_below(c, nats, sinks):
+    """All keys score 0 but one per KV head, `nats` above, whose V is 0: what is left is the weights of the many."""
+    c.ks.fill_(1.0)
+    c.scale = 1.0
+    c.k.zero_()
+    c.q.zero_()
+    c.q[:, :, 0] = nats
+    for s, t in enumerate(sinks):
+        p, slot = int(c.tab[s, t // c.bs]), t % c.bs
+        c.k[p, :, slot, 0] = 0x38                          # 1.0
+        c.v[p, :, :, slot] = 0
+
+
+@pytest.mark.parametrize("nats", [6.0, 10.0, 14.0, 17.5, 18.5, 22.0])
+@pytest.mark.parametrize("n", [4, 64])
+@pytest.mark.parametrize("sink", ["first", "middle", "last"])
+def test_many_small_weights_over_codes(nats, n, sink):
+    """A key that takes nearly all of the weight and has no V, over thousands of others (the reference they are measured from)."""
+    ns = np.array([n, 2, n])
+    hist = np.array([30000, 400, 3000])
+    c = Case(ns, ns + hist, 8, 2, 64, 32, seed=n, fp8=True)
+    far_below(c, nats, {"first": [0] * 3, "middle": list(hist // 2), "last": list(hist - 1)}[sink])
+    got = c.run().double().cpu().numpy()
+    want, size = c.want()
+    assert np.isfinite(got).all()
+    # as in close(): weights fp16, 2^-11 of each while they are normal, that is down to 2^-24 of the largest (16.6 nats); from there on off by
+    # at most half of fp16's least step, 2^-25, beside a largest of 2^10 or more: 2^-35 of that, 2^-35 e^nats of such a weight
+    weights = max(2.0 ** -11, 2.0 ** -35 * math.exp(nats))
+    tol = 2.0 ** -8 * abs(want) + (weights + 2.0 ** -12) * size + 1e-30
+    err = abs(got - want)
+    assert (err <= tol).all(), (err / tol).max()
+
+
+@pytest.mark.parametrize("n", [4, 64])
+def test_scores_that_grow_and_are_large(n):
+    """The maximum rises with every key tile, by little and by much, up to scores of some 10^6: no weight leaves fp16's range."""
+    for step in (0.5, 2.0, 24.0):
+        ns = np.array([n, n])
+        c = Case(ns, ns + np.array([9000, 640]), 8, 2, 64, 32, seed=n, fp8=True)
+        c.ks.fill_(1.0)
+        c.k.zero_()
+        c.q.zero_()
+        # a key of tile t of the history scores q . k = 8 a + b/2 with t = 16 a + b (a < 16, b < 16), times the scale
+        c.q[:, :, 0], c.q[:, :, 1] = 8.0, 0.5
+        c.scale = 2.0 * step
+        for s in range(2):
+            for t in range(int(c.L[s]) // 64):
+                key = np.arange(t * 64, t * 64 + 64)
+                pages, slots = (torch.from_numpy(x).cuda() for x in (c.tab[s, key // 32].astype(np.int64), key % 32))
+                for ch, x in ((0, t // 16), (1, t % 16)):
+                    c.k[pages, :, slots, ch] = int(torch.tensor(float(x)).to(torch.float8_e4m3fn).view(torch.uint8))
+        close(c.run(), *c.want(), True)
+    c.q.mul_(512.0)                                          # one tile's keys, equal among themselves, take all
+    close(c.run(), *c.want(), True)
