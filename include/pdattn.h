@@ -172,7 +172,8 @@ pdattn_status pdattn_decode_multi(const pdattn_args* args, int num_query_tokens,
  * Both pools dense (the stride fields of args are ignored); everything else as in pdattn_decode_ex,
  * including the treatment of bad page ids and of slots past the end (any code, NaN codes too).
  * The codes are widened exactly; q is rounded to fp16 for the products (values below 2^-14 lose bits) and
- * the softmax weights to fp16 (11 bits), accumulation in fp32; out is bf16.
+ * the softmax weights to fp16 (2^-11 of each down to 2^-29 of the row's largest, 2^-40 of the largest below),
+ * accumulation in fp32; out is bf16.
  *   Requirements: head_dim 128 or 64, every page size of pdattn_decode_ex.  Workspace as for pdattn_decode_ex.
  */
 pdattn_status pdattn_decode_fp8(const pdattn_args* args, const float* k_scale, const float* v_scale,

@@ -178,46 +178,25 @@ __device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 __device__ __forceinline__ int tree_uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }   // known to be the same in every lane
-__device__ __forceinline__ uint64_t tree_pack2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void tree_unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ uint64_t tree_fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t tree_add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ uint64_t tree_mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // 2^x of two values on the FMA pipe, x <= 127: x = n + f with n the nearest whole number, and 2^f by the polynomial of degree 4 with the
 // smallest largest relative error on [-1/2, 1/2] (2^-18.5).  0 from x = -126.5 down, NaN for NaN.
 __device__ __forceinline__ void tree_exp2_pair(float& a, float& b) {
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-127.f));
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-127.f));
-  const uint64_t x = tree_pack2(a, b);
+  const uint64_t x = pack_f32x2(a, b);
   constexpr float kMagic = 12582912.f;               // 1.5 * 2^23: the sum's last bits are n
-  const uint64_t t = tree_add2(x, tree_pack2(kMagic, kMagic));
-  const uint64_t n = tree_add2(t, tree_pack2(-kMagic, -kMagic));
-  const uint64_t f = tree_fma2(n, tree_pack2(-1.f, -1.f), x);
-  uint64_t p = tree_fma2(tree_pack2(0.009570089168846607f, 0.009570089168846607f), f, tree_pack2(0.05591785907745361f, 0.05591785907745361f));
-  p = tree_fma2(p, f, tree_pack2(0.2402474582195282f, 0.2402474582195282f));
-  p = tree_fma2(p, f, tree_pack2(0.6931217908859253f, 0.6931217908859253f));
-  p = tree_fma2(p, f, tree_pack2(0.9999992847442627f, 0.9999992847442627f));
+  const uint64_t t = add_f32x2(x, pack_f32x2(kMagic, kMagic));
+  const uint64_t n = add_f32x2(t, pack_f32x2(-kMagic, -kMagic));
+  const uint64_t f = fma_f32x2(n, pack_f32x2(-1.f, -1.f), x);
+  uint64_t p = fma_f32x2(pack_f32x2(0.009570089168846607f, 0.009570089168846607f), f, pack_f32x2(0.05591785907745361f, 0.05591785907745361f));
+  p = fma_f32x2(p, f, pack_f32x2(0.2402474582195282f, 0.2402474582195282f));
+  p = fma_f32x2(p, f, pack_f32x2(0.6931217908859253f, 0.6931217908859253f));
+  p = fma_f32x2(p, f, pack_f32x2(0.9999992847442627f, 0.9999992847442627f));
   float ta, tb;
-  tree_unpack2(t, ta, tb);
-  p = tree_mul2(p, tree_pack2(__uint_as_float((__float_as_uint(ta) << 23) + 0x3f800000u),
+  unpack_f32x2(t, ta, tb);
+  p = mul_f32x2(p, pack_f32x2(__uint_as_float((__float_as_uint(ta) << 23) + 0x3f800000u),
                               __uint_as_float((__float_as_uint(tb) << 23) + 0x3f800000u)));
-  tree_unpack2(p, a, b);
+  unpack_f32x2(p, a, b);
 }
 // D[tmem] (+)= A[smem] . B[smem], e4m3 operands
 __device__ __forceinline__ void umma_ss_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum) {
@@ -1075,14 +1054,14 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         uint64_t sum0 = 0ull, sum1 = 0ull;
         const float off = F8 ? __fadd_rd(kFactor, -mu) : -mu;
-        const uint64_t sc2 = tree_pack2(sc, sc), mu2 = tree_pack2(off, off);
+        const uint64_t sc2 = pack_f32x2(sc, sc), mu2 = pack_f32x2(off, off);
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t pk[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             float p0, p1;
-            tree_unpack2(tree_fma2(tree_pack2(__uint_as_float(x[q * 32 + 2 * i]), __uint_as_float(x[q * 32 + 2 * i + 1])), sc2, mu2), p0, p1);
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[q * 32 + 2 * i]), __uint_as_float(x[q * 32 + 2 * i + 1])), sc2, mu2), p0, p1);
             // PAIR: a quarter on the FMA pipe (8 x 64 tokens 388 -> 379 us under the power cap; split, 256 x 8: 281 -> 287)
             if (PAIR && (i & 3) == 3) {
               tree_exp2_pair(p0, p1);
@@ -1090,9 +1069,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
               p0 = fast_exp2(p0);
               p1 = fast_exp2(p1);
             }
-            const uint64_t pp = tree_pack2(p0, p1);
-            if (i & 1) sum1 = tree_add2(sum1, pp);
-            else sum0 = tree_add2(sum0, pp);
+            const uint64_t pp = pack_f32x2(p0, p1);
+            if (i & 1) sum1 = add_f32x2(sum1, pp);
+            else sum0 = add_f32x2(sum0, pp);
             pk[i] = F8 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);
           }
           tmem_st16(tS + b * 64 + q * 16, pk);          // (over scores that have been read)
@@ -1106,8 +1085,8 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         last = b;
         {
           float a0, a1, b0, b1;
-          tree_unpack2(sum0, a0, a1);
-          tree_unpack2(sum1, b0, b1);
+          unpack_f32x2(sum0, a0, a1);
+          unpack_f32x2(sum1, b0, b1);
           l = l * alpha + ((a0 + a1) + (b0 + b1));
         }
       }

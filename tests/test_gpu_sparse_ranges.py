@@ -1,0 +1,60 @@
+"""Sparse steps at the borders of their kernels' forms, and values far apart."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_09207_b200 import pdattn
+from paper_2607_09207_b200 import workloads as W
+from test_gpu_sparse import F8, i32, reference, run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("nats", [6.0, 9.0, 12.0, 17.5, 19.0, 24.0])
+@pytest.mark.parametrize("form", ["selected", "plain", "grouped", "scored"])
+def test_many_small_weights_over_codes(nats, form):
+    """A key that takes nearly all of the weight and has no V, over thousands of others."""
+    bs, d, Hq, Hkv = 32, 128, 8, 2
+    w = W.make_custom([20000, 20000, 300, 6000], Hq, Hkv, d, bs, seed=5, device="cuda:0")
+    one, vs = torch.ones(2, device="cuda"), torch.full((2,), 0.03, device="cuda")
+    k8, v8 = W.fp8_caches(w, one, vs)
+    if form == "grouped":                                      # rows 0 and 1 share their first pages
+        w.block_table[1, :300] = w.block_table[0, :300]
+    k8.zero_()
+    w.q.zero_()
+    w.q[:, :, 0] = nats
+    w.scale = 1.0
+    table = w.block_table.cpu().numpy()
+    for s, t in enumerate((700, 700, 5, 5999)):
+        p, slot = int(table[s, t // bs]), t % bs
+        k8[p, :, slot, 0] = 0x38                               # 1.0
+        v8[p, :, :, slot] = 0
+    k = k8.view(F8).double()
+    v = v8.view(F8).double().transpose(2, 3) * vs.double().view(1, -1, 1, 1)
+    P = w.block_table.shape[1]
+    sel = np.broadcast_to(np.arange(P, dtype=np.int32), (4, Hkv, P))
+    if form == "selected":
+        got = [run(w, sel, hosted, fp8=(k8, v8, one, vs)) for hosted in (True, False)]
+    else:
+        out = torch.full_like(w.q, 7.0)
+        args = (w.q, k8, v8, one, vs, w.block_table, w.context_lens, w.scale, out)
+        if form == "plain":
+            pdattn.decode_fp8(*args, pdattn.alloc_workspace(4, Hq, Hkv, d, bs))
+        elif form == "scored":
+            pdattn.decode_scored_fp8(*args, pdattn.alloc_workspace(4, Hq, Hkv, d, bs), pdattn.Score())
+        else:
+            pre = i32([150, 0])
+            ws = pdattn.alloc_grouped_workspace(4, Hq, Hkv, d, bs)
+            pdattn.decode_grouped_fp8(*args, ws, w.context_lens_host, 2, pre, pre.cpu().numpy())
+        got = [out]
+    want, size = reference(w, sel, k, v)
+    for out in got:
+        out = out.double().cpu().numpy()
+        assert np.isfinite(out).all()
+        # weights fp16, 2^-11 of each while they are normal, that is down to 2^-29 of the largest (20 nats); from there on off by at most half
+        # of fp16's least step, 2^-25, beside a largest of 2^15: 2^-40 of that, 2^-40 e^nats of such a weight.  Scores and sums as in close()
+        weights = max(2.0 ** -11, 2.0 ** -40 * math.exp(nats))
+        tol = 2.0 ** -8 * abs(want) + (weights + 2.0 ** -12) * size + 1e-30
+        assert (abs(out - want) <= tol).all(), (abs(out - want) / tol).max()
