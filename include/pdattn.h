@@ -54,7 +54,8 @@ typedef int pdattn_status;
 #define PDATTN_OUT_OF_PAGES        (-9) /* reported by pdattn_check(): pdattn_pages_reserve / _fork asked for
                                            more pages than the pool holds; nothing was changed       */
 #define PDATTN_BAD_SEQUENCE       (-10) /* reported by pdattn_check(): a page operation was given a row it
-                                           cannot serve (out of range, not empty, named twice, too long) */
+                                           cannot serve (out of range, not empty, named twice, too long),
+                                           or a call over trees a range of tokens or a path that is none */
 
 typedef struct CUstream_st* pdattn_stream_t; /* a cudaStream_t */
 
@@ -349,7 +350,8 @@ pdattn_status pdattn_decode_scored_fp8(const pdattn_args* args, const pdattn_sco
  *     the end).  What it sees does, as in pdattn_score_args.
  *   - Bad page ids and contexts longer than their table row: as in pdattn_decode_ex without a host copy of the lengths.
  *   - A sequence with more than max_tree_tokens tokens is left out, its rows of out as they were, and pdattn_check reports
- *     PDATTN_UNSUPPORTED.  Rows of out at or past cu_tokens[num_seqs] are left as they were.
+ *     PDATTN_UNSUPPORTED.  So is one whose cu_tokens descend or lie outside 0 .. num_tokens: PDATTN_BAD_SEQUENCE.  Rows of out at or
+ *     past cu_tokens[num_seqs] are left as they were.
  *   - Requirements: num_seqs <= 65536; args->workspace holds pdattn_tree_workspace_size() bytes; pdattn_workspace_init before its
  *     first use, and calls that share it must not overlap.  The order of every sum is fixed by lengths and sizes: results are
  *     bit-identical from run to run and under any renumbering of the pages.
@@ -660,7 +662,8 @@ pdattn_status pdattn_set_prefix_engine(int engine);
  * error word (hence a non-const pointer).  Returns PDATTN_OK, PDATTN_BAD_PAGE_INDEX, PDATTN_DEVICE_TIMEOUT, or
  * PDATTN_UNSUPPORTED when the device-side planner refused a batch of more than 2^30 tiles (with
  * context_lens_host the call itself returns PDATTN_INVALID_ARG for such a batch), which then computed nothing, or when
- * pdattn_decode_tree met a tree of more than max_tree_tokens tokens.
+ * pdattn_decode_tree met a tree of more than max_tree_tokens tokens; PDATTN_BAD_SEQUENCE and PDATTN_OUT_OF_PAGES as the calls
+ * that raise them say.
  * workspace: DEVICE.
  */
 pdattn_status pdattn_check(void* workspace, pdattn_stream_t stream);

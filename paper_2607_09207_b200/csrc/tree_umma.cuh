@@ -220,20 +220,26 @@ __host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N) {
 // What the batch asks of one sequence.
 struct TreeSeq {
   int n, row0, L, keys, tiles, units;
+  int wrong;                     // why it is left out (an error bit), or 0
 };
 template <bool PAIR>
 __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& P, int s) {
   TreeSeq q;
-  q.units = q.tiles = q.n = q.row0 = q.L = q.keys = 0;
+  q.units = q.tiles = q.n = q.row0 = q.L = q.keys = q.wrong = 0;
   if (s >= P.S) return q;
   q.row0 = __ldg(P.cu_tokens + s);
-  q.n = __ldg(P.cu_tokens + s + 1) - q.row0;
+  const int row1 = __ldg(P.cu_tokens + s + 1);
+  if (row1 != q.row0) {
+    if (q.row0 < 0 || row1 < q.row0 || row1 > P.N) q.wrong = ERR_BAD_SEQUENCE;     // not a range of the call's tokens
+    else if (row1 - q.row0 > P.max_n) q.wrong = ERR_TOO_LARGE;
+    else q.n = row1 - q.row0;
+  }
   q.L = max(0, __ldg(P.context_lens + s));
   // tokens past the end of the table row are left out like those of a bad page
   q.keys = static_cast<int>(min(static_cast<int64_t>(q.L), static_cast<int64_t>(P.MB) << P.bs_log2));
   q.tiles = static_cast<int>((static_cast<int64_t>(q.keys) + kTreeKeys - 1) / kTreeKeys);
   const int tokens = PAIR ? 2 * P.TQ : P.TQ;
-  if (q.row0 >= 0 && q.n > 0 && q.n <= P.max_n && static_cast<int64_t>(q.row0) + q.n <= P.N) q.units = (q.n + tokens - 1) / tokens * P.Hkv;
+  q.units = (q.n + tokens - 1) / tokens * P.Hkv;
   return q;
 }
 
@@ -339,7 +345,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       chunk_cost[c] = cost;
       chunk_units[c] = units;
     }
-    if (q.n > P.max_n && blockIdx.x == 0) atomicOr(&P.hdr->err, ERR_TOO_LARGE);
+    if (q.wrong && blockIdx.x == 0) atomicOr(&P.hdr->err, q.wrong);
   }
   tc_fence_before();
   __syncthreads();

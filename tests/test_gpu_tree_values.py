@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_tree import Case, close
+from paper_2607_09207_b200 import pdattn
+from test_gpu_tree import Case, close, i32
 
 pytestmark = pytest.mark.gpu
 
@@ -136,3 +137,26 @@ def test_scores_that_grow_and_are_large(n):
         close(c.run(), *c.want(), True)
     c.q.mul_(512.0)                                          # one tile's keys, equal among themselves, take all
     close(c.run(), *c.want(), True)
+
+
+@pytest.mark.parametrize("top", [8, 64])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_ranges_of_tokens_that_are_none(top, fp8):
+    """A sequence whose tokens are not all among the call's is left out, as before, and reported; the others are served."""
+    n, L = np.array([5, 6, 3]), np.array([100, 260, 40])
+    for cu, good in (([0, 5, 11, 15], (0, 1)), ([0, 5, 11, 1 << 30], (0, 1)), ([-1, 5, 11, 14], (1, 2)), ([0, 5, 4, 4], (0,)),
+                     ([-(1 << 31), 5, 11, 14], (1, 2)), ([0, 5, 11, -(1 << 31)], (0, 1))):
+        c = Case(n, L, 8, 2, 64, 16, fp8=fp8).upload()
+        want, size = c.want()
+        out = torch.full_like(c.q, 7.0)
+        c.dev_cu = i32(cu)
+        c.call(out, top)
+        assert pdattn.check(c.ws) == pdattn.BAD_SEQUENCE, cu
+        rows = np.concatenate([np.arange(int(c.cu[s]), int(c.cu[s + 1])) for s in good])
+        close(out[rows], want[rows], size[rows], fp8)
+        assert (out[np.setdiff1d(np.arange(14), rows)] == 7).all()
+        out.fill_(7.0)                                       # (the workspace is as good as new)
+        c.dev_cu = i32(c.cu)
+        c.call(out, top)
+        assert pdattn.check(c.ws) == pdattn.OK
+        close(out, want, size, fp8)
