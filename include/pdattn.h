@@ -403,7 +403,8 @@ typedef struct {
   void* workspace;                  /* DEVICE, may be NULL: its error word, as in pdattn_rope_args     */
 } pdattn_summary_args;
 /* The pages that the last n_s of context_lens[s] tokens filled: page b of the sequence with
- * context_lens[s] - n_s < (b + 1) * block_size <= context_lens[s].  cu_tokens as in pdattn_rope_append (NULL: one token each). */
+ * context_lens[s] - n_s < (b + 1) * block_size <= context_lens[s].  cu_tokens as in pdattn_rope_append (NULL: one token each);
+ * num_tokens is cu_tokens[num_seqs] or more: sequences with tokens past it are left out, PDATTN_BAD_SEQUENCE from pdattn_check. */
 pdattn_status pdattn_summarize_append(const pdattn_summary_args* args, const int32_t* block_table, const int32_t* context_lens,
                                       const int32_t* cu_tokens, int num_tokens, int num_seqs, int max_blocks_per_seq,
                                       pdattn_stream_t stream);

@@ -158,6 +158,8 @@ summarize_kernel(const __grid_constant__ SummaryParams P) {
   } else {
     int s = slot, n = 1, k = 0;
     if (P.cu) {
+      // (tokens past the call's number are left out, with the sequences they belong to)
+      if (slot == 0 && threadIdx.x == 0 && P.err && __ldg(P.cu + P.S) > P.n) atomicOr(P.err, ERR_BAD_SEQUENCE);
       int lo = 0, len = P.S;                           // the last sequence whose first slot is at or before this one
       while (len > 1) {
         const int step = (len + 31) / 32, i = lane * step;

@@ -7,7 +7,7 @@ import torch
 
 from paper_2607_09207_b200 import pdattn
 from paper_2607_09207_b200 import workloads as W
-from test_gpu_sparse import F8, i32, reference, run
+from test_gpu_sparse import F8, i32, pool, reference, run
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,21 @@ def test_many_small_weights_over_codes(nats, form):
         weights = max(2.0 ** -11, 2.0 ** -40 * math.exp(nats))
         tol = 2.0 ** -8 * abs(want) + (weights + 2.0 ** -12) * size + 1e-30
         assert (abs(out - want) <= tol).all(), (abs(out - want) / tol).max()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_new_tokens_past_their_number_are_reported(fp8):
+    """num_tokens below cu_tokens[S]: what lies past it is left out, and said so."""
+    bs, d, Hkv = 16, 64, 2
+    n = np.array([20, 40, 40])
+    L = n + np.array([3, 0, 9])
+    k, scale = pool(20, Hkv, bs, d, seed=3, fp8=fp8)
+    table = np.arange(18).reshape(3, 6)
+    ws = torch.zeros(8448, dtype=torch.uint8, device="cuda")
+    for num, served in ((100, 3), (101, 3), (99, 2), (60, 2), (59, 1), (1, 0)):
+        s = pdattn.PageSummary.create(20, Hkv, d)
+        s.exponents.fill_(99)
+        pdattn.summarize_append(k, s, i32(table), i32(L), cu_tokens=i32([0, 20, 60, 100]), num_tokens=num, k_scale=scale, workspace=ws)
+        assert pdattn.check(ws) == (pdattn.OK if served == 3 else pdattn.BAD_SEQUENCE), num
+        filled = {int(table[r, b]) for r in range(served) for b in range((L[r] - n[r]) // bs, L[r] // bs)}
+        assert set(np.flatnonzero((s.exponents.cpu().numpy() != 99).any(1)).tolist()) == filled, num
