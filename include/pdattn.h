@@ -420,7 +420,9 @@ pdattn_status pdattn_summarize_pages(const pdattn_summary_args* args, const int3
  * with equal scores in ascending order of b.  lo, hi, e_b: the page's summary (exponent 127: the score is infinite); e_h is the smallest
  * exponent in -40 .. 40 with max |q_h| <= 127 * 2^e_h and c_h = q_h / 2^e_h rounded to nearest even, within +-127.  A head with an
  * element that is not finite takes no part.  Scores are exact, so the choice depends on nothing but the inputs.
- *   - A used table entry that is no page: lowest score, error word set.  Tokens past the table row are left out, error word set.
+ *   - A table entry with a score that is no page: lowest score, error word set.  The entries of pages that are taken in any case (the
+ *     first, the last, and all where n <= num_selected) are not looked at: pdattn_decode_selected reports those.  Tokens past the
+ *     table row are left out, error word set.
  */
 typedef struct {
   const void* q;                    /* DEVICE bf16 [num_seqs, num_q_heads, head_dim], dense           */

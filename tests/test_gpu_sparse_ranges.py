@@ -7,7 +7,7 @@ import torch
 
 from paper_2607_09207_b200 import pdattn
 from paper_2607_09207_b200 import workloads as W
-from test_gpu_sparse import F8, i32, pool, reference, run
+from test_gpu_sparse import F8, close, i32, pool, reference, run
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +76,22 @@ def test_new_tokens_past_their_number_are_reported(fp8):
         assert pdattn.check(ws) == (pdattn.OK if served == 3 else pdattn.BAD_SEQUENCE), num
         filled = {int(table[r, b]) for r in range(served) for b in range((L[r] - n[r]) // bs, L[r] // bs)}
         assert set(np.flatnonzero((s.exponents.cpu().numpy() != 99).any(1)).tolist()) == filled, num
+
+
+def test_pages_without_a_score_are_the_steps_to_report():
+    """The choice looks at the table entries it scores; those it takes in any case go on as they are, and the step reports them."""
+    w = W.make_custom([40 * 16, 5 * 16], 4, 2, 64, 16, device="cuda:0")
+    s = pdattn.PageSummary.create(w.num_blocks, 2, 64)
+    pdattn.summarize_pages(w.k_cache, s, i32(np.arange(w.num_blocks)))
+    w.block_table[0, 0], w.block_table[0, 39], w.block_table[1, 2] = w.num_blocks + 3, -9, -1
+    sel = torch.zeros(2, 2, 10, dtype=torch.int32, device="cuda")
+    ws = pdattn.alloc_select_workspace(2, 2, w.block_table.shape[1])
+    pdattn.select_pages(w.q, s, w.block_table, w.context_lens, sel, 16, ws, num_first=1, num_recent=1)
+    assert pdattn.check(ws) == pdattn.OK
+    assert (sel[0, :, 0] == 0).all() and (sel[0, :, 9] == 39).all() and (sel[1, :, :5].cpu() == torch.arange(5)).all()
+    host_sel = sel.cpu().numpy()
+    out = run(w, host_sel, hosted=False, expect=pdattn.BAD_PAGE_INDEX)
+    left = host_sel.copy()
+    left[0, :, [0, 9]] = -1
+    left[1, :, 2] = -1
+    close(out, *reference(w, left), 2.0 ** -15)
