@@ -7,7 +7,7 @@ import torch
 
 from paper_2607_09207_b200 import pdattn
 from paper_2607_09207_b200 import workloads as W
-from test_gpu_sparse import F8, close, i32, pool, reference, run
+from test_gpu_sparse import F8, chosen, close, host, i32, pool, reference, run, run_select, select_case
 
 pytestmark = pytest.mark.gpu
 
@@ -95,3 +95,32 @@ def test_pages_without_a_score_are_the_steps_to_report():
     left[0, :, [0, 9]] = -1
     left[1, :, 2] = -1
     close(out, *reference(w, left), 2.0 ** -15)
+
+
+@pytest.mark.parametrize("S,pages", [(37, 2049), (74, 2049), (148, 2049), (148, 2048), (148, 2047)])
+def test_selection_where_the_blocks_shares_change(S, pages):
+    """As many (sequence, head) pairs as make a block score 512, 1024 and 2048 pages at a time; rows of 2047, 2048 and 2049 pages with a
+    score among them, so that a row is one block's or two blocks' work, and a block's keys lie in its shared memory or not."""
+    Hkv, first, recent = 4, 1, 2
+    r = np.random.default_rng(S)
+    rows = r.integers(1, 300, S)
+    rows[:6] = [pages, 2047, 2048, min(pages, 2049), 513, 1025]
+    rows[-2:] = [512, pages]
+    rows = np.minimum(rows, pages) + first + recent
+    L = rows * 16 - r.integers(0, 16, S)
+    q, s, table = select_case(L, 8, Hkv, 64, 16, seed=S + pages, NB=5000, MB=pages + first + recent)
+    got, st = run_select(q, s, table, L, 16, 40, first, recent)
+    assert st == pdattn.OK
+    some = np.r_[0:10, S - 4:S]
+    assert (got[some] == chosen(q[some].double().cpu().numpy(), *host(q, s)[1:], table[some], L[some], 16, 40, first, recent)).all()
+
+
+def test_long_rows_beside_more_units_than_the_workspace_numbers():
+    """Above 2048 (sequence, head) pairs a block has a whole one, and its keys in memory where they are more than 2048."""
+    L = np.random.default_rng(1).integers(1, 60 * 16, 700)
+    L[[0, 1, 2, 350, 699]] = np.array([2200, 2052, 2051, 2199, 2050]) * 16
+    q, s, table = select_case(L, 3, 3, 64, 16, seed=9, NB=4000)
+    got, st = run_select(q, s, table, L, 16, 24, 1, 1)
+    some = np.r_[0:5, 345:355, 690:700]
+    assert st == pdattn.OK
+    assert (got[some] == chosen(q[some].double().cpu().numpy(), *host(q, s)[1:], table[some], L[some], 16, 24, 1, 1)).all()
