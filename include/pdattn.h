@@ -371,6 +371,8 @@ pdattn_status pdattn_decode_tree_fp8(const pdattn_args* args, const int32_t* cu_
  *   - The path ascends strictly and names tokens of the tree; otherwise (or with a count below 0 or past n_s) the sequence is left
  *     as it is: PDATTN_BAD_SEQUENCE from pdattn_check.  The same with PDATTN_BAD_PAGE_INDEX where a page that is read or written is
  *     no page.  Pages that are written must be owned by one sequence only.
+ *   - Whole pages among those that are written get other keys: summaries of them (pdattn_summarize_append) come after this call and
+ *     the trim, with the accepted counts in cu_tokens' place.
  *   - element_bytes and strides as in pdattn_pages_copy; workspace (may be NULL) as in pdattn_rope_args.
  */
 pdattn_status pdattn_tree_accept(void* k_cache, void* v_cache, const int32_t* block_table, const int32_t* context_lens,
@@ -390,7 +392,8 @@ pdattn_status pdattn_tree_accept(void* k_cache, void* v_cache, const int32_t* bl
  *   exponents[page][head] = e;   a page with a key that is not finite: codes 0, exponent 127.
  * (fp8 cache: k = k_scale * code, one fp32 product.)  A summary belongs to its page: rows that share the page share it, and a page
  * that is copied or moved (pdattn_pages_fork copies partial pages only; pdattn_pages_compact moves whole ones) is summarised
- * again at its new place, with pdattn_summarize_pages over copy_dst.
+ * again at its new place, with pdattn_summarize_pages over copy_dst.  Drafted tokens are not summarised when they are appended but
+ * when their path has been taken over (pdattn_tree_accept) and the sequence is as long as it stays.
  */
 typedef struct {
   const void* k_cache;              /* DEVICE bf16 with the strides below, or the K pool of pdattn_decode_fp8   */

@@ -792,7 +792,8 @@ def _expect_pools(where, k_cache, v_cache):
 def tree_accept(k_cache, v_cache, block_table, context_lens, cu_tokens, accepted, accepted_counts, workspace=None, stream=None,
                 check: bool = True) -> int:
     """pdattn_tree_accept: K and V of the tree's tokens accepted[s, :accepted_counts[s]] (int32 [S, M], [S]) move to the front of the tree's
-    slots, in bf16 caches or the uint8 code pools of decode_fp8; the lengths stay."""
+    slots, in bf16 caches or the uint8 code pools of decode_fp8; the lengths stay.  Pages are summarised after this and pages_trim, by
+    summarize_append with the accepted counts."""
     where = "pdattn_tree_accept"
     _expect_dense(where, torch.int32, block_table, context_lens, cu_tokens, accepted, accepted_counts)
     _expect_pools(where, k_cache, v_cache)
@@ -854,7 +855,7 @@ def _summary_args(where, k_cache, summary: PageSummary, k_scale, workspace) -> S
 def summarize_append(k_cache, summary: PageSummary, block_table, context_lens, cu_tokens=None, num_tokens: Optional[int] = None, k_scale=None,
                      workspace=None, stream=None, check: bool = True) -> int:
     """pdattn_summarize_append: summaries of the pages that the last cu_tokens[s + 1] - cu_tokens[s] tokens of every sequence filled (None:
-    one token each).  num_tokens, needed with cu_tokens: cu_tokens[S], or more."""
+    one token each).  num_tokens, needed with cu_tokens: cu_tokens[S], or more.  Not for drafted tokens (see tree_accept)."""
     where = "pdattn_summarize_append"
     _expect_dense(where, torch.int32, block_table, context_lens, cu_tokens)
     a = _summary_args(where, k_cache, summary, k_scale, workspace)

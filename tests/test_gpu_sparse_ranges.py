@@ -7,7 +7,7 @@ import torch
 
 from paper_2607_09207_b200 import pdattn
 from paper_2607_09207_b200 import workloads as W
-from test_gpu_sparse import F8, chosen, close, host, i32, pool, reference, run, run_select, select_case
+from test_gpu_sparse import F8, chosen, close, host, i32, keys_of, pool, reference, run, run_select, select_case, summary_of
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,29 @@ def test_long_rows_beside_more_units_than_the_workspace_numbers():
     some = np.r_[0:5, 345:355, 690:700]
     assert st == pdattn.OK
     assert (got[some] == chosen(q[some].double().cpu().numpy(), *host(q, s)[1:], table[some], L[some], 16, 24, 1, 1)).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_a_draft_is_summarised_once_its_path_has_been_taken(fp8):
+    """The accepted path overwrites slots of whole pages: their summaries follow it, by the accepted counts."""
+    bs, d, Hkv, n, L = 16, 64, 2, np.array([16, 5]), np.array([36, 16])
+    path = np.array([[0, 3, 4, 5, 7, 8, 9, 10, 12, 13, 14, 15], [1] + [-1] * 11])
+    count = np.array([12, 1])                                       # 32 and 12 tokens stay
+    k, scale = pool(8, Hkv, bs, d, seed=2, fp8=fp8)
+    v = torch.zeros(8, Hkv, *((d, bs) if fp8 else (bs, d)), device="cuda", dtype=k.dtype)
+    table, lens = i32([[4, 1, 6], [2, 3, 5]]), i32(L)
+    s = pdattn.PageSummary.create(8, Hkv, d)
+    ws = torch.zeros(8448, dtype=torch.uint8, device="cuda")
+    cu = i32(np.concatenate([[0], np.cumsum(n)]))
+    pdattn.summarize_pages(k, s, i32([4, 1]), k_scale=scale)
+    old = s.codes[1].clone()
+    pdattn.tree_accept(k, v, table, lens, cu, i32(path), i32(count), workspace=ws)
+    lens = i32(L - n + count)
+    s.exponents.fill_(99)
+    pdattn.summarize_append(k, s, table, lens, cu_tokens=i32([0, 12, 13]), num_tokens=13, k_scale=scale, workspace=ws)
+    assert pdattn.check(ws) == pdattn.OK
+    for h in range(Hkv):
+        want = summary_of(keys_of(k, 1, h, scale))
+        assert (s.codes[1, h].cpu().numpy() == want[0]).all() and int(s.exponents[1, h]) == want[1]
+    assert not torch.equal(old, s.codes[1])
+    assert (s.exponents[[0, 2, 3, 4, 5, 6, 7]] == 99).all()         # (page 2 of the second sequence is not whole any more)
