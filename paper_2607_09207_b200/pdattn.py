@@ -761,7 +761,8 @@ def _tree(where, call, q, a: Args, cu_tokens, tree_mask, max_tree_tokens, scales
 def decode_tree(q, k_cache, v_cache, block_table, context_lens, cu_tokens, tree_mask, scale, out, workspace, *,
                 max_tree_tokens: int = 64, stream=None, check: bool = True) -> int:
     """pdattn_decode_tree: q and out [N, Hq, d]; the drafted tokens cu_tokens[s] .. cu_tokens[s + 1] are the last ones of sequence s's
-    context_lens[s], and token j of them sees token i of the tree where bit i of its tree_mask (int64 or uint64 [N]) is set."""
+    context_lens[s], and token j of them sees token i of the tree where bit i of its tree_mask (int64 or uint64 [N]) is set.  Give the
+    batch's max_tree_tokens where it is known: small trees take longer in the form for 64 (256 of 8 tokens 270 us in place of 238)."""
     where = "pdattn_decode_tree"
     _expect_caches(where, k_cache, v_cache)
     a = _step_args(where, q, k_cache, v_cache, k_cache.stride()[:3], block_table, context_lens, scale, out, workspace)
