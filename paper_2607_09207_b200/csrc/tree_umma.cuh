@@ -31,12 +31,14 @@
 // in the second product.
 //
 // Numbers: scores, maxima, sums and O in fp32.  The weights are rounded to bf16 for the second product (at most 2^-8 of each,
-// independent): the size of the final rounding.  The reference of the online softmax follows the running maximum when that grew by
+// independent): the size of the final rounding.  (Two terms, as the single-token steps have them, would cost half as much tensor work
+// again, where the products are a third to two thirds of a key tile's time.)  In the paired form a quarter of the exponentials is a
+// polynomial good to 2^-18.5, the others to 2^-22.  The reference of the online softmax follows the running maximum when that grew by
 // more than 2^8, so O is rarely rescaled.  The fp8 form rounds them to fp16 (2^-11 of each), whose range is short: all carry a factor
 // 2^11, which l and O then have alike, and the reference, a whole number at or above the maximum when it moves, lags by 2^4 at most.
 // So weights end at 2^15 and have all bits down to 2^-24 of the row's largest; smaller ones are off by at most 2^-35 of it.  (With plain
 // weights what lies 2^-25 below vanished, and with it what thousands of keys 17 below the largest score add up to.)  All rows of a warp
-// move their references when one must: the factors are powers of two, so that changes no bit of them, and there are fewer moves (each
+// move their references when one must: the factors are powers of two, so that changes no bit of normal weights, and there are fewer moves (each
 // row by itself, with a lag of 2^2: 304 -> 342 us for 32 x 16 tokens).
 //
 // Bound and times (replays of a graph; in brackets under the power cap, which long runs of this kernel reach):
@@ -44,7 +46,7 @@
 //       to the next (the groups meet, results), 0.65 a key tile
 //   8 x 64 over up to 32,000, 64/8 heads    324 us [385]   0.94 PFLOP/s: the chain of a group, scores -> weights -> product; a
 //       key tile takes a pair of row tiles 1950 cycles, 1280 of them MMAs (48 cycles one of scores: 128 x 16 x 64, Q from shared memory)
-//   32 x 16 over up to 32,767, e4m3 codes, 64/8 heads    304 us [356]   the same; 1190 cycles a key tile, 640 of them MMAs
+//   32 x 16 over up to 32,767, e4m3 codes, 64/8 heads    307 us [360]   the same; 1190 cycles a key tile, 640 of them MMAs
 // Built and not faster: key tiles of 128 read twice (8 x 64 417 instead of 385 under the cap), two warps a row (324 -> 372, codes
 // 306 -> 355: the chain's latencies stay and its halves have to meet), the maximum of the tile before, turns at the exponential unit,
 // four loading warps instead of two (256 x 8: the same).  Rows of small trees twice in the row tile, each with half of a tile's keys, so
