@@ -428,8 +428,8 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
       }
       if (aborted) return;
       if constexpr (EB == 1) {
-        // the V scale of this KV head, once per piece: the accumulator is linear in V
-        const float vs = __ldg(P.v_scale + pc.g);
+        // the V scale of this KV head, once per piece: the accumulator is linear in V.  The weights' factor goes with it.
+        const float vs = __ldg(P.v_scale + pc.g) * (1.f / kF8Factor);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -448,7 +448,7 @@ __device__ __forceinline__ void consume_chain(const DecodeParams& P, const PlanP
           v += __shfl_xor_sync(0xffffffffu, v, 4);
           v += __shfl_xor_sync(0xffffffffu, v, 8);
           v += __shfl_xor_sync(0xffffffffu, v, 16);
-          l[nt][e] = v;
+          l[nt][e] = EB == 1 ? v * (1.f / kF8Factor) : v;
         }
 
       // ---- the chain of classes

@@ -198,10 +198,11 @@ prefix_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ C
         v += __shfl_xor_sync(0xffffffffu, v, 4);
         v += __shfl_xor_sync(0xffffffffu, v, 8);
         v += __shfl_xor_sync(0xffffffffu, v, 16);
-        l[0][e] = v;
+        l[0][e] = EB == 1 ? v * (1.f / kF8Factor) : v;
       }
       const int drow = lane >> 2;
-      const float vs = EB == 1 ? __ldg(P.v_scale + g) : 1.f;   // fp8 cache: the accumulator is linear in V
+      // fp8 cache: the accumulator is linear in V; the weights' factor goes with V's scale
+      const float vs = EB == 1 ? __ldg(P.v_scale + g) * (1.f / kF8Factor) : 1.f;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int r = warp * 8 + qcol + e;

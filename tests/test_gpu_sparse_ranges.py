@@ -150,3 +150,37 @@ def test_a_draft_is_summarised_once_its_path_has_been_taken(fp8):
         assert (s.codes[1, h].cpu().numpy() == want[0]).all() and int(s.exponents[1, h]) == want[1]
     assert not torch.equal(old, s.codes[1])
     assert (s.exponents[[0, 2, 3, 4, 5, 6, 7]] == 99).all()         # (page 2 of the second sequence is not whole any more)
+
+
+@pytest.mark.parametrize("form", ["selected", "plain", "grouped", "scored"])
+def test_v_scales_of_any_size(form):
+    """A power of two as V's scale is the results' power of two, bit for bit."""
+    bs, d, Hq, Hkv = 32, 128, 8, 2
+    w = W.make_custom([20000, 20000, 300, 6000, 5, 64], Hq, Hkv, d, bs, seed=6, device="cuda:0")
+    one = torch.ones(2, device="cuda")
+    k8, v8 = W.fp8_caches(w, one, one * 0.03)
+    w.block_table[1, :300] = w.block_table[0, :300]
+    P = w.block_table.shape[1]
+    sel = i32(np.broadcast_to(np.arange(P), (6, Hkv, P)))
+    ws = pdattn.alloc_grouped_workspace(6, Hq, Hkv, d, bs)
+    pre = i32([150, 0, 0])
+
+    def call(vs):
+        out = torch.full_like(w.q, 7.0)
+        args = (w.q, k8, v8, one * 0.05, vs, w.block_table, w.context_lens)
+        if form == "selected":
+            pdattn.decode_selected_fp8(*args, sel, w.scale, out, ws)
+        elif form == "plain":
+            pdattn.decode_fp8(*args, w.scale, out, ws)
+        elif form == "scored":
+            pdattn.decode_scored_fp8(*args, w.scale, out, ws, pdattn.Score(window=5000))
+        else:
+            pdattn.decode_grouped_fp8(*args, w.scale, out, ws, w.context_lens_host, 2, pre, pre.cpu().numpy())
+        assert pdattn.check(ws) == pdattn.OK
+        return out.double()
+    want = call(one)
+    for k in (104, 60, -80):
+        vs = torch.tensor([2.0 ** k, -(2.0 ** k)], device="cuda")
+        out = call(vs)
+        out[:, 4:] = -out[:, 4:]
+        assert torch.equal(out, want * 2.0 ** k), k
