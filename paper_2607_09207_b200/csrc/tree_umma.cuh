@@ -35,7 +35,7 @@
 // again, where the products are a third to two thirds of a key tile's time.)  In the paired form a quarter of the exponentials is a
 // polynomial good to 2^-18.5, the others to 2^-22.  The reference of the online softmax follows the running maximum when that grew by
 // more than 2^8, so O is rarely rescaled.  The fp8 form rounds them to fp16 (2^-11 of each), whose range is short: all carry a factor
-// 2^11, which l and O then have alike, and the reference, a whole number at or above the maximum when it moves, lags by 2^4 at most.
+// 2^11, which l and O have alike within a piece, and the reference, a whole number at or above the maximum when it moves, lags by 2^4 at most.
 // So weights end at 2^15 and have all bits down to 2^-24 of the row's largest; smaller ones are off by at most 2^-35 of it.  (With plain
 // weights what lies 2^-25 below vanished, and with it what thousands of keys 17 below the largest score add up to.)  All rows of a warp
 // move their references when one must: the factors are powers of two, so that changes no bit of normal weights, and there are fewer moves (each
@@ -964,6 +964,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     int c0 = 0;                        // key tiles of the CTA before this item
     uint32_t ns = 0;                   // bit b: parity of s_full (and of p_full, pv_done) of this group's buffer b
     constexpr float kLag = F8 ? 4.f : 8.f, kFactor = 11.f;   // (base 2)
+    constexpr float kUnfactor = F8 ? 1.f / 2048.f : 1.f;     // a piece's results leave without the factor
     for (int k = 0; get_item(k, ip); ++k) {
       const TreeItem& it = *ip;
       const int tb = it.tb, te = it.te, edge = it.edge, rows = it.rows[t], keys = it.keys;
@@ -1114,7 +1115,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
       if (PAIR) {
         have[0] = any && t == 0;
         have[1] = any && t == 1;
-        f[t] = l == 0.f ? kUnseen : whole ? 1.f / l : 1.f;
+        f[t] = l == 0.f ? kUnseen : whole ? 1.f / l : kUnfactor;
       } else {
         const int even = tb + (c0 & 1), odds = tb + ((c0 & 1) ^ 1);
         have[0] = te > even;
@@ -1132,11 +1133,9 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
           f[1] = other.x == NEG_INF ? 0.f : fast_exp2(other.x - M);
           m = M;
           l = l * f[0] + other.y * f[1];
-          if (whole) {
-            const float inv = 1.f / l;                  // (used where something was seen)
-            f[0] *= inv;
-            f[1] *= inv;
-          }
+          const float inv = whole ? 1.f / l : kUnfactor;      // (used where something was seen)
+          f[0] *= inv;
+          f[1] *= inv;
           if (!saw0) f[0] = kUnseen;
           if (!saw1) f[1] = kUnseen;
           ctrl->ml[r] = make_float2(f[0], f[1]);
@@ -1157,7 +1156,7 @@ tree_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         float* part = whole ? nullptr : P.partials + (static_cast<int64_t>(it.part) * 2 + (PAIR ? t : 0)) * ((D + 2) * 128) + r;
         if (part && valid && (PAIR || t == 0)) {
           part[D * 128] = m;
-          part[(D + 1) * 128] = l;
+          part[(D + 1) * 128] = l * kUnfactor;
         }
         __nv_bfloat16* out0 = P.out + (static_cast<int64_t>(it.row0 + it.tok0 + (PAIR ? t * P.TQ : 0)) * P.Hq + it.g * P.G) * D;
         const int offset = valid ? (rj * P.Hq + rh) * D : -1;     // of this thread's row

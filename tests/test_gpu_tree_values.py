@@ -160,3 +160,18 @@ def test_ranges_of_tokens_that_are_none(top, fp8):
         c.call(out, top)
         assert pdattn.check(c.ws) == pdattn.OK
         close(out, want, size, fp8)
+
+
+@pytest.mark.parametrize("n", [4, 64])
+@pytest.mark.parametrize("hist", [200, 9000])
+def test_v_scales_of_any_size(n, hist):
+    """A power of two as V's scale is the results' power of two, bit for bit, whether a unit is cut or not."""
+    ns = np.array([n, 1, n])
+    c = Case(ns, ns + np.array([hist, 3, hist // 3]), 8, 2, 128, 16, seed=7, fp8=True)
+    c.vs.fill_(1.0)
+    one = c.run()
+    for k in (108, 60, -80):
+        c.vs[0], c.vs[1] = 2.0 ** k, -(2.0 ** k)
+        out = c.run().double()
+        out[:, 4:] = -out[:, 4:]
+        assert torch.equal(out, one.double() * 2.0 ** k), k
