@@ -342,9 +342,9 @@ pdattn_status pdattn_decode_scored_fp8(const pdattn_args* args, const pdattn_sco
  *   out[j, h, :] = softmax_t( scale * q[j, h, :] . K[t, h / G, :] ) . V[t, h / G, :]
  * q, out DEVICE bf16 [num_tokens, num_q_heads, head_dim], dense; cu_tokens DEVICE int32 [num_seqs + 1], ascending from 0;
  * tree_mask DEVICE uint64 [num_tokens].  Takes no host copies (args->context_lens_host is not read).  Weights of the softmax are
- * rounded to bf16 for the second product, where the single-token steps and pdattn_decode_multi carry 16 bits of them (over the fp8 cache to fp16: 2^-11 of each down to 2^-24 of the row's largest, 2^-35 of the
- * largest below); fp32 otherwise, but for q over the fp8 cache: there a row is the sum of two e4m3 terms per element, off by at most
- * 2^-17.8 of the row's largest element.
+ * rounded to bf16 for the second product, where the single-token steps and pdattn_decode_multi carry 16 bits of them; over the fp8
+ * cache to fp16, 2^-11 of each down to 2^-24 of the row's largest, 2^-35 of the largest below.  fp32 otherwise, but for q over the fp8
+ * cache: there a row is the sum of two e4m3 terms per element, off by at most 2^-17.8 of the row's largest element.
  *   - A token that sees no key gets zeros, as does one before position 0 (n_s > context_lens[s]).
  *   - What a token does not see never reaches its output, infinities and NaN included (other branches of the tree, slots past
  *     the end).  What it sees does, as in pdattn_score_args.

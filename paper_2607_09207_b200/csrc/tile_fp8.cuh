@@ -13,10 +13,11 @@ namespace pdattn {
 // (V is stored transposed inside a page; with pages of 32 or 64 tokens the 16-byte rows that ldmatrix
 // reads lie 32 or 64 bytes apart and collide two or four ways in the banks).  The codes are widened to fp16 in registers (exact) and both
 // products run as fp16 MMAs; Q arrives as fp16 fragments and P is rounded to fp16 (11 bits, one term).
-// fp16's range is short, so P carries a factor 2^15, which l and the accumulators then have alike; it leaves both with V's scale, at the
-// end of a piece (kept longer, a large V scale would overflow them).  So weights have all bits down to 2^-29 of the largest so far, and smaller ones are off by at most 2^-40 of it.  (Without the factor they lose bits
-// below 2^-14 and vanish below 2^-25, and with them what thousands of keys 17 below the largest score add up to.)  The factor, applied
-// to two weights at once, costs no time: the step over 256 sequences 150 us with it and without.
+// fp16's range is short, so P carries a factor 2^15, which l and the accumulators then have alike; it leaves both with V's scale at the
+// end of a piece (kept longer, a large V scale would overflow them).  So weights have all bits down to 2^-29 of the largest so far, and
+// smaller ones are off by at most 2^-40 of it.  (Without the factor they lose bits below 2^-14 and vanish below 2^-25, and with them what
+// thousands of keys 17 below the largest score add up to.)  Applied to two weights at once it costs no time: the step over 256
+// sequences takes 150 us with it and without.
 // ldmatrix moves 16-bit units, i.e. PAIRS of codes, so a lane receives four consecutive elements of
 // the contraction dimension where the MMA fragment wants two plus two eight further on.  Both
 // products therefore run with the contraction index permuted inside every block of 16:
